@@ -368,6 +368,163 @@ int cola_block_bwd(const cola_block_desc* desc, const cola_block_weights* w, con
                    const void* saved, size_t saved_bytes, const void* dx2, void* dx0,
                    const cola_block_grads* grads, void* ws, size_t ws_bytes, cola_stream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Serving: rotary positions, a paged key/value cache and attention over it.
+ * What a program needs between the projections q, k, v (cola_group_infer) and
+ * o (cola_infer) when it answers requests; the rotation also serves training
+ * (its gradient is cola_rope_bwd).
+ *
+ * The cache.  K and V are [n_pages][heads][page_size][head_dim], contiguous,
+ * 16-byte aligned: in a page, the tokens of one head lie one after the other,
+ * so a head's keys are read in runs of page_size * head_dim elements.  Slot s
+ * is token s % page_size of page s / page_size.  A table is a list of page
+ * numbers: token j of a sequence lies in page table[j / page_size].  page_size
+ * is a power of two from 16 to 4096.  Page numbers and slots are checked on the
+ * GPU: a key in a page outside 0 .. n_pages - 1 is not seen by any query, and a
+ * row with a slot outside the cache is not written.
+ *
+ * Lengths, starts, positions, tables and slots are int32 in GPU memory, read
+ * when the kernels run: a captured graph follows them from replay to replay.
+ * Only the bounds in the descriptors are fixed by the call.
+ * ------------------------------------------------------------------------ */
+
+/* Which elements of a head turn together: element i with i + rot_dim/2 (half,
+ * the decoder block's), or 2i with 2i + 1 (interleaved), i < rot_dim/2. */
+typedef enum { COLA_ROPE_HALF = 0, COLA_ROPE_INTERLEAVED = 1 } cola_rope_layout;
+
+/* Radians per position of pair i, with f_i = base^(-2i/rot_dim):
+ *   NONE        f_i
+ *   LINEAR      f_i / factor (positions interpolated)
+ *   BASE        f_i of base * factor^(rot_dim / (rot_dim - 2)): the slowest pair
+ *               turns factor times slower, the fastest as before
+ *   YARN        (1 - w_i) f_i + w_i f_i / factor with a ramp w_i from 0 to 1
+ *               between the pairs that make `high` and `low` turns in orig_len
+ *               positions: p(t) = rot_dim ln(orig_len / (2 pi t)) / (2 ln base),
+ *               w_i = (i - floor p(high)) / (ceil p(low) - floor p(high)), the
+ *               ends kept within 0 .. rot_dim/2 - 1 (equal ends: 0.001 apart)
+ *               (arXiv 2309.00071); cosine and sine times 1 + 0.1 ln factor
+ *   WAVELENGTH  s_i f_i + (1 - s_i) f_i / factor, s_i = (orig_len f_i / (2 pi) -
+ *               low) / (high - low) kept within 0 .. 1 */
+typedef enum {
+    COLA_ROPE_NONE = 0, COLA_ROPE_LINEAR = 1, COLA_ROPE_BASE = 2, COLA_ROPE_YARN = 3, COLA_ROPE_WAVELENGTH = 4
+} cola_rope_scaling;
+
+typedef struct {
+    int64_t T;                /* rows (tokens); 0 is an empty batch */
+    int64_t heads_q, heads_k; /* heads of q and of k; 0: that tensor is not there (its pointers NULL) */
+    int64_t head_dim;         /* 1 .. 512 */
+    int64_t rot_dim;          /* leading elements of each head that turn: even, 0 .. head_dim; the rest is copied */
+    int64_t seq_len;          /* positions NULL: row t is at position t % seq_len (0: at t) */
+    int64_t ldq, ldk, ldv;    /* row pitches of the inputs, 0 = contiguous (ldv: cola_cache_append) */
+    int64_t ldqo, ldko;       /* row pitches of the outputs, 0 = contiguous */
+    int32_t dtype;            /* cola_dtype */
+    int32_t layout;           /* cola_rope_layout */
+    int32_t scaling;          /* cola_rope_scaling */
+    int32_t reserved;         /* 0 */
+    double base;              /* > 1 */
+    double factor;            /* >= 1 (NONE: not read) */
+    double low, high;         /* YARN, WAVELENGTH: 0 < low < high */
+    double mscale;            /* factor on cosine and sine, 0 = 1 (YARN: 1 + 0.1 ln factor) */
+    int64_t orig_len;         /* YARN, WAVELENGTH: >= 1 */
+} cola_rope_desc;
+
+/* Rows of q [T][ldq] and k [T][ldk] (head h in columns h * head_dim ..) turned
+ * by their positions (int32 [T], negative ones too; NULL: by seq_len) into q_out
+ * [T][ldqo] and k_out [T][ldko].  An output may be its input (same pointer and
+ * pitch); any other overlap is not allowed.  The angle is formed in 64 bits
+ * from frequencies in 64 bits, whatever the dtype; the products are fp32,
+ * rounded once. Rows and pitches of any alignment run at full speed; the
+ * vector width falls with the largest power of two that divides head_dim and
+ * rot_dim / 2. */
+int cola_rope_fwd(const cola_rope_desc* desc, const void* q, const void* k, const int32_t* positions,
+                  void* q_out, void* k_out, cola_stream_t stream);
+/* The gradient: dq_out, dk_out (pitches ldq, ldk) turned back into dq, dk
+ * (pitches ldqo, ldko): the transpose of the forward's linear map. */
+int cola_rope_bwd(const cola_rope_desc* desc, const void* dq_out, const void* dk_out, const int32_t* positions,
+                  void* dq, void* dk, cola_stream_t stream);
+
+typedef struct {
+    int64_t n_pages, page_size;
+    int64_t heads, head_dim;  /* key heads */
+    int32_t dtype;            /* cola_dtype */
+    int32_t reserved;         /* 0 */
+} cola_cache_desc;
+
+/* New tokens on their way to the attention, in one launch: q turned into q_out
+ * (rot's heads_q may be 0: no q), k turned into the cache, v copied into it, row
+ * t at slots[t] (a slot outside the cache: k and v of that row are not written,
+ * q is turned all the same).  rot->heads_k, head_dim and dtype are the cache's;
+ * rot_dim = 0 turns nothing.  Two rows with the same slot leave either row's
+ * elements there. */
+int cola_cache_append(const cola_rope_desc* rot, const cola_cache_desc* cache, const void* q, const void* k,
+                      const void* v, const int32_t* positions, const int32_t* slots, void* q_out, void* K, void* V,
+                      cola_stream_t stream);
+
+/* A step of a batch of requests: where its new tokens go.  Request r holds
+ * kv_len[r] tokens at the end of the step, the last n_new[r] of them new
+ * (n_new outside 0 .. kv_len is taken as the nearer end, a negative kv_len as 0).
+ *   start[r]      the batch's row of r's first new token: n_new summed over the
+ *                 requests before r; start[n_req] is the sum of all
+ *   table[r][j]   for the pages that r needs beyond those of its kv_len - n_new
+ *                 older tokens: the next pages of the free list, in the order of
+ *                 the requests; other entries are read, not written
+ *   slots[t], positions[t]   of the new token in row t: its place in the cache
+ *                 and pos0 + its index in its request; in rows t >= start[n_req]
+ *                 -1 and 0
+ *   free_next[0]  free_at[0] + the number of pages taken from free_pages
+ * free_at[0] (NULL: 0) is the list's first unused entry.  Where the list ends
+ * too early (free_next > n_free) the missing entries are -1, and so are slots in
+ * such pages and slots of tokens past max_pages * page_size; tokens past T have
+ * no row.  free_next must not be free_at: a step that runs twice on the same
+ * inputs writes the same values. */
+typedef struct {
+    int64_t n_req;            /* 0 .. COLA_PAGE_MAP_MAX_REQ */
+    int64_t T;                /* rows of slots and positions */
+    int64_t page_size;        /* a power of two, 1 .. 4096 */
+    int64_t max_pages;        /* entries per row of the table */
+    int64_t n_free;           /* entries of free_pages */
+    int64_t pos0;             /* position of every request's token 0 (the shared prefix's length) */
+} cola_page_map_desc;
+#define COLA_PAGE_MAP_MAX_REQ 4096
+int cola_page_map(const cola_page_map_desc* desc, const int32_t* kv_len, const int32_t* n_new,
+                  const int32_t* free_pages, const int32_t* free_at, int32_t* table, int32_t* start, int32_t* slots,
+                  int32_t* positions, int32_t* free_next, cola_stream_t stream);
+
+/* Attention of a batch whose requests share their first prefix_len tokens, over
+ * the paged cache: the prefix's keys are read once for all rows of the batch.
+ * Request r has its rows (new tokens) in start[r] .. start[r + 1] - 1 (start NULL:
+ * one row each, row r) and kv_len[r] tokens of its own in the cache, in the pages
+ * table[r][..], its new ones the last of them.  Query head h reads key head
+ * h / (heads_q / heads).  Row i of n rows sees the whole prefix and its own
+ * tokens 0 .. kv_len - n + i:
+ *   out = softmax(scale q K^T over the seen keys) V,   lse = ln sum exp(scale q K^T)
+ * (lse fp32 [heads_q][T], or NULL).  A row that sees nothing gets out = 0 and
+ * lse = -inf.  Rows of no request (before start[0], from start[n_req] on, past T)
+ * are left as they were.  What lies in the cache past a row's seen tokens does
+ * not reach it, infinities and NaN included.
+ * max_kv and max_new bound kv_len and a request's rows: tokens past max_kv are not
+ * seen, rows past max_new are left as they were.  They size the launch and the
+ * workspace; lengths below them cost less.  Results depend on the descriptor and
+ * the data alone (fixed order of every sum).
+ * bf16; head_dim 64 or 128; q, out, K, V, ws 16-byte aligned, ldq and ldo
+ * multiples of 8; out must not overlap q.  Products and sums are fp32, the
+ * probabilities rounded to bf16 for the second product. */
+typedef struct {
+    int64_t n_req;            /* requests, 0 .. 65535 */
+    int64_t T;                /* rows of q and out; T * heads_q < 2^31 */
+    int64_t heads_q;          /* a multiple of the cache's heads */
+    int64_t prefix_len;       /* tokens in the pages of prefix_table (0: NULL) */
+    int64_t max_kv;           /* largest kv_len (0: table and kv_len may be NULL) */
+    int64_t max_new;          /* most rows of one request (>= 1) */
+    int64_t max_pages;        /* entries per row of table, 0 = as many as max_kv needs */
+    int64_t ldq, ldo;         /* row pitches, 0 = heads_q * head_dim */
+    double scale;             /* 0 = 1 / sqrt(head_dim); not negative */
+} cola_prefix_attn_desc;
+size_t cola_prefix_attn_workspace_bytes(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache);
+int cola_prefix_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, const void* q, const void* K,
+                     const void* V, const int32_t* prefix_table, const int32_t* table, const int32_t* kv_len,
+                     const int32_t* start, void* out, float* lse, void* ws, size_t ws_bytes, cola_stream_t stream);
+
 /* Tuning options, process-wide (every GPU and thread of the process), read
  * at each call; for tuning, comparisons and tests, not needed for correct
  * results.  Every setting gives results within the stated tolerances;
@@ -422,7 +579,12 @@ typedef enum {
     COLA_KC_NORM = 16,     /* block: RMSNorm forward (+ residual sum)     */
     COLA_KC_NORM_BWD = 17, /* block: RMSNorm backward (+ residual grad)   */
     COLA_KC_POINTWISE = 18,/* block: gated product, residual add, sigma   */
-    COLA_KC_COUNT = 19
+    COLA_KC_ROPE = 19,     /* serving: rotation of q and k, either way    */
+    COLA_KC_APPEND = 20,   /* serving: rotated q, k and v into the cache  */
+    COLA_KC_PAGE_MAP = 21, /* serving: tables, slots, positions           */
+    COLA_KC_PREFIX_ATTN = 22, /* serving: attention over prefix and own tokens */
+    COLA_KC_PREFIX_JOIN = 23, /* serving: its partial results joined      */
+    COLA_KC_COUNT = 24
 } cola_kernel_class;
 
 /* Per-class totals since the last reset: launches, elapsed milliseconds,

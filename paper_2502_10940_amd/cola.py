@@ -27,7 +27,8 @@ WS_LEAN = 16                  # COLA_WS_LEAN: added to a phase, the least worksp
 
 KERNEL_CLASSES = ("fwd_z_sigma", "fwd_y", "bwd_dz", "bwd_dx", "bwd_da", "bwd_db",
                   "reduce_splits", "dense_fwd", "dense_dx", "dense_dw", "fill_zero", "infer_h",
-                  "outer_grad", "bwd_da_db", "attn_fwd", "attn_bwd", "norm", "norm_bwd", "pointwise")
+                  "outer_grad", "bwd_da_db", "attn_fwd", "attn_bwd", "norm", "norm_bwd", "pointwise",
+                  "rope", "cache_append", "page_map", "prefix_attn", "prefix_join")
 
 
 class ColaError(RuntimeError):
@@ -80,6 +81,34 @@ class BlockGrads(ctypes.Structure):
 BLOCK_SLOTS = ("x1", "Z_qkv", "Z_o", "Z_gu", "Z_down", "a", "H_qkv", "q", "k", "v", "att", "lse", "H_o", "b",
                "H_gu", "gate", "up", "m", "H_down")
 
+# serving: rotary positions, the paged cache, attention behind a shared prefix
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "yarn": 3, "wavelength": 4}
+PAGE_MAP_MAX_REQ = 4096
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "heads_q", "heads_k", "head_dim", "rot_dim", "seq_len", "ldq", "ldk",
+                                              "ldv", "ldqo", "ldko")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "layout", "scaling", "reserved")] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "low", "high", "mscale")] + \
+               [("orig_len", ctypes.c_int64)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_pages", "page_size", "heads", "head_dim")] + \
+               [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class PageMapDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_req", "T", "page_size", "max_pages", "n_free", "pos0")]
+
+
+class PrefixAttnDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_req", "T", "heads_q", "prefix_len", "max_kv", "max_new", "max_pages",
+                                              "ldq", "ldo")] + [("scale", ctypes.c_double)]
+
+
 _lib = None
 
 _P = ctypes.c_void_p
@@ -119,6 +148,13 @@ EXPORTS = {
                        ctypes.c_int),
     "cola_block_bwd": ([ctypes.POINTER(BlockDesc), ctypes.POINTER(BlockWeights), _P, _P, _SZ, _P, _P,
                         ctypes.POINTER(BlockGrads), _P, _SZ, _P], ctypes.c_int),
+    "cola_rope_fwd": ([ctypes.POINTER(RopeDesc), _P, _P, _P, _P, _P, _P], ctypes.c_int),
+    "cola_rope_bwd": ([ctypes.POINTER(RopeDesc), _P, _P, _P, _P, _P, _P], ctypes.c_int),
+    "cola_cache_append": ([ctypes.POINTER(RopeDesc), ctypes.POINTER(CacheDesc)] + [_P] * 9, ctypes.c_int),
+    "cola_page_map": ([ctypes.POINTER(PageMapDesc)] + [_P] * 10, ctypes.c_int),
+    "cola_prefix_attn_workspace_bytes": ([ctypes.POINTER(PrefixAttnDesc), ctypes.POINTER(CacheDesc)], _SZ),
+    "cola_prefix_attn": ([ctypes.POINTER(PrefixAttnDesc), ctypes.POINTER(CacheDesc)] + [_P] * 10 + [_SZ, _P],
+                         ctypes.c_int),
     "cola_set_option": ([ctypes.c_int, ctypes.c_int], ctypes.c_int),
     "cola_get_option": ([ctypes.c_int], ctypes.c_int),
 }
@@ -624,3 +660,201 @@ def block_bwd(d: BlockDesc, w: dict, x0, saved, dx2, dx0, grads: dict, ws, saved
     G = BlockGrads(*[_ptr(grads[n]) for n in BLOCK_PARAMS])
     _check(lib().cola_block_bwd(ctypes.byref(d), ctypes.byref(W), _ptr(x0), _ptr(saved), saved_bytes, _ptr(dx2),
                                 _ptr(dx0), ctypes.byref(G), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# serving (cola_rope_*, cola_cache_append, cola_page_map, cola_prefix_attn)
+# ---------------------------------------------------------------------------
+
+def _one_device(named):
+    """Every tensor on the current device: a kernel launched here reads no other GPU's memory."""
+    _on_gpu(named)
+    import torch
+    for name, t in named:
+        if t is not None and not isinstance(t, int) and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name}: tensor is on {t.device}, the call runs on cuda:{torch.cuda.current_device()}")
+
+
+def _try_here(name, stream, args):
+    """_try for the serving calls, which also see that every tensor is on the current device."""
+    m = _native if _native is not None else _native_calls()
+    if not m:
+        return False
+    import torch
+    if not torch.cuda.is_initialized():
+        return False
+    here = _device()
+    if stream is None:
+        stream = _raw_stream(here)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    st = getattr(m, name)(*args, here, stream)
+    if st is None:
+        return False
+    if st != OK:
+        _check(st)
+    return True
+
+
+def _need_rows(name, t, rows, width, ld, dtype):
+    """_need for kernels that read no padding: the last row ends with its `width` elements."""
+    if isinstance(t, int) or t is None or rows == 0:
+        return
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor or an integer device pointer")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, the descriptor needs {dtype}")
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < width:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} is not [{rows}][{width}]")
+    if t.stride(1) != 1 or (rows > 1 and t.stride(0) != ld):
+        raise ValueError(f"{name}: strides {t.stride()} do not match a row pitch of {ld} elements with contiguous rows")
+
+
+def _need_flat(name, t, shape, dtype):
+    """t must be a contiguous tensor of `dtype` with at least `shape` (its last
+    dimensions exactly): [n] of n or more, [rows][width] of rows or more.  The
+    library knows where None is allowed."""
+    if t is None or isinstance(t, int):
+        return
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor or an integer device pointer")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, the call needs {dtype}")
+    if t.dim() != len(shape) or t.shape[0] < shape[0] or tuple(t.shape[1:]) != tuple(shape[1:]) or not t.is_contiguous():
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}, the call needs contiguous {tuple(shape)}")
+
+
+def rope_desc(T, heads_q, heads_k, head_dim, rot_dim=None, dtype="bf16", layout="half", scaling="none", base=10000.0,
+              factor=1.0, orig_len=0, low=0.0, high=0.0, mscale=0.0, seq_len=0, ldq=0, ldk=0, ldv=0, ldqo=0, ldko=0):
+    """Descriptor of a rotation (rot_dim None: the whole head turns)."""
+    pick = lambda names, x: names[x] if isinstance(x, str) else int(x)
+    return RopeDesc(T, heads_q, heads_k, head_dim, head_dim if rot_dim is None else rot_dim, seq_len, ldq, ldk, ldv, ldqo,
+                    ldko, pick(DTYPES, dtype), pick(ROPE_LAYOUTS, layout), pick(ROPE_SCALINGS, scaling), 0, base, factor,
+                    low, high, mscale, orig_len)
+
+
+def cache_desc(n_pages, page_size, heads, head_dim, dtype="bf16"):
+    """Descriptor of a paged cache: K and V [n_pages][heads][page_size][head_dim]."""
+    return CacheDesc(n_pages, page_size, heads, head_dim, DTYPES[dtype] if isinstance(dtype, str) else int(dtype), 0)
+
+
+def _check_rope(d: RopeDesc, q, k, positions, q_out, k_out):
+    import torch
+    if d.dtype not in (F32, BF16) or min(d.T, d.heads_q, d.heads_k, d.head_dim, d.ldq, d.ldk, d.ldqo, d.ldko) < 0:
+        return                      # the library refuses the descriptor itself
+    dt = _torch_dtype(d.dtype)
+    wq, wk = d.heads_q * d.head_dim, d.heads_k * d.head_dim
+    for name, t, w, ld in (("q", q, wq, d.ldq), ("q_out", q_out, wq, d.ldqo), ("k", k, wk, d.ldk), ("k_out", k_out, wk, d.ldko)):
+        if w > 0:
+            _need_rows(name, t, d.T, w, ld or w, dt)
+    _need_flat("positions", positions, (d.T,), torch.int32)
+    if d.T > 0:
+        _one_device([("q", q), ("k", k), ("positions", positions), ("q_out", q_out), ("k_out", k_out)])
+
+
+def rope_fwd(d: RopeDesc, q, k, positions, q_out, k_out, stream=None):
+    """Rows of q and k turned by their positions (None: by their place in a sequence)."""
+    if _try_here("rope_fwd", stream, (d, q, k, positions, q_out, k_out)):
+        return
+    _check_rope(d, q, k, positions, q_out, k_out)
+    _check(lib().cola_rope_fwd(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(positions), _ptr(q_out), _ptr(k_out),
+                               _stream(stream)))
+
+
+def rope_bwd(d: RopeDesc, dq_out, dk_out, positions, dq, dk, stream=None):
+    """Gradients of rope_fwd: the rows turned back."""
+    if _try_here("rope_bwd", stream, (d, dq_out, dk_out, positions, dq, dk)):
+        return
+    _check_rope(d, dq_out, dk_out, positions, dq, dk)
+    _check(lib().cola_rope_bwd(ctypes.byref(d), _ptr(dq_out), _ptr(dk_out), _ptr(positions), _ptr(dq), _ptr(dk),
+                               _stream(stream)))
+
+
+def _check_pages(c: CacheDesc, K, V):
+    if c.dtype not in (F32, BF16) or min(c.n_pages, c.page_size, c.heads, c.head_dim) < 0:
+        return
+    for name, t in (("K", K), ("V", V)):
+        _need_flat(name, t, (c.n_pages, c.heads, c.page_size, c.head_dim), _torch_dtype(c.dtype))
+
+
+def cache_append(d: RopeDesc, c: CacheDesc, q, k, v, positions, slots, q_out, K, V, stream=None):
+    """q turned into q_out, k turned and v as it is into the cache at each row's slot."""
+    if _try_here("cache_append", stream, (d, c, q, k, v, positions, slots, q_out, K, V)):
+        return
+    import torch
+    if d.dtype in (F32, BF16) and min(d.T, d.heads_q, d.heads_k, d.head_dim, d.ldq, d.ldk, d.ldv, d.ldqo) >= 0:
+        dt = _torch_dtype(d.dtype)
+        wq, wk = d.heads_q * d.head_dim, d.heads_k * d.head_dim
+        for name, t, w, ld in (("q", q, wq, d.ldq), ("q_out", q_out, wq, d.ldqo), ("k", k, wk, d.ldk), ("v", v, wk, d.ldv)):
+            if w > 0:
+                _need_rows(name, t, d.T, w, ld or w, dt)
+        _need_flat("positions", positions, (d.T,), torch.int32)
+        _need_flat("slots", slots, (d.T,), torch.int32)
+        _check_pages(c, K, V)
+        if d.T > 0:
+            _one_device([("q", q), ("k", k), ("v", v), ("positions", positions), ("slots", slots), ("q_out", q_out),
+                         ("K", K), ("V", V)])
+    _check(lib().cola_cache_append(ctypes.byref(d), ctypes.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(positions),
+                                   _ptr(slots), _ptr(q_out), _ptr(K), _ptr(V), _stream(stream)))
+
+
+def page_map_desc(n_req, T, page_size, max_pages, n_free, pos0=0):
+    """Descriptor of a step's tables: n_req requests, T rows, a free list of n_free pages."""
+    return PageMapDesc(n_req, T, page_size, max_pages, n_free, pos0)
+
+
+def page_map(d: PageMapDesc, kv_len, n_new, free_pages, free_at, table, start, slots, positions, free_next, stream=None):
+    """Where a step's new tokens go: start, slots, positions and the new pages in table."""
+    if _try_here("page_map", stream, (d, kv_len, n_new, free_pages, free_at, table, start, slots, positions, free_next)):
+        return
+    import torch
+    if min(d.n_req, d.T, d.max_pages, d.n_free) >= 0:
+        for name, t, shape in (("kv_len", kv_len, (d.n_req,)), ("n_new", n_new, (d.n_req,)),
+                               ("free_pages", free_pages, (d.n_free,)), ("free_at", free_at, (1,)),
+                               ("table", table, (d.n_req, d.max_pages)), ("start", start, (d.n_req + 1,)),
+                               ("slots", slots, (d.T,)), ("positions", positions, (d.T,)), ("free_next", free_next, (1,))):
+            _need_flat(name, t, shape, torch.int32)
+        _one_device([("kv_len", kv_len), ("n_new", n_new), ("free_pages", free_pages), ("free_at", free_at),
+                     ("table", table), ("start", start), ("slots", slots), ("positions", positions),
+                     ("free_next", free_next)])
+    _check(lib().cola_page_map(ctypes.byref(d), _ptr(kv_len), _ptr(n_new), _ptr(free_pages), _ptr(free_at), _ptr(table),
+                               _ptr(start), _ptr(slots), _ptr(positions), _ptr(free_next), _stream(stream)))
+
+
+def prefix_attn_desc(n_req, T, heads_q, prefix_len, max_kv, max_new=1, max_pages=0, ldq=0, ldo=0, scale=0.0):
+    """Descriptor of attention behind a shared prefix (scale 0: 1 / sqrt(head_dim))."""
+    return PrefixAttnDesc(n_req, T, heads_q, prefix_len, max_kv, max_new, max_pages, ldq, ldo, scale)
+
+
+def prefix_attn_workspace_bytes(d: PrefixAttnDesc, c: CacheDesc) -> int:
+    return int(lib().cola_prefix_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(c)))
+
+
+def prefix_attn(d: PrefixAttnDesc, c: CacheDesc, q, K, V, prefix_table, table, kv_len, start, out, lse, ws=None,
+                ws_bytes=None, stream=None):
+    """out and lse of a batch whose requests see prefix_len shared tokens and their own (start None: a row each)."""
+    if _try_here("prefix_attn", stream, (d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, ws_bytes)):
+        return
+    import torch
+    ws_bytes = _ws_bytes(ws, ws_bytes)
+    ps = c.page_size
+    if min(d.n_req, d.T, d.heads_q, d.prefix_len, d.max_kv, d.max_pages, d.ldq, d.ldo, c.head_dim) >= 0 and ps > 0:
+        w = d.heads_q * c.head_dim
+        _need_rows("q", q, d.T, w, d.ldq or w, torch.bfloat16)
+        _need_rows("out", out, d.T, w, d.ldo or w, torch.bfloat16)
+        _check_pages(c, K, V)
+        width = d.max_pages or -(-d.max_kv // ps)
+        _need_flat("prefix_table", prefix_table, (-(-d.prefix_len // ps),), torch.int32)
+        if d.max_kv > 0:
+            _need_flat("table", table, (d.n_req, width), torch.int32)
+            _need_flat("kv_len", kv_len, (d.n_req,), torch.int32)
+        _need_flat("start", start, (d.n_req + 1,), torch.int32)
+        _need_flat("lse", lse, (d.heads_q, d.T), torch.float32)
+        if d.T > 0 and d.n_req > 0:
+            _one_device([("q", q), ("K", K), ("V", V), ("prefix_table", prefix_table), ("table", table),
+                         ("kv_len", kv_len), ("start", start), ("out", out), ("lse", lse), ("ws", ws)])
+    _check(lib().cola_prefix_attn(ctypes.byref(d), ctypes.byref(c), _ptr(q), _ptr(K), _ptr(V), _ptr(prefix_table),
+                                  _ptr(table), _ptr(kv_len), _ptr(start), _ptr(out), _ptr(lse), _ptr(ws), ws_bytes,
+                                  _stream(stream)))

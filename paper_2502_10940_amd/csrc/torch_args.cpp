@@ -1,4 +1,4 @@
-// torch_args.cpp -- the layer and group calls of cola.py with their checks in
+// torch_args.cpp -- the layer, group and serving calls of cola.py with their checks in
 // native code (CPython extension _torch_args).
 //
 // cola.py checks every tensor against the descriptor before a call (dtype,
@@ -6,7 +6,7 @@
 // cost 10 us of a forward call and 17 us of a backward call, as much as the
 // kernels of a small layer take; here about 1 us.  Each function takes the
 // arguments of the cola.py function of the same name (with the stream as an
-// integer) and returns the library's status, or None when any argument is not
+// integer; the serving calls have the current device before it) and returns the library's status, or None when any argument is not
 // the plain case (a tensor of the expected kind, or None where that is allowed):
 // cola.py then runs its own checks, which raise the error or take the call.
 #include <Python.h>
@@ -291,9 +291,166 @@ PyObject* group_bwd(PyObject*, Args v, Py_ssize_t n) {   // d, dY, X, Z_all, H_a
     });
 }
 
+// ---- serving ----
+
+struct Here {                                            // the current device, stream
+    int64_t device, stream;
+    bool init(Args v) { return take_int(v[0], &device) && take_int(v[1], &stream); }
+    cola_stream_t s() const { return reinterpret_cast<cola_stream_t>(stream); }
+
+    const at::Tensor* mine(PyObject* o, at::ScalarType dtype) const {
+        if (!THPVariable_CheckExact(o)) return nullptr;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.has_storage() || !t.is_cuda() || t.get_device() != device || t.scalar_type() != dtype) return nullptr;
+        return &t;
+    }
+    // [rows][width] at a row pitch of ld; None where no element is needed
+    bool rows(PyObject* o, int64_t rows, int64_t width, int64_t ld, at::ScalarType dtype, void** out) const {
+        *out = nullptr;
+        if (width == 0) return o == Py_None;
+        const at::Tensor* t = mine(o, dtype);
+        if (!t || t->dim() != 2 || t->size(0) < rows || t->size(1) < width) return false;
+        if (t->stride(1) != 1 || (rows > 1 && t->stride(0) != (ld ? ld : width))) return false;
+        *out = t->data_ptr();
+        return true;
+    }
+    // contiguous, at least n0 along the first dimension, the others exactly
+    bool flat(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype, bool none_ok, void** out) const {
+        *out = nullptr;
+        if (o == Py_None) return none_ok;
+        const at::Tensor* t = mine(o, dtype);
+        if (!t || t->dim() != (int64_t)shape.size() || !t->is_contiguous() || t->size(0) < shape[0]) return false;
+        for (size_t i = 1; i < shape.size(); ++i)
+            if (t->size(i) != shape[i]) return false;
+        *out = t->data_ptr();
+        return true;
+    }
+    bool ints(PyObject* o, int64_t n, bool none_ok, const int32_t** out) const {
+        void* p;
+        if (!flat(o, {n}, at::kInt, none_ok, &p)) return false;
+        *out = static_cast<const int32_t*>(p);
+        return true;
+    }
+};
+
+bool count_ok(int64_t v) { return v >= 0 && v <= kMaxDim; }
+
+struct Rope {
+    cola_rope_desc d;
+    at::ScalarType t;
+    int64_t wq, wk;
+
+    bool init(PyObject* o) {
+        if (!take_desc(o, &d) || (d.dtype != COLA_F32 && d.dtype != COLA_BF16)) return false;
+        if (d.T < 1) return false;
+        for (int64_t v : {d.T, d.heads_q, d.heads_k, d.head_dim, d.ldq, d.ldk, d.ldv, d.ldqo, d.ldko})
+            if (!count_ok(v)) return false;
+        t = d.dtype == COLA_BF16 ? at::kBFloat16 : at::kFloat;
+        wq = d.heads_q * d.head_dim;
+        wk = d.heads_k * d.head_dim;
+        return true;
+    }
+};
+
+struct Cache {
+    cola_cache_desc c;
+    bool init(PyObject* o) {
+        if (!take_desc(o, &c) || (c.dtype != COLA_F32 && c.dtype != COLA_BF16)) return false;
+        return dim_ok(c.n_pages) && dim_ok(c.page_size) && dim_ok(c.heads) && dim_ok(c.head_dim);
+    }
+    bool pages(const Here& h, PyObject* o, void** out) const {
+        return h.flat(o, {c.n_pages, c.heads, c.page_size, c.head_dim},
+                      c.dtype == COLA_BF16 ? at::kBFloat16 : at::kFloat, false, out);
+    }
+};
+
+template <class F>
+PyObject* rope(Args v, Py_ssize_t n, F f) {              // d, q, k, positions, q_out, k_out, device, stream
+    return call([&](int* st) {
+        Rope r;
+        Here h;
+        void *q, *k, *qo, *ko;
+        const int32_t* pos;
+        if (n != 8 || !h.init(v + 6) || !r.init(v[0]) || !h.rows(v[1], r.d.T, r.wq, r.d.ldq, r.t, &q) ||
+            !h.rows(v[2], r.d.T, r.wk, r.d.ldk, r.t, &k) || !h.ints(v[3], r.d.T, true, &pos) ||
+            !h.rows(v[4], r.d.T, r.wq, r.d.ldqo, r.t, &qo) || !h.rows(v[5], r.d.T, r.wk, r.d.ldko, r.t, &ko))
+            return false;
+        COLA_CALL(f(&r.d, q, k, pos, qo, ko, h.s()));
+    });
+}
+PyObject* rope_fwd(PyObject*, Args v, Py_ssize_t n) { return rope(v, n, cola_rope_fwd); }
+PyObject* rope_bwd(PyObject*, Args v, Py_ssize_t n) { return rope(v, n, cola_rope_bwd); }
+
+PyObject* cache_append(PyObject*, Args v, Py_ssize_t n) { // d, c, q, k, v, positions, slots, q_out, K, V, device, stream
+    return call([&](int* st) {
+        Rope r;
+        Cache c;
+        Here h;
+        void *q, *k, *val, *qo, *K, *V;
+        const int32_t *pos, *slots;
+        if (n != 12 || !h.init(v + 10) || !r.init(v[0]) || !c.init(v[1]) ||
+            !h.rows(v[2], r.d.T, r.wq, r.d.ldq, r.t, &q) || !h.rows(v[3], r.d.T, r.wk, r.d.ldk, r.t, &k) ||
+            !h.rows(v[4], r.d.T, r.wk, r.d.ldv, r.t, &val) || !h.ints(v[5], r.d.T, true, &pos) ||
+            !h.ints(v[6], r.d.T, false, &slots) || !h.rows(v[7], r.d.T, r.wq, r.d.ldqo, r.t, &qo) ||
+            !c.pages(h, v[8], &K) || !c.pages(h, v[9], &V))
+            return false;
+        COLA_CALL(cola_cache_append(&r.d, &c.c, q, k, val, pos, slots, qo, K, V, h.s()));
+    });
+}
+
+PyObject* page_map(PyObject*, Args v, Py_ssize_t n) {    // d, kv_len, n_new, free_pages, free_at, table, start, slots, positions, free_next, device, stream
+    return call([&](int* st) {
+        cola_page_map_desc d;
+        Here h;
+        void* table;
+        const int32_t *kv, *nw, *list, *at, *start, *slots, *pos, *next;
+        if (n != 12 || !h.init(v + 10) || !take_desc(v[0], &d) || !dim_ok(d.n_req) || !dim_ok(d.T) || !dim_ok(d.max_pages) ||
+            !dim_ok(d.n_free) || !h.ints(v[1], d.n_req, false, &kv) || !h.ints(v[2], d.n_req, false, &nw) ||
+            !h.ints(v[3], d.n_free, false, &list) || !h.ints(v[4], 1, true, &at) ||
+            !h.flat(v[5], {d.n_req, d.max_pages}, at::kInt, false, &table) || !h.ints(v[6], d.n_req + 1, false, &start) ||
+            !h.ints(v[7], d.T, false, &slots) || !h.ints(v[8], d.T, false, &pos) || !h.ints(v[9], 1, false, &next))
+            return false;
+        auto out = [](const int32_t* p) { return const_cast<int32_t*>(p); };
+        COLA_CALL(cola_page_map(&d, kv, nw, list, at, static_cast<int32_t*>(table), out(start), out(slots), out(pos),
+                                out(next), h.s()));
+    });
+}
+
+PyObject* prefix_attn(PyObject*, Args v, Py_ssize_t n) { // d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, ws_bytes, device, stream
+    return call([&](int* st) {
+        cola_prefix_attn_desc d;
+        Cache c;
+        Here h;
+        void *q, *K, *V, *table = nullptr, *out, *lse, *ws;
+        const int32_t *prefix, *kv = nullptr, *start;
+        size_t ws_bytes;
+        if (n != 15 || !h.init(v + 13) || !take_desc(v[0], &d) || !c.init(v[1]) || c.c.dtype != COLA_BF16 || d.n_req < 1 ||
+            d.T < 1)
+            return false;
+        for (int64_t x : {d.n_req, d.T, d.heads_q, d.prefix_len, d.max_kv, d.max_pages, d.ldq, d.ldo})
+            if (!count_ok(x)) return false;
+        const int64_t w = d.heads_q * c.c.head_dim, ps = c.c.page_size;
+        if (!h.rows(v[2], d.T, w, d.ldq, at::kBFloat16, &q) || !c.pages(h, v[3], &K) || !c.pages(h, v[4], &V) ||
+            !h.ints(v[5], (d.prefix_len + ps - 1) / ps, d.prefix_len == 0, &prefix))
+            return false;
+        if (d.max_kv > 0) {
+            const int64_t width = d.max_pages ? d.max_pages : (d.max_kv + ps - 1) / ps;
+            if (!h.flat(v[6], {d.n_req, width}, at::kInt, false, &table) || !h.ints(v[7], d.n_req, false, &kv)) return false;
+        }
+        if (!h.ints(v[8], d.n_req + 1, true, &start) || !h.rows(v[9], d.T, w, d.ldo, at::kBFloat16, &out) ||
+            !h.flat(v[10], {d.heads_q, d.T}, at::kFloat, true, &lse) || !take_ws(v[11], v[12], &ws, &ws_bytes))
+            return false;
+        if (ws && THPVariable_Unpack(v[11]).get_device() != h.device) return false;
+        COLA_CALL(cola_prefix_attn(&d, &c.c, q, K, V, prefix, static_cast<const int32_t*>(table), kv, start, out,
+                                   static_cast<float*>(lse), ws, ws_bytes, h.s()));
+    });
+}
+
 #define COLA_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {COLA_METHOD(fwd),       COLA_METHOD(fwd_outer), COLA_METHOD(infer),       COLA_METHOD(bwd),
                          COLA_METHOD(bwd_outer), COLA_METHOD(group_fwd), COLA_METHOD(group_infer), COLA_METHOD(group_bwd),
+                         COLA_METHOD(rope_fwd),  COLA_METHOD(rope_bwd),  COLA_METHOD(cache_append), COLA_METHOD(page_map),
+                         COLA_METHOD(prefix_attn),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,261 @@
+"""The serving entry points on the CPU: descriptors and pointers that must be
+refused before anything is enqueued, workspace sizes, the Python checks, and the
+plain references against closed forms."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import serve_ref as R
+from paper_2502_10940_amd import cola
+
+FAKE = 0x1000            # never dereferenced: every call below fails before a launch
+BF, I32 = torch.bfloat16, torch.int32
+
+
+def refused(status, fn, *args):
+    with pytest.raises(cola.ColaError) as e:
+        fn(*args)
+    assert e.value.status == status
+
+
+# ---- rope ----
+
+def rope(d, q=FAKE, k=FAKE, pos=None, qo=FAKE, ko=FAKE, fn=cola.rope_fwd):
+    fn(d, q, k, pos, qo, ko, 0)
+
+
+@pytest.mark.parametrize("fn", (cola.rope_fwd, cola.rope_bwd))
+def test_rope_refusals(fn):
+    D = cola.rope_desc
+    bad = [D(4, 0, 0, 64), D(-1, 2, 2, 64), D(4, -1, 2, 64), D(4, 2, 2, 0), D(4, 2, 2, 513), D(4, 2, 2, 64, 63),
+           D(4, 2, 2, 64, 66), D(4, 2, 2, 64, -2), D(4, 2, 2, 64, ldq=127), D(4, 2, 2, 64, ldk=127),
+           D(4, 2, 2, 64, ldqo=127), D(4, 2, 2, 64, ldko=127), D(4, 2, 2, 64, ldq=(1 << 22) + 1), D(1 << 31, 2, 2, 64),
+           D(4, 2, 2, 64, seq_len=-1), D(4, 2, 2, 64, 2, scaling="base", factor=2.0), D(4, 1 << 23, 2, 64)]
+    for d in bad:
+        refused(cola.ERR_BAD_SHAPE, rope, d, FAKE, FAKE, None, FAKE, FAKE, fn)
+    nan, inf = math.nan, math.inf
+    bad = [D(4, 2, 2, 64, dtype=7), D(4, 2, 2, 64, layout=2), D(4, 2, 2, 64, layout=-1), D(4, 2, 2, 64, scaling=5),
+           D(4, 2, 2, 64, base=1.0), D(4, 2, 2, 64, base=nan), D(4, 2, 2, 64, base=inf), D(4, 2, 2, 64, mscale=-1.0),
+           D(4, 2, 2, 64, mscale=nan), D(4, 2, 2, 64, scaling="linear", factor=0.5),
+           D(4, 2, 2, 64, scaling="linear", factor=nan), D(4, 2, 2, 64, scaling="yarn", factor=2.0, low=1.0, high=32.0),
+           D(4, 2, 2, 64, scaling="yarn", factor=2.0, orig_len=8, low=2.0, high=2.0),
+           D(4, 2, 2, 64, scaling="wavelength", factor=2.0, orig_len=8, low=0.0, high=2.0)]
+    for d in bad:
+        refused(cola.ERR_INVALID_ARG, rope, d, FAKE, FAKE, None, FAKE, FAKE, fn)
+    d = D(4, 2, 2, 64)
+    d.reserved = 1
+    refused(cola.ERR_INVALID_ARG, rope, d, FAKE, FAKE, None, FAKE, FAKE, fn)
+    d = D(4, 2, 2, 64)
+    for args in ((None, FAKE, None, FAKE, FAKE), (FAKE, None, None, FAKE, FAKE), (FAKE, FAKE, None, None, FAKE),
+                 (FAKE, FAKE, None, FAKE, None), (FAKE + 1, FAKE, None, FAKE, FAKE), (FAKE, FAKE, FAKE + 2, FAKE, FAKE)):
+        refused(cola.ERR_INVALID_ARG, rope, d, *args, fn)
+    # in place at another pitch
+    refused(cola.ERR_INVALID_ARG, rope, D(4, 2, 2, 64, ldqo=256), FAKE, FAKE, None, FAKE, FAKE + 4096, fn)
+    rope(D(0, 2, 2, 64), None, None, None, None, None, fn)     # an empty batch enqueues nothing
+
+
+def test_append_refusals():
+    D, C = cola.rope_desc, cola.cache_desc
+
+    def call(d, c, q=FAKE, k=FAKE, v=FAKE, pos=None, slots=FAKE, qo=FAKE, K=FAKE, V=FAKE + 4096):
+        cola.cache_append(d, c, q, k, v, pos, slots, qo, K, V, 0)
+
+    d, c = D(4, 4, 2, 64), C(8, 16, 2, 64)
+    for bad in (C(8, 16, 3, 64), C(8, 16, 2, 128), C(8, 8, 2, 64), C(8, 24, 2, 64), C(8, 8192, 2, 64), C(-1, 16, 2, 64),
+                C(8, 0, 2, 64)):
+        refused(cola.ERR_BAD_SHAPE, call, d, bad)
+    for bad in (D(4, 4, 0, 64), D(4, 4, 2, 64, ldv=127)):
+        refused(cola.ERR_BAD_SHAPE, call, bad, c)
+    refused(cola.ERR_INVALID_ARG, call, d, C(8, 16, 2, 64, "f32"))
+    refused(cola.ERR_INVALID_ARG, call, d, C(8, 16, 2, 64, 9))
+    for key in ("q", "k", "v", "slots", "qo", "K", "V"):
+        refused(cola.ERR_INVALID_ARG, lambda key=key: call(d, c, **{key: None}))
+    for key, p in (("K", FAKE + 8), ("V", FAKE + 8), ("V", FAKE), ("slots", FAKE + 2), ("pos", FAKE + 1), ("v", FAKE + 1)):
+        refused(cola.ERR_INVALID_ARG, lambda key=key, p=p: call(d, c, **{key: p}))
+    call(D(0, 4, 2, 64), c, None, None, None, None, None, None, None, None)
+
+
+def test_page_map_refusals():
+    D = cola.page_map_desc
+
+    def call(d, **kw):
+        a = dict(kv=FAKE, n=FAKE, free=FAKE, at=None, table=FAKE, start=FAKE, slots=FAKE, pos=FAKE, nxt=FAKE)
+        a.update(kw)
+        cola.page_map(d, a["kv"], a["n"], a["free"], a["at"], a["table"], a["start"], a["slots"], a["pos"], a["nxt"], 0)
+
+    for bad in (D(-1, 4, 16, 2, 8), D(4097, 4, 16, 2, 8), D(2, -1, 16, 2, 8), D(2, 4, 0, 2, 8), D(2, 4, 24, 2, 8),
+                D(2, 4, 8192, 2, 8), D(2, 4, 16, -1, 8), D(2, 4, 16, 1 << 30, 8), D(2, 4, 16, 2, -1), D(2, 4, 16, 2, 8, -1),
+                D(2, 1 << 31, 16, 2, 8), D(2, 4, 16, 2, 1 << 31), D(2, 4, 16, 2, 8, 1 << 31)):
+        refused(cola.ERR_BAD_SHAPE, call, bad)
+    d = D(2, 4, 16, 2, 8)
+    for key in ("kv", "n", "free", "table", "start", "slots", "pos", "nxt"):
+        refused(cola.ERR_INVALID_ARG, lambda key=key: call(d, **{key: None}))
+        refused(cola.ERR_INVALID_ARG, lambda key=key: call(d, **{key: FAKE + 2}))
+    refused(cola.ERR_INVALID_ARG, lambda: call(d, at=FAKE))          # the list's place in and out
+
+
+def attn_args(**kw):
+    a = dict(q=FAKE, K=FAKE, V=FAKE, ptab=FAKE, tab=FAKE, kv=FAKE, start=FAKE, out=FAKE + 4096, lse=FAKE, ws=FAKE, n=1 << 40)
+    a.update(kw)
+    return [a[k] for k in ("q", "K", "V", "ptab", "tab", "kv", "start", "out", "lse", "ws", "n")]
+
+
+def test_attention_refusals():
+    D, C = cola.prefix_attn_desc, cola.cache_desc
+
+    def call(d, c, **kw):
+        cola.prefix_attn(d, c, *attn_args(**kw), 0)
+
+    c, d = C(8, 16, 2, 64), D(3, 5, 4, 40, 30, 2)
+    for bad in (C(8, 16, 2, 64, "f32"), C(8, 16, 2, 96), C(8, 16, 2, 32), C(8, 16, 2, 256)):
+        refused(cola.ERR_UNSUPPORTED, call, d, bad)
+    for bad in (C(8, 24, 2, 64), C(8, 8, 2, 64), C(8, 16, 0, 64), C(8, 16, 3, 64)):
+        refused(cola.ERR_BAD_SHAPE, call, d, bad)
+    for bad in (D(-1, 5, 4, 40, 30), D(65536, 5, 4, 40, 30), D(3, -1, 4, 40, 30), D(3, 5, 0, 40, 30), D(3, 5, 3, 40, 30),
+                D(3, 5, 4, -1, 30), D(3, 5, 4, 40, -1), D(3, 5, 4, 40, 30, 0), D(3, 5, 4, (1 << 30) + 1, 30),
+                D(3, 5, 4, 40, 30, max_pages=1), D(3, 5, 4, 40, 30, ldq=248), D(3, 5, 4, 40, 30, ldq=260),
+                D(3, 5, 4, 40, 30, ldo=255), D(3, 1 << 30, 4, 40, 30), D(3, 5, 4, 40, 30, max_pages=-1)):
+        refused(cola.ERR_BAD_SHAPE, call, bad, c)
+        assert cola.prefix_attn_workspace_bytes(bad, c) == 0
+    for s in (-1.0, math.nan, math.inf, 1e-40, 1e38):
+        refused(cola.ERR_INVALID_ARG, call, D(3, 5, 4, 40, 30, scale=s), c)
+    for key in ("q", "K", "V", "ptab", "tab", "kv", "out"):
+        refused(cola.ERR_INVALID_ARG, lambda key=key: call(d, c, **{key: None}))
+    for key in ("q", "K", "V", "out", "ws"):
+        refused(cola.ERR_INVALID_ARG, lambda key=key: call(d, c, **{key: FAKE + 8}))
+    for key in ("ptab", "tab", "kv", "start", "lse"):
+        refused(cola.ERR_INVALID_ARG, lambda key=key: call(d, c, **{key: FAKE + 2}))
+    refused(cola.ERR_INVALID_ARG, lambda: call(d, c, out=FAKE))      # out over q
+    need = cola.prefix_attn_workspace_bytes(d, c)
+    assert need > 0
+    refused(cola.ERR_WORKSPACE, lambda: call(d, c, n=need - 1))
+    refused(cola.ERR_WORKSPACE, lambda: call(d, c, ws=None))
+    # empty batches enqueue nothing
+    for e in (D(0, 5, 4, 40, 30), D(3, 0, 4, 40, 30)):
+        assert cola.prefix_attn_workspace_bytes(e, c) == 0
+        cola.prefix_attn(e, c, *[None] * 10, 0, 0)
+
+
+def test_workspace_sizes_cover_their_parts():
+    """One fp32 partial row and its two statistics for each part of the keys, and a
+    size that does not shrink when a bound grows past another's."""
+    for hq, hk, hd in ((4, 4, 64), (32, 8, 128)):
+        for T in (1, 17, 300):
+            for L, kv in ((0, 1000), (1000, 0), (1, 1), (100000, 3000)):
+                c, d = cola.cache_desc(10000, 16, hk, hd), cola.prefix_attn_desc(T, T, hq, L, kv)
+                n = cola.prefix_attn_workspace_bytes(d, c)
+                row = T * hq * (hd + 2) * 4
+                assert n == 0 or (n >= row and n <= 128 * row + 1024), (hq, T, L, kv, n)
+                if L and kv:
+                    assert n >= 2 * row
+
+
+def test_python_checks():
+    z = lambda *s, dt=BF: torch.zeros(s, dtype=dt)
+    d = cola.rope_desc(4, 2, 1, 64)
+    ok = [z(4, 128), z(4, 64), z(4, dt=I32), z(4, 128), z(4, 64)]
+    for i, t in ((0, z(4, 128, dt=torch.float32)), (0, z(3, 128)), (0, z(4, 127)), (1, z(64, 4).t()), (2, z(4, dt=torch.int64)),
+                 (2, z(3, dt=I32)), (3, z(4, 256)[:, :128]), (4, z(4 * 64)), (2, z(8, dt=I32)[::2])):
+        a = list(ok)
+        a[i] = t
+        with pytest.raises(ValueError):
+            cola.rope_fwd(d, *a)
+    with pytest.raises(ValueError, match="GPU"):
+        cola.rope_fwd(d, *ok)
+    with pytest.raises(TypeError):
+        cola.rope_bwd(d, "q", *ok[1:])
+    c = cola.cache_desc(3, 16, 1, 64)
+    K = z(3, 1, 16, 64)
+    for bad in (z(2, 1, 16, 64), z(3, 2, 16, 64), z(3, 1, 32, 64), z(3, 1, 16, 64, dt=torch.float32), z(3, 1, 32, 64)[:, :, ::2]):
+        with pytest.raises(ValueError):
+            cola.cache_append(d, c, ok[0], ok[1], z(4, 64), None, z(4, dt=I32), ok[3], K, bad)
+    i = lambda *s: torch.zeros(s, dtype=I32)
+    m = cola.page_map_desc(2, 4, 16, 3, 5)
+    good = [i(2), i(2), i(5), i(1), i(2, 3), i(3), i(4), i(4), i(1)]
+    for j, t in ((0, i(1)), (2, i(4)), (4, i(2, 4)), (5, i(2)), (6, i(3)), (7, i(4).long()), (8, i(0))):
+        a = list(good)
+        a[j] = t
+        with pytest.raises(ValueError):
+            cola.page_map(m, *a)
+    ad, ac = cola.prefix_attn_desc(2, 3, 2, 20, 40), cola.cache_desc(3, 16, 1, 64)
+    good = [z(3, 128), K, K, i(2), i(2, 3), i(2), i(3), z(3, 128), z(2, 3, dt=torch.float32)]
+    for j, t in ((0, z(3, 127)), (1, z(3, 1, 16, 63)), (3, i(1)), (4, i(2, 2)), (5, i(1)), (6, i(2)), (7, z(3, 128, dt=torch.float32)),
+                 (8, z(3, 2, dt=torch.float32)), (8, z(2, 3))):
+        a = list(good)
+        a[j] = t
+        with pytest.raises(ValueError):
+            cola.prefix_attn(ad, ac, *a)
+
+
+def test_native_checks_hand_back():
+    m = cola._native_calls()
+    assert m
+    for name in ("rope_fwd", "rope_bwd", "cache_append", "page_map", "prefix_attn"):
+        assert getattr(m, name)() is None and getattr(m, name)(*range(12)) is None
+    z = torch.zeros((4, 128), dtype=BF)
+    assert m.rope_fwd(cola.rope_desc(4, 2, 2, 64), z, z, None, z, z, 0, 0) is None       # CPU tensors
+
+
+def test_another_device_is_refused(monkeypatch):
+    """A tensor of a GPU that is not the current one: the check sees the device index."""
+    class On:
+        def __init__(self, index):
+            self.device = torch.device("cuda", index)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    cola._one_device([("q", On(0)), ("k", None), ("v", 4096)])
+    with pytest.raises(ValueError, match="cuda:1"):
+        cola._one_device([("q", On(0)), ("k", On(1))])
+
+
+# ---- the references ----
+
+def test_rope_reference_is_a_rotation():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((5, 2 * 16))
+    pos = np.array([0, 1, 7, -3, 2 ** 31 - 1])
+    for layout in ("half", "interleaved"):
+        y = R.rope(x, 2, 16, 12, pos, layout)
+        assert np.allclose(R.rope(y, 2, 16, 12, pos, layout, back=True), x)
+        assert np.allclose(y[0], x[0]) and np.allclose(y.reshape(5, 2, 16)[..., 12:], x.reshape(5, 2, 16)[..., 12:])
+        # a scalar product after turning depends on the difference of the positions alone
+        a, b = x[:1], x[1:2]
+        s = [float(np.vdot(R.rope(a, 2, 16, 16, [p], layout), R.rope(b, 2, 16, 16, [p + 5], layout))) for p in (0, 3, 1000)]
+        assert np.allclose(s, s[0])
+    # the transpose: <R x, y> = <x, R^T y>
+    y = rng.standard_normal((5, 2 * 16))
+    assert math.isclose(np.vdot(R.rope(x, 2, 16, 16, pos, mscale=1.5), y), np.vdot(x, R.rope(y, 2, 16, 16, pos, back=True, mscale=1.5)))
+
+
+def test_scalings_at_their_ends():
+    plain, _ = R.frequencies(64)
+    kw = dict(factor=8.0, orig_len=4096)
+    yarn, m = R.frequencies(64, "yarn", low=1.0, high=32.0, **kw)
+    assert math.isclose(yarn[0], plain[0]) and math.isclose(yarn[-1], plain[-1] / 8) and math.isclose(m, 1 + 0.1 * math.log(8))
+    wave, _ = R.frequencies(64, "wavelength", low=1.0, high=4.0, **kw)
+    assert math.isclose(wave[0], plain[0]) and math.isclose(wave[-1], plain[-1] / 8)
+    b, _ = R.frequencies(64, "base", factor=8.0)
+    assert b[0] == 1.0 and math.isclose(b[-1], plain[-1] / 8)
+
+
+def test_attention_reference_against_one_sequence():
+    """A prefix and own tokens in pages are one causal sequence."""
+    rng = np.random.default_rng(1)
+    hd, page, L, kv, n = 8, 16, 21, 19, 7
+    k, v = (rng.standard_normal((L + kv, hd)) for _ in range(2))
+    K, V = np.zeros((6, 1, page, hd)), np.zeros((6, 1, page, hd))
+    ptab, tab = [4, 1], [[0, 5]]
+    for j in range(L + kv):
+        p, o = (ptab[j // page], j % page) if j < L else (tab[0][(j - L) // page], (j - L) % page)
+        K[p, 0, o], V[p, 0, o] = k[j], v[j]
+    q = rng.standard_normal((n, 2 * hd))
+    out, lse, _ = R.attention(q, K, V, 2, ptab, L, tab, [kv], [0, n], page)
+    for i in range(n):
+        end = L + kv - n + i + 1
+        for h in range(2):
+            s = k[:end] @ q[i, h * hd:(h + 1) * hd] / math.sqrt(hd)
+            w = np.exp(s) / np.exp(s).sum()
+            assert np.allclose(out[i, h * hd:(h + 1) * hd], w @ v[:end])
+            assert math.isclose(lse[h, i], math.log(np.exp(s).sum()))
