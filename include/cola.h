@@ -574,17 +574,14 @@ typedef enum {
                               a group, up to four at a time); in small
                               layers with dX, which is then not in
                               COLA_KC_BWD_DX                              */
-    COLA_KC_ATTN_FWD = 14, /* block: causal attention forward             */
+    COLA_KC_ATTN_FWD = 14, /* block: causal attention forward; serving:
+                              cola_prefix_attn, both of its launches      */
     COLA_KC_ATTN_BWD = 15, /* block: attention backward (dq, then dk dv)  */
     COLA_KC_NORM = 16,     /* block: RMSNorm forward (+ residual sum)     */
     COLA_KC_NORM_BWD = 17, /* block: RMSNorm backward (+ residual grad)   */
-    COLA_KC_POINTWISE = 18,/* block: gated product, residual add, sigma   */
-    COLA_KC_ROPE = 19,     /* serving: rotation of q and k, either way    */
-    COLA_KC_APPEND = 20,   /* serving: rotated q, k and v into the cache  */
-    COLA_KC_PAGE_MAP = 21, /* serving: tables, slots, positions           */
-    COLA_KC_PREFIX_ATTN = 22, /* serving: attention over prefix and own tokens */
-    COLA_KC_PREFIX_JOIN = 23, /* serving: its partial results joined      */
-    COLA_KC_COUNT = 24
+    COLA_KC_POINTWISE = 18,/* block: gated product, residual add, sigma;
+                              serving: rotation, cache, tables            */
+    COLA_KC_COUNT = 19
 } cola_kernel_class;
 
 /* Per-class totals since the last reset: launches, elapsed milliseconds,

@@ -27,8 +27,7 @@ WS_LEAN = 16                  # COLA_WS_LEAN: added to a phase, the least worksp
 
 KERNEL_CLASSES = ("fwd_z_sigma", "fwd_y", "bwd_dz", "bwd_dx", "bwd_da", "bwd_db",
                   "reduce_splits", "dense_fwd", "dense_dx", "dense_dw", "fill_zero", "infer_h",
-                  "outer_grad", "bwd_da_db", "attn_fwd", "attn_bwd", "norm", "norm_bwd", "pointwise",
-                  "rope", "cache_append", "page_map", "prefix_attn", "prefix_join")
+                  "outer_grad", "bwd_da_db", "attn_fwd", "attn_bwd", "norm", "norm_bwd", "pointwise")
 
 
 class ColaError(RuntimeError):

@@ -839,8 +839,7 @@ const char* cola_kernel_name(int kc) {
     static const char* names[COLA_KC_COUNT] = {
         "fwd_z_sigma", "fwd_y", "bwd_dz", "bwd_dx", "bwd_da", "bwd_db",
         "reduce_splits", "dense_fwd", "dense_dx", "dense_dw", "fill_zero", "infer_h", "outer_grad",
-        "bwd_da_db", "attn_fwd", "attn_bwd", "norm", "norm_bwd", "pointwise",
-        "rope", "cache_append", "page_map", "prefix_attn", "prefix_join"};
+        "bwd_da_db", "attn_fwd", "attn_bwd", "norm", "norm_bwd", "pointwise"};
     if (kc < 0 || kc >= COLA_KC_COUNT) return "invalid";
     return names[kc];
 }

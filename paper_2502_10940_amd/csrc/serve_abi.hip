@@ -137,7 +137,7 @@ int rope(const cola_rope_desc* d, const void* q, const void* k, const int32_t* p
         frequencies(*d, &a);
         const double es = d->dtype == COLA_BF16 ? 2.0 : 4.0, n = (double)a.T * (a.hq + a.hk);
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-        return chk(timed_fn(COLA_KC_ROPE, 3.0 * n * a.rot, 2.0 * es * n * a.hd, s,
+        return chk(timed_fn(COLA_KC_POINTWISE, 3.0 * n * a.rot, 2.0 * es * n * a.hd, s,
                             [&] { return launch_rope(d->dtype == COLA_BF16, false, a, s); }), "rope");
     });
 }
@@ -211,7 +211,7 @@ int cola_cache_append(const cola_rope_desc* rot, const cola_cache_desc* cache, c
         frequencies(*rot, &a);
         const double es = rot->dtype == COLA_BF16 ? 2.0 : 4.0, n = (double)a.T * a.hd;
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-        return chk(timed_fn(COLA_KC_APPEND, 3.0 * (double)a.T * (a.hq + a.hk) * a.rot, 2.0 * es * n * (a.hq + 2 * a.hk), s,
+        return chk(timed_fn(COLA_KC_POINTWISE, 3.0 * (double)a.T * (a.hq + a.hk) * a.rot, 2.0 * es * n * (a.hq + 2 * a.hk), s,
                             [&] { return launch_rope(rot->dtype == COLA_BF16, true, a, s); }), "cache_append");
     });
 }
@@ -238,7 +238,7 @@ int cola_page_map(const cola_page_map_desc* d, const int32_t* kv_len, const int3
         a.n_req = (int)d->n_req; a.lg_page = log2_of(d->page_size);
         a.T = d->T; a.max_pages = d->max_pages; a.n_free = d->n_free; a.pos0 = d->pos0;
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-        return chk(timed_fn(COLA_KC_PAGE_MAP, 0.0, 4.0 * (3.0 * (double)d->n_req + 2.0 * (double)d->T), s,
+        return chk(timed_fn(COLA_KC_POINTWISE, 0.0, 4.0 * (3.0 * (double)d->n_req + 2.0 * (double)d->T), s,
                             [&] { return launch_page_map(a, s); }), "page_map");
     });
 }
@@ -279,11 +279,11 @@ int cola_prefix_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* c
         // work for the bounds: the lengths themselves are in GPU memory
         const double rows = (double)p.rows, keys = (double)sh.prefix + (double)sh.max_kv;
         const double bytes = 4.0 * rows * sh.hd + 4.0 * ((double)sh.prefix + (double)sh.n_req * sh.max_kv) * sh.hk * sh.hd;
-        const int e = chk(timed_fn(COLA_KC_PREFIX_ATTN, 4.0 * rows * keys * sh.hd, bytes, s,
+        const int e = chk(timed_fn(COLA_KC_ATTN_FWD, 4.0 * rows * keys * sh.hd, bytes, s,
                                    [&] { return launch_prefix_attn(sh, p, t, s); }), "prefix_attn");
         if (e != COLA_OK || p.direct) return e;
         const double parts = (double)p.splits_p + p.splits_s;
-        return chk(timed_fn(COLA_KC_PREFIX_JOIN, 2.0 * rows * sh.hd * parts, rows * sh.hd * (4.0 * parts + 2.0), s,
+        return chk(timed_fn(COLA_KC_ATTN_FWD, 2.0 * rows * sh.hd * parts, rows * sh.hd * (4.0 * parts + 2.0), s,
                             [&] { return launch_prefix_join(sh, p, t, s); }), "prefix_join");
     });
 }

@@ -676,4 +676,4 @@ def test_timing_classes_count_the_launches():
     finally:
         cola.timing_enable(False)
         cola.timing_reset()
-    assert [n[k] for k in ("rope", "cache_append", "page_map", "prefix_attn", "prefix_join")] == [1] * 5
+    assert n["pointwise"] == 3 and n["attn_fwd"] == 2 and sum(n.values()) == 5
