@@ -34,14 +34,12 @@
 
 #include "serve.hpp"
 #include "device_math.hpp"
+#include "row_tile.hpp"
 
 namespace cola {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int NW = 4;                     // waves per workgroup
 constexpr int KB = 32;                    // keys per block of a wave
@@ -69,10 +67,9 @@ struct Args {
     float c;                              // scale log2 e
 };
 
-__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The maximum and the sum over lanes l, l ^ 16, l ^ 32, l ^ 48: a column's four.
 __device__ __forceinline__ float column_max(float x) {
@@ -139,6 +136,11 @@ template <>
 struct VRow<4> { typedef u32x2 type; };
 
 __device__ __forceinline__ bool not_finite(uint32_t bf16) { return (bf16 & 0x7f80u) == 0x7f80u; }
+// The top bit of each half of a pair that is not finite: its exponent plus one
+// carries there and no further.
+__device__ __forceinline__ uint32_t not_finite2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// The pair with those halves zero.
+__device__ __forceinline__ uint32_t finite2(uint32_t x) { return x & ~((not_finite2(x) >> 15) * 0xffffu); }
 
 // The value operand of output tile t: element t of the lane's 8 keys.
 template <int D, class R>
@@ -150,48 +152,46 @@ __device__ __forceinline__ bf16x8 v_frag(const R (&v)[8], int t) {
     return __builtin_bit_cast(bf16x8, f);
 }
 
-// One block of 32 keys from kb on.  MASK: some row does not see all of them, or
-// a page is missing; keys from `end` on hold no tokens.
+// Where 16 keys from k0 on lie: the place of the first in K and V, in rows of HD,
+// and whether their page is in the cache.  Tiles that begin at or past `end` are
+// looked up at the last one before it, missing pages at page 0: what is read
+// there is memory of the cache and is masked.
+struct Place {
+    int64_t row;
+    bool there;
+};
+__device__ __forceinline__ Place place(const Args& a, const int32_t* table, int head, int k0, int end) {
+    const int k = min(k0, (end - 1) & ~15);
+    const int64_t page = table[k >> a.lg_page];
+    Place p;
+    p.there = page >= 0 && page < a.n_pages;
+    p.row = (((p.there ? page : 0) * a.hk + head) << a.lg_page) + (k & ((1 << a.lg_page) - 1));
+    return p;
+}
+
+// One block of 32 keys from kb on, at the places at[0], at[1].  MASK: some row does
+// not see all of them, or a page is missing; keys from `end` on hold no tokens.
 template <int HD, int NT, bool MASK>
-__device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const int32_t* table, int head, int kb, int end,
-                                      int lane) {
+__device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const Place (&at)[2], int kb, int end, int lane) {
     constexpr int KK = HD / 32, D = HD / 16;
     typedef typename VRow<D>::type R;
     const int g = lane >> 4, c = lane & 15;
-    int64_t base[2];
-    bool there[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int k0 = kb + 16 * i;
-        int64_t page = 0;
-        there[i] = true;
-        if (!MASK || k0 < end) page = table[k0 >> a.lg_page];
-        else there[i] = false;
-        if (page < 0 || page >= a.n_pages) {
-            there[i] = false;
-            page = 0;
-        }
-        base[i] = ((((page * a.hk + head) << a.lg_page) + (k0 & ((1 << a.lg_page) - 1)))) * HD;
-    }
     u32x4 kf[2][KK];
     R v[8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const uint16_t* p = a.K + base[i] + c * HD + 8 * g;
-        const bool ok = !MASK || (there[i] && kb + 16 * i + c < end);
+        const uint16_t* p = a.K + at[i].row * HD + c * HD + 8 * g;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-            kf[i][kk] = ok ? *reinterpret_cast<const u32x4*>(p + 32 * kk) : u32x4{0, 0, 0, 0};
+        for (int kk = 0; kk < KK; ++kk) kf[i][kk] = *reinterpret_cast<const u32x4*>(p + 32 * kk);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const uint16_t* p = a.V + base[i] + 4 * g * HD + D * c;
+        const uint16_t* p = a.V + at[i].row * HD + 4 * g * HD + D * c;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool ok = !MASK || (there[i] && kb + 16 * i + 4 * g + j < end);
-            R x{};
-            if (ok) x = *reinterpret_cast<const R*>(p + j * HD);
-            v[4 * i + j] = x;
+            v[4 * i + j] = *reinterpret_cast<const R*>(p + j * HD);
+            if constexpr (MASK)
+                if (!at[i].there || kb + 16 * i + 4 * g + j >= end) v[4 * i + j] = R{};
         }
     }
     f32x4 s[2][NT];
@@ -201,7 +201,7 @@ __device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const int3
         for (int i = 0; i < 2; ++i) {
             s[i][n] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) s[i][n] = mfma(__builtin_bit_cast(bf16x8, kf[i][kk]), w.q[n][kk], s[i][n]);
+            for (int kk = 0; kk < KK; ++kk) s[i][n] = mfma16(__builtin_bit_cast(bf16x8, kf[i][kk]), w.q[n][kk], s[i][n]);
         }
     bf16x8 p[NT];
 #pragma unroll
@@ -211,7 +211,7 @@ __device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const int3
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (!there[i] || kb + 16 * i + 4 * g + j >= w.lim[n]) s[i][n][j] = -INFINITY;
+                    if (!at[i].there || kb + 16 * i + 4 * g + j >= w.lim[n]) s[i][n][j] = -INFINITY;
         }
         float mb = -INFINITY;
 #pragma unroll
@@ -246,34 +246,30 @@ __device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const int3
     // the rows that see them by themselves.
     bool odd = false;
     if constexpr (MASK) {
+        uint32_t any = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-            for (int x = 0; x < D / 2; ++x) odd |= not_finite(v[j][x] & 0xffffu) || not_finite(v[j][x] >> 16);
-        odd = __ballot(odd) != 0;
-        if (odd) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int x = 0; x < D / 2; ++x)
-                    v[j][x] &= (not_finite(v[j][x] & 0xffffu) ? 0u : 0xffffu) |
-                               (not_finite(v[j][x] >> 16) ? 0u : 0xffff0000u);
-        }
+            for (int x = 0; x < D / 2; ++x) {
+                any |= not_finite2(v[j][x]);
+                v[j][x] = finite2(v[j][x]);
+            }
+        odd = __ballot(any != 0) != 0;
     }
 #pragma unroll
     for (int t = 0; t < D; ++t) {
         const bf16x8 vf = v_frag<D>(v, t);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) w.o[t][n] = mfma(vf, p[n], w.o[t][n]);
+        for (int n = 0; n < NT; ++n) w.o[t][n] = mfma16(vf, p[n], w.o[t][n]);
     }
     if constexpr (MASK) {
         if (odd) {
 #pragma unroll 1
             for (int k = 0; k < KB; ++k) {
                 const int i = k / 16;
-                if (!(i ? there[1] : there[0]) || kb + k >= end) continue;
+                if (!(i ? at[1].there : at[0].there) || kb + k >= end) continue;
                 // this lane's elements of its rows: 4 D from 4 D g on
-                const uint16_t* x = a.V + (i ? base[1] : base[0]) + (k - 16 * i) * HD + 4 * D * g;
+                const uint16_t* x = a.V + ((i ? at[1].row : at[0].row) + k - 16 * i) * HD + 4 * D * g;
 #pragma unroll
                 for (int e = 0; e < 4 * D; ++e) {
                     const uint32_t y = x[e];
@@ -357,16 +353,12 @@ __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* t
         }
     }
     // keys that the tile's first row sees, and its last
-    const int all = seen(tile0), any = min(seen(min(tile0 + 16 * NT, n_rows) - 1), k0 + chunk);
+    const int any = a.n_pages > 0 ? min(seen(min(tile0 + 16 * NT, n_rows) - 1), k0 + chunk) : 0, all = min(seen(tile0), any);
 #pragma unroll 1
     for (int kb = k0 + KB * wave; kb < any; kb += KB * NW) {
-        bool whole = kb + KB <= min(all, any);
-        if (whole) {
-            const int64_t p0 = table[kb >> a.lg_page], p1 = table[(kb + 16) >> a.lg_page];
-            whole = p0 >= 0 && p0 < a.n_pages && p1 >= 0 && p1 < a.n_pages;
-        }
-        if (whole) block<HD, NT, false>(w, a, table, head, kb, any, lane);
-        else block<HD, NT, true>(w, a, table, head, kb, any, lane);
+        const Place at[2] = {place(a, table, head, kb, any), place(a, table, head, kb + 16, any)};
+        if (kb + KB <= all && at[0].there && at[1].there) block<HD, NT, false>(w, a, at, kb, any, lane);
+        else block<HD, NT, true>(w, a, at, kb, any, lane);
     }
     // waves 2, 3 into 0, 1, then 1 into 0
     float* mine = lds + (wave & 1) * kStateFloats<HD, NT>;
@@ -411,15 +403,269 @@ __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* t
     }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows: a tile of 128, 32 to a wave, against keys staged in LDS
+// ---------------------------------------------------------------------------
+
+constexpr int WROWS = 32 * NW;            // rows of a wide tile
+
+// STG keys of one head on their way into LDS: load() has them in registers while
+// the stage before is used, put() writes them.  Tiles of 16 keys lie in one page.
+template <int HD>
+struct KeyStage {
+    static constexpr int CPR = HD / 8;                 // 16-byte chunks per row
+    static constexpr int RPI = NTHR / CPR;             // rows that one instruction of the workgroup covers
+    static constexpr int NI = STG / RPI;
+    u32x4 k[NI], v[NI];
+    int kb;                                            // first key
+    uint32_t there;                                    // bit i: the page of keys kb + 16 i .. is in the cache
+
+    // Tile of 16 of this thread's rows in step `it`: the same for all lanes of a wave.
+    __device__ static __forceinline__ int tile(int it) {
+        return (RPI * it + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / CPR)) / 16;
+    }
+
+    __device__ __forceinline__ void load(const Args& a, const int32_t* table, int head, int first, int end) {
+        kb = first;
+        there = 0;
+        Place at[STG / 16];
+#pragma unroll
+        for (int i = 0; i < STG / 16; ++i) {
+            at[i] = place(a, table, head, kb + 16 * i, end);
+            there |= (uint32_t)at[i].there << i;
+        }
+#pragma unroll
+        for (int it = 0; it < NI; ++it) {
+            int64_t b;
+            if constexpr (NI == 4) {
+                b = at[it].row;
+            } else {
+                const int64_t lo = at[2 * it].row, hi = at[2 * it + 1].row;
+                b = tile(it) & 1 ? hi : lo;
+            }
+            const int row = (threadIdx.x / CPR + RPI * it) & 15, c = threadIdx.x % CPR;
+            k[it] = *reinterpret_cast<const u32x4*>(a.K + b * HD + (row * HD + 8 * c));
+            v[it] = *reinterpret_cast<const u32x4*>(a.V + b * HD + (row * HD + 8 * c));
+        }
+    }
+
+    // MASK: values that no row sees (from `end` on, or of a missing page) become
+    // zeros, and those that are not finite, too (true: there are some).
+    template <bool MASK>
+    __device__ __forceinline__ bool put(char* kt, char* vt, int end) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int it = 0; it < NI; ++it) {
+            const int row = threadIdx.x / CPR + RPI * it, c = threadIdx.x % CPR;
+            if constexpr (MASK) {
+                if (!(there >> tile(it) & 1) || kb + row >= end) v[it] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    any |= not_finite2(v[it][x]);
+                    v[it][x] = finite2(v[it][x]);
+                }
+            }
+            *reinterpret_cast<u32x4*>(kt + RowTile<HD>::off(row, c)) = k[it];
+            *reinterpret_cast<u32x4*>(vt + RowTile<HD>::off(row, c)) = v[it];
+        }
+        return any != 0;
+    }
+};
+
+template <int HD>
+struct WideWave {
+    bf16x8 q[HD / 16];
+    f32x16 o[HD / 32];
+    float m, l;                                        // l: of this lane's keys
+    int lim;
+};
+
+// The 64 keys of a stage: one online-softmax step of this lane's row.
+template <int HD, bool MASK>
+__device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, const char* vt, int kb, uint32_t there,
+                                           float c, int lane) {
+    const int hh = lane >> 5;
+    f32x16 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        s[b] = f32x16{};
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) s[b] = mfma(RowTile<HD>::frag(kt, 32 * b, i, lane), w.q[i], s[b]);
+    }
+    if constexpr (MASK) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int k = 32 * b + acc_row(v, hh);
+                if (!(there >> (2 * b + v / 8) & 1) || kb + k >= w.lim) s[b][v] = -INFINITY;
+            }
+    }
+    float mb = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; v += 2) mb = fmaxf(fmaxf(mb, s[b][v]), s[b][v + 1]);
+    mb = xor32_max(mb) * c;
+    if (__ballot(mb > w.m + kSlack) != 0) {
+        const float mn = fmaxf(w.m, mb);
+        const float alpha = exp2_hw(w.m - mn);
+        w.l *= alpha;
+#pragma unroll
+        for (int t = 0; t < HD / 32; ++t) w.o[t] *= alpha;
+        w.m = mn;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            u32x4 f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = exp2_hw(fmaf(s[b][8 * i + 2 * j], c, -w.m)), y = exp2_hw(fmaf(s[b][8 * i + 2 * j + 1], c, -w.m));
+                w.l += x + y;
+                f[j] = pack_bf16x2(x, y);
+            }
+            const bf16x8 p = __builtin_bit_cast(bf16x8, f);
+#pragma unroll
+            for (int t = 0; t < HD / 32; ++t) w.o[t] = mfma(RowTile<HD>::frag_tr(vt, 32 * b, t, i, lane), p, w.o[t]);
+        }
+}
+
+// Bytes of LDS: two stages of keys and values, and their flags.
+template <int HD>
+constexpr int kWideBytes = 4 * RowTile<HD>::BYTES + 16;
+
+// item() for a tile of 128 rows: the same rows, keys and results.
+template <int HD, bool CAUSAL>
+__device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
+                                          int n_rows, int first, int end, int k0, int chunk, int slot) {
+    constexpr int B = RowTile<HD>::BYTES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
+    int* flags = reinterpret_cast<int*>(lds + 4 * B);  // the stage of each buffer that holds values that are not finite
+    auto seen = [&](int rho) { return CAUSAL ? (int)min((int64_t)first + 1 + rho / a.g, (int64_t)end) : end; };
+    const int rho = tile0 + 32 * wave + (lane & 31), t = rho / a.g;
+    const bool live = rho < n_rows;
+    const int64_t row = row0 + t;
+    const int h = head * a.g + (rho - t * a.g);
+    WideWave<HD> w;
+    w.m = kNone;
+    w.l = 0.0f;
+    w.lim = live ? seen(rho) : 0;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) w.o[i] = f32x16{};
+    const uint16_t* qp = a.q + row * a.ldq + h * HD + 8 * hh;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) {
+        u32x4 x = {0, 0, 0, 0};
+        if (live) x = *reinterpret_cast<const u32x4*>(qp + 16 * i);
+        w.q[i] = __builtin_bit_cast(bf16x8, x);
+    }
+    // what the tile's last row sees, and what this wave's first and last row see
+    const int any = a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0, all = min(seen(tile0), any);
+    const int w0 = tile0 + 32 * wave;
+    const int w_any = w0 < n_rows ? min(seen(min(w0 + 32, n_rows) - 1), any) : 0, w_all = w0 < n_rows ? min(seen(w0), any) : 0;
+    KeyStage<HD> st;
+    auto put = [&](int i) {                            // stage i into its buffer
+        char* kt = lds + 2 * B * (i & 1);
+        if (st.kb + STG <= all && st.there == 15u) st.template put<false>(kt, kt + B, any);
+        else if (st.template put<true>(kt, kt + B, any)) flags[i & 1] = i;
+    };
+    const int n = any > k0 ? (any - k0 + STG - 1) / STG : 0;
+    if (threadIdx.x < 2) flags[threadIdx.x] = -1;
+    __syncthreads();
+    uint32_t there = 0, there_next = 0;
+    if (n > 0) {
+        st.load(a, table, head, k0, any);
+        there = st.there;
+        put(0);
+        if (n > 1) st.load(a, table, head, k0 + STG, any);
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        const int kb = k0 + STG * i;
+        if (i + 1 < n) {
+            there_next = st.there;
+            put(i + 1);
+            if (i + 2 < n) st.load(a, table, head, kb + 2 * STG, any);
+        }
+        const char *kt = lds + 2 * B * (i & 1), *vt = kt + B;
+        if (kb + STG <= w_all && there == 15u) {
+            wide_block<HD, false>(w, kt, vt, kb, there, a.c, lane);
+        } else if (kb < w_any) {
+            wide_block<HD, true>(w, kt, vt, kb, there, a.c, lane);
+            if (flags[i & 1] == i) {
+#pragma unroll 1
+                for (int k = 0; k < STG; ++k) {
+                    if (!(there >> (k / 16) & 1) || kb + k >= any) continue;
+                    const int64_t page = table[(kb + k) >> a.lg_page];
+                    const uint16_t* x = a.V + (((page * a.hk + head) << a.lg_page) + ((kb + k) & ((1 << a.lg_page) - 1))) * HD;
+#pragma unroll
+                    for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const uint32_t y = x[32 * u + acc_row(v, hh)];
+                            if (not_finite(y) && kb + k < w.lim) w.o[u][v] += bf16_to_f32(y);
+                        }
+                }
+            }
+        }
+        there = there_next;
+        __syncthreads();
+    }
+    // lane (hh, row): elements 32 u + 8 j + 4 hh .. + 3 in o[u][4 j ..]
+    const float l = w.l + __shfl_xor(w.l, 32);
+    if (!live) return;
+    const int64_t id = row * a.hq + h;
+    if (a.direct) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t* y = a.out + row * a.ldo + h * HD + 4 * hh;
+#pragma unroll
+        for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const u32x2 x = {pack_bf16x2(w.o[u][4 * j] * inv, w.o[u][4 * j + 1] * inv),
+                                 pack_bf16x2(w.o[u][4 * j + 2] * inv, w.o[u][4 * j + 3] * inv)};
+                *reinterpret_cast<u32x2*>(y + 32 * u + 8 * j) = x;
+            }
+        if (a.lse && hh == 0) a.lse[h * a.T + row] = l == 0.0f ? -INFINITY : (w.m + log2f(l)) * kLn2;
+    } else {
+        float* y = a.part + (slot * a.rows + id) * HD + 4 * hh;
+#pragma unroll
+        for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<f32x4*>(y + 32 * u + 8 * j) =
+                    f32x4{w.o[u][4 * j], w.o[u][4 * j + 1], w.o[u][4 * j + 2], w.o[u][4 * j + 3]};
+        if (hh == 0) *reinterpret_cast<float2*>(a.ml + 2 * (slot * a.rows + id)) = make_float2(w.m, l);
+    }
+}
+
 // Parts of the keys that a request of `end` own tokens has.
 __device__ __forceinline__ int parts_of(const Args& a, int end) {
     return a.splits_s > 0 ? min((end + a.chunk_s - 1) / a.chunk_s, a.splits_s) : 0;
 }
 
-template <int HD, int NTP, int NTS>
-__global__ __launch_bounds__(NTHR, 1) void prefix_attn_kernel(const Args a) {
-    constexpr int NTM = NTP > NTS ? NTP : NTS;
-    __shared__ __attribute__((aligned(16))) float lds[2 * kStateFloats<HD, NTM>];
+// Rows of a tile whose kind is n: 16 n, keys in registers, or a wide one.
+constexpr int WIDE = 8;
+template <int HD, int N>
+constexpr int kLdsBytes = N == WIDE ? kWideBytes<HD> : 8 * kStateFloats<HD, N>;
+
+template <int HD, int N, bool CAUSAL>
+__device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
+                                         int n_rows, int first, int end, int k0, int chunk, int slot) {
+    if constexpr (N == WIDE)
+        wide_item<HD, CAUSAL>(a, lds, table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+    else
+        item<HD, N, CAUSAL>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+}
+
+// NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
+template <int HD, int NP, int NS>
+__global__ __launch_bounds__(NTHR, (NP == WIDE ? 2 : 1)) void prefix_attn_kernel(const Args a) {
+    constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
     for (int64_t at = blockIdx.x; at < a.items; at += gridDim.x) {
         if (at != blockIdx.x) __syncthreads();          // the item before has left the LDS
         if (at < a.items_p) {
@@ -429,10 +675,10 @@ __global__ __launch_bounds__(NTHR, 1) void prefix_attn_kernel(const Args a) {
             const int head = b % a.hk, split = b / a.hk;
             // rows of the batch up to the last that holds a token
             const int64_t hi = a.start ? min(max((int64_t)a.start[a.n_req], (int64_t)0), a.T) : min((int64_t)a.n_req, a.T);
-            const int tile0 = tile * 16 * NTP, n_rows = (int)hi * a.g;
+            const int tile0 = tile * 16 * NP, n_rows = (int)hi * a.g;
             if (tile0 < n_rows)
-                item<HD, NTP, false>(a, lds, a.prefix_table, head, 0, tile0, n_rows, 0, a.prefix, split * a.chunk_p,
-                                     a.chunk_p, split);
+                any_item<HD, NP, false>(a, lds, a.prefix_table, head, 0, tile0, n_rows, 0, a.prefix, split * a.chunk_p,
+                                        a.chunk_p, split);
         } else {
             int64_t b = at - a.items_p;
             const int tile = (int)(b % a.tiles_s);
@@ -441,10 +687,10 @@ __global__ __launch_bounds__(NTHR, 1) void prefix_attn_kernel(const Args a) {
             b /= a.hk;
             const int split = (int)(b % a.splits_s), r = (int)(b / a.splits_s);
             const Span s = span_of(a, r);
-            const int tile0 = tile * 16 * NTS, n_rows = s.n * a.g;
+            const int tile0 = tile * 16 * NS, n_rows = s.n * a.g;
             if (tile0 < n_rows && (a.direct || split < parts_of(a, s.end)))
-                item<HD, NTS, true>(a, lds, a.table + r * a.max_pages, head, s.row, tile0, n_rows, s.first, s.end,
-                                    split * a.chunk_s, a.chunk_s, a.splits_p + split);
+                any_item<HD, NS, true>(a, lds, a.table + r * a.max_pages, head, s.row, tile0, n_rows, s.first, s.end,
+                                       split * a.chunk_s, a.chunk_s, a.splits_p + split);
         }
     }
 }
@@ -503,12 +749,15 @@ Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAtt
 template <int HD>
 hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t s) {
     if (p.nt_p == 1) prefix_attn_kernel<HD, 1, 1><<<grid, NTHR, 0, s>>>(a);
-    else if (p.nt_s == 1) prefix_attn_kernel<HD, 2, 1><<<grid, NTHR, 0, s>>>(a);
-    else prefix_attn_kernel<HD, 2, 2><<<grid, NTHR, 0, s>>>(a);
+    else if (p.nt_p == 2 && p.nt_s == 1) prefix_attn_kernel<HD, 2, 1><<<grid, NTHR, 0, s>>>(a);
+    else if (p.nt_p == 2) prefix_attn_kernel<HD, 2, 2><<<grid, NTHR, 0, s>>>(a);
+    else if (p.nt_s == 1) prefix_attn_kernel<HD, WIDE, 1><<<grid, NTHR, 0, s>>>(a);
+    else if (p.nt_s == 2) prefix_attn_kernel<HD, WIDE, 2><<<grid, NTHR, 0, s>>>(a);
+    else prefix_attn_kernel<HD, WIDE, WIDE><<<grid, NTHR, 0, s>>>(a);
     return hipGetLastError();
 }
 
-int columns(int64_t rows) { return rows <= 16 ? 1 : 2; }
+int columns(int64_t rows) { return rows <= 16 ? 1 : (rows <= 32 ? 2 : WIDE); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
@@ -536,7 +785,7 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
         }
         int64_t k = ceil_div(ceil_div(keys, KB), chunk);
         if (k > 64) k = 64;
-        *len = ceil_div(ceil_div(keys, k), KB) * KB;
+        *len = ceil_div(ceil_div(keys, k), STG) * STG;
         *n = (int)ceil_div(keys, *len);
     };
     parts(sh.prefix, &p.splits_p, &p.chunk_p);
