@@ -51,21 +51,38 @@
 #include "internal.hpp"
 #include "block.hpp"
 #include "device_math.hpp"
-#include "row_tile.hpp"
 
 namespace cola {
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4* lptr4_t;
 
 constexpr int NW = 4;            // waves per workgroup
 constexpr int WB = 32;           // queries (keys) per wave
 constexpr int CHUNK = NW * WB;   // queries (keys) per workgroup
+constexpr int STG = 64;          // rows (keys or queries) staged in LDS per barrier pair: two 32-row sub-blocks
 constexpr float kLog2e = 1.4426950408889634f;
 // 1 / sqrt(HD), the scale of the scores
 template <int HD>
 constexpr float kScale = HD == 64 ? 0.125f : 0.08838834764831845f;
 
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
 __device__ __forceinline__ bf16x8 as_frag(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+// exp2 by the hardware instruction alone (no range reduction for denormal
+// results): its arguments here are scores minus their running maximum or
+// minus the log-sum-exp, so a result it flushes to zero is below 2^-126 and
+// far below the bf16 resolution of the probabilities it feeds.
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ void unpack8(u32x4 v, float (&f)[8]) {
 #pragma unroll
@@ -158,6 +175,38 @@ __device__ __forceinline__ void load_row_frags(bf16x8 (&f)[HD / 16], const uint1
     row_frags<HD, ROT>(f, raw, pos, rope, hh);
 }
 
+// LDS tile of STG rows x HD, row-major, 16-byte chunks XOR-swizzled by the
+// row (conflict-free fragment reads of both kinds below).
+template <int HD>
+struct RowTile {
+    static constexpr int BYTES = STG * HD * 2;
+    __device__ static __forceinline__ int off(int row, int chunk) { return row * (HD * 2) + ((chunk ^ (row & 7)) << 4); }
+    // A-operand fragment of step s (HD elements 16 s ..) for rows r0 .. r0 + 31
+    // (lane: row r0 + lane % 32)
+    __device__ static __forceinline__ bf16x8 frag(const char* t, int r0, int s, int lane) {
+        const int row = r0 + (lane & 31);
+        return *reinterpret_cast<const bf16x8*>(t + off(row, 2 * s + (lane >> 5)));
+    }
+    // A-operand fragment of the transpose: 32 HD elements (tile nt) x 16 rows
+    // (step s of the 32-row sub-block at r0), by two transposing reads.  Lane
+    // (n = 32 nt + lane % 32, hh = lane / 32) receives rows
+    // r0 + 16 s + 4 hh + 0..3 and r0 + 16 s + 8 + 4 hh + 0..3 at element n --
+    // the order in which the transposed score tile leaves those rows in a
+    // lane's accumulator registers 8 s .. 8 s + 7.  (In each 16-lane group,
+    // lanes 4q .. 4q + 3 point at row q of a 4 x 16 block, four consecutive
+    // elements each, and lane i receives element i of the block.)
+    __device__ static __forceinline__ bf16x8 frag_tr(const char* t, int r0, int nt, int s, int lane) {
+        const int g = lane >> 4, i = lane & 15;
+        const int m = 32 * nt + 16 * (g & 1) + 4 * (i & 3);
+        const int k = r0 + 16 * s + 4 * (g >> 1) + (i >> 2);
+        const int byte = (m & 7) * 2;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)(t + off(k, m >> 3) + byte));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)(t + off(k + 8, m >> 3) + byte));
+        const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        return __builtin_bit_cast(bf16x8, v);
+    }
+};
+
 // STG rows (sequence positions p0 .. p0 + STG - 1, zeros from L on) of one
 // head on their way into a row-major LDS tile: load() brings this thread's
 // share into registers (issued a stage ahead, so the loads fly during the
@@ -209,6 +258,9 @@ struct Stage {
     }
 };
 
+// Row (key or query) of register v of a 32 x 32 accumulator, within its tile.
+__device__ __forceinline__ int acc_row(int v, int hh) { return 8 * (v >> 2) + 4 * hh + (v & 3); }
+
 // Store a [HD rows x 32 columns] accumulator set (tiles nt = 0 .. HD/32 - 1,
 // transposed output: column = this lane's token, rows = head elements) as
 // bf16 into the token's row, scaled, with RoPE's transpose when ROT.
@@ -253,6 +305,13 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[HD / 32], float s
             w[1] = pack_bf16x2(x[t][4 * g + 2], x[t][4 * g + 3]);
             *reinterpret_cast<u32x2*>(out + row * ld + col0 + n) = w;
         }
+}
+
+// Max with lane l ^ 32 (the other half of a query's scores) by one
+// v_permlane32_swap.
+__device__ __forceinline__ float xor32_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // Probabilities may reach 2^kSlack against a stale softmax reference.

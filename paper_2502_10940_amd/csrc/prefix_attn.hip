@@ -34,12 +34,19 @@
 
 #include "serve.hpp"
 #include "device_math.hpp"
-#include "row_tile.hpp"
 
 namespace cola {
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4* lptr4_t;
+typedef __attribute__((address_space(3))) void* lptr_t;
 
 constexpr int NW = 4;                     // waves per workgroup
 constexpr int KB = 32;                    // keys per block of a wave
@@ -71,6 +78,13 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// exp2 by the hardware instruction alone: results that it flushes to zero are far
+// below the resolution of what they are added to.
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // The maximum and the sum over lanes l, l ^ 16, l ^ 32, l ^ 48: a column's four.
 __device__ __forceinline__ float column_max(float x) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -86,6 +100,13 @@ __device__ __forceinline__ float column_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// An entry of the tables, lengths and starts, which no launch of this file writes:
+// through the constant address space, so that it comes by the scalar unit and no
+// wait for it is one for the vector loads in flight.
+__device__ __forceinline__ int entry(const int32_t* p, int64_t i) {
+    return ((const __attribute__((address_space(4))) int32_t*)p)[i];
+}
+
 // Request r, from whatever the arrays hold: its first row and how many (at most
 // max_new), and of its own tokens the index of the first new one and the end.
 struct Span {
@@ -96,12 +117,12 @@ __device__ __forceinline__ Span span_of(const Args& a, int r) {
     int64_t all = r < a.T ? 1 : 0;
     s.row = r;
     if (a.start) {
-        const int64_t lo = min(max((int64_t)a.start[r], (int64_t)0), a.T), hi = min((int64_t)a.start[r + 1], a.T);
+        const int64_t lo = min(max((int64_t)entry(a.start, r), (int64_t)0), a.T), hi = min((int64_t)entry(a.start, r + 1), a.T);
         s.row = (int)lo;
         all = max(hi - lo, (int64_t)0);
     }
     s.n = (int)min(all, (int64_t)a.max_new);
-    const int kv = a.max_kv > 0 ? max(a.kv_len[r], 0) : 0;
+    const int kv = a.max_kv > 0 ? max(entry(a.kv_len, r), 0) : 0;
     s.first = (int)(kv - all);
     s.end = min(kv, a.max_kv);
     return s;
@@ -162,7 +183,7 @@ struct Place {
 };
 __device__ __forceinline__ Place place(const Args& a, const int32_t* table, int head, int k0, int end) {
     const int k = min(k0, (end - 1) & ~15);
-    const int64_t page = table[k >> a.lg_page];
+    const int64_t page = entry(table, k >> a.lg_page);
     Place p;
     p.there = page >= 0 && page < a.n_pages;
     p.row = (((p.there ? page : 0) * a.hk + head) << a.lg_page) + (k & ((1 << a.lg_page) - 1));
@@ -406,92 +427,80 @@ __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* t
 // ---------------------------------------------------------------------------
 // Many rows: a tile of 128, 32 to a wave, against keys staged in LDS
 // ---------------------------------------------------------------------------
+//
+// Stages of 64 keys, double buffered, loaded straight into LDS while the stage
+// before is used; wave w loads the w-th 16 keys, which lie in one page.  A wave
+// multiplies with v_mfma_f32_32x32x16_bf16: S^T = K Q^T leaves a lane 32 scores of
+// one row (lane l, register v: key 8 (v / 4) + 4 (l / 32) + v % 4 of 32, row l %
+// 32), and registers 8 i .. 8 i + 7 are the 8 probabilities that the second
+// product O^T += V^T P^T wants from that lane when V's rows come in the same
+// order, which the transposing LDS reads give.
 
 constexpr int WROWS = 32 * NW;            // rows of a wide tile
+constexpr int STG = 16 * NW;              // keys of a stage
 
-// STG keys of one head on their way into LDS: load() has them in registers while
-// the stage before is used, put() writes them.  Tiles of 16 keys lie in one page.
+// A stage's keys or values in LDS: [STG][HD] bf16, 16-byte chunk c of row r at chunk
+// c ^ swz(r).  The swizzle gives 16 rows of one chunk, and four neighbouring rows of
+// 64 bytes, all 64 banks once: the reads of the two products.
 template <int HD>
-struct KeyStage {
-    static constexpr int CPR = HD / 8;                 // 16-byte chunks per row
-    static constexpr int RPI = NTHR / CPR;             // rows that one instruction of the workgroup covers
-    static constexpr int NI = STG / RPI;
-    u32x4 k[NI], v[NI];
-    int kb;                                            // first key
-    uint32_t there;                                    // bit i: the page of keys kb + 16 i .. is in the cache
-
-    // Tile of 16 of this thread's rows in step `it`: the same for all lanes of a wave.
-    __device__ static __forceinline__ int tile(int it) {
-        return (RPI * it + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / CPR)) / 16;
+struct KeyTile {
+    static constexpr int ROW = 2 * HD, BYTES = STG * ROW;
+    static constexpr int CPR = HD / 8;                 // chunks per row
+    static constexpr int RPI = 64 / CPR;               // rows of a 1 KB load
+    static constexpr int NL = 16 / RPI;                // loads of 16 rows
+    __device__ static __forceinline__ int swz(int row) {
+        const int x = HD == 128 ? row & 15 : (row >> 1) & 7;
+        return HD == 128 ? ((x & 3) << 2) | (x >> 2) : ((x & 1) << 2) | (x >> 1);
     }
-
-    __device__ __forceinline__ void load(const Args& a, const int32_t* table, int head, int first, int end) {
-        kb = first;
-        there = 0;
-        Place at[STG / 16];
-#pragma unroll
-        for (int i = 0; i < STG / 16; ++i) {
-            at[i] = place(a, table, head, kb + 16 * i, end);
-            there |= (uint32_t)at[i].there << i;
-        }
-#pragma unroll
-        for (int it = 0; it < NI; ++it) {
-            int64_t b;
-            if constexpr (NI == 4) {
-                b = at[it].row;
-            } else {
-                const int64_t lo = at[2 * it].row, hi = at[2 * it + 1].row;
-                b = tile(it) & 1 ? hi : lo;
-            }
-            const int row = (threadIdx.x / CPR + RPI * it) & 15, c = threadIdx.x % CPR;
-            k[it] = *reinterpret_cast<const u32x4*>(a.K + b * HD + (row * HD + 8 * c));
-            v[it] = *reinterpret_cast<const u32x4*>(a.V + b * HD + (row * HD + 8 * c));
-        }
+    __device__ static __forceinline__ int off(int row, int chunk) { return row * ROW + ((chunk ^ swz(row)) << 4); }
+    // Load j of a tile of 16 rows: where this lane reads, from the tile's first byte.
+    __device__ static __forceinline__ uint32_t from(int j, int lane) {
+        const int row = RPI * j + lane / CPR;
+        return row * ROW + (((lane % CPR) ^ swz(row)) << 4);
     }
-
-    // MASK: values that no row sees (from `end` on, or of a missing page) become
-    // zeros, and those that are not finite, too (true: there are some).
-    template <bool MASK>
-    __device__ __forceinline__ bool put(char* kt, char* vt, int end) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int it = 0; it < NI; ++it) {
-            const int row = threadIdx.x / CPR + RPI * it, c = threadIdx.x % CPR;
-            if constexpr (MASK) {
-                if (!(there >> tile(it) & 1) || kb + row >= end) v[it] = u32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    any |= not_finite2(v[it][x]);
-                    v[it][x] = finite2(v[it][x]);
-                }
-            }
-            *reinterpret_cast<u32x4*>(kt + RowTile<HD>::off(row, c)) = k[it];
-            *reinterpret_cast<u32x4*>(vt + RowTile<HD>::off(row, c)) = v[it];
-        }
-        return any != 0;
+    // K operand, step i: elements 16 i + 8 (lane / 32) .. of row lane % 32.
+    __device__ static __forceinline__ int key_at(int i, int lane) { return off(lane & 31, 2 * i + (lane >> 5)); }
+    // V^T operand of output tile t: element 32 t + lane % 32 of the rows 4 (lane /
+    // 32) .. + 3 (x = 0) or 8 more (x = 1).  In each 16-lane group lanes 4 q .. 4 q +
+    // 3 point at row q, four consecutive elements each; lane i gets column i.
+    __device__ static __forceinline__ int val_at(int t, int x, int lane) {
+        const int g = lane >> 4, i = lane & 15;
+        const int m = 32 * t + 16 * (g & 1) + 4 * (i & 3);
+        return off(8 * x + 4 * (g >> 1) + (i >> 2), m >> 3) + (m & 7) * 2;
     }
 };
+
+__device__ __forceinline__ bf16x8 lds_frag(const char* p) { return *reinterpret_cast<const bf16x8*>(p); }
+__device__ __forceinline__ bf16x8 lds_frag_tr(const char* p, const char* q) {
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)q);
+    const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(bf16x8, v);
+}
+// Element of a 32-row accumulator register.
+__device__ __forceinline__ int acc_row(int v, int hh) { return 8 * (v >> 2) + 4 * hh + (v & 3); }
 
 template <int HD>
 struct WideWave {
     bf16x8 q[HD / 16];
     f32x16 o[HD / 32];
     float m, l;                                        // l: of this lane's keys
-    int lim;
+    int lim;                                           // keys that this lane's row sees
+    int key[HD / 16], val[HD / 32][2];                 // LDS addresses within a tile
 };
 
-// The 64 keys of a stage: one online-softmax step of this lane's row.
-template <int HD, bool MASK>
-__device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, const char* vt, int kb, uint32_t there,
-                                           float c, int lane) {
-    const int hh = lane >> 5;
-    f32x16 s[2];
+// The keys kb .. of a stage (K at kt, V behind it): one online-softmax step of this
+// lane's row.  MASK: some row does not see all of them.  ODD: and a key that one
+// row sees and another does not may hold values that are not finite; those
+// leave the product (0 * inf), and true is returned if there are any.
+template <int HD, bool MASK, bool ODD>
+__device__ __forceinline__ bool wide_block(WideWave<HD>& w, const char* kt, int kb, uint32_t there, float c, int hh) {
+    typedef KeyTile<HD> Tile;
+    f32x16 s[2] = {f32x16{}, f32x16{}};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        s[b] = f32x16{};
+    for (int i = 0; i < HD / 16; ++i)
 #pragma unroll
-        for (int i = 0; i < HD / 16; ++i) s[b] = mfma(RowTile<HD>::frag(kt, 32 * b, i, lane), w.q[i], s[b]);
-    }
+        for (int b = 0; b < 2; ++b) s[b] = mfma32(lds_frag(kt + w.key[i] + 32 * b * Tile::ROW), w.q[i], s[b]);
     if constexpr (MASK) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -506,7 +515,8 @@ __device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, cons
     for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int v = 0; v < 16; v += 2) mb = fmaxf(fmaxf(mb, s[b][v]), s[b][v + 1]);
-    mb = xor32_max(mb) * c;
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
+    mb = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * c;
     if (__ballot(mb > w.m + kSlack) != 0) {
         const float mn = fmaxf(w.m, mb);
         const float alpha = exp2_hw(w.m - mn);
@@ -515,6 +525,8 @@ __device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, cons
         for (int t = 0; t < HD / 32; ++t) w.o[t] *= alpha;
         w.m = mn;
     }
+    uint32_t odd = 0;
+    const char* vt = kt + Tile::BYTES;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -527,22 +539,36 @@ __device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, cons
                 f[j] = pack_bf16x2(x, y);
             }
             const bf16x8 p = __builtin_bit_cast(bf16x8, f);
+            const char* v0 = vt + (32 * b + 16 * i) * Tile::ROW;
 #pragma unroll
-            for (int t = 0; t < HD / 32; ++t) w.o[t] = mfma(RowTile<HD>::frag_tr(vt, 32 * b, t, i, lane), p, w.o[t]);
+            for (int t = 0; t < HD / 32; ++t) {
+                bf16x8 v = lds_frag_tr(v0 + w.val[t][0], v0 + w.val[t][1]);
+                if constexpr (ODD) {
+                    u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        odd |= not_finite2(x[e]);
+                        x[e] = finite2(x[e]);
+                    }
+                    v = __builtin_bit_cast(bf16x8, x);
+                }
+                w.o[t] = mfma32(v, p, w.o[t]);
+            }
         }
+    return ODD && __ballot(odd != 0) != 0;
 }
 
-// Bytes of LDS: two stages of keys and values, and their flags.
+// LDS of two stages of keys and values.
 template <int HD>
-constexpr int kWideBytes = 4 * RowTile<HD>::BYTES + 16;
+constexpr int kWideBytes = 4 * KeyTile<HD>::BYTES;
 
 // item() for a tile of 128 rows: the same rows, keys and results.
 template <int HD, bool CAUSAL>
 __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
                                           int n_rows, int first, int end, int k0, int chunk, int slot) {
-    constexpr int B = RowTile<HD>::BYTES;
+    typedef KeyTile<HD> Tile;
+    constexpr int B = Tile::BYTES;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
-    int* flags = reinterpret_cast<int*>(lds + 4 * B);  // the stage of each buffer that holds values that are not finite
     auto seen = [&](int rho) { return CAUSAL ? (int)min((int64_t)first + 1 + rho / a.g, (int64_t)end) : end; };
     const int rho = tile0 + 32 * wave + (lane & 31), t = rho / a.g;
     const bool live = rho < n_rows;
@@ -553,66 +579,97 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
     w.l = 0.0f;
     w.lim = live ? seen(rho) : 0;
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) w.o[i] = f32x16{};
+    for (int i = 0; i < HD / 32; ++i) {
+        w.o[i] = f32x16{};
+        w.val[i][0] = Tile::val_at(i, 0, lane);
+        w.val[i][1] = Tile::val_at(i, 1, lane);
+    }
     const uint16_t* qp = a.q + row * a.ldq + h * HD + 8 * hh;
 #pragma unroll
     for (int i = 0; i < HD / 16; ++i) {
         u32x4 x = {0, 0, 0, 0};
         if (live) x = *reinterpret_cast<const u32x4*>(qp + 16 * i);
         w.q[i] = __builtin_bit_cast(bf16x8, x);
+        w.key[i] = Tile::key_at(i, lane);
     }
+    uint32_t from[Tile::NL];
+#pragma unroll
+    for (int j = 0; j < Tile::NL; ++j) from[j] = Tile::from(j, lane);
     // what the tile's last row sees, and what this wave's first and last row see
-    const int any = a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0, all = min(seen(tile0), any);
+    const int any = a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0;
     const int w0 = tile0 + 32 * wave;
     const int w_any = w0 < n_rows ? min(seen(min(w0 + 32, n_rows) - 1), any) : 0, w_all = w0 < n_rows ? min(seen(w0), any) : 0;
-    KeyStage<HD> st;
-    auto put = [&](int i) {                            // stage i into its buffer
-        char* kt = lds + 2 * B * (i & 1);
-        if (st.kb + STG <= all && st.there == 15u) st.template put<false>(kt, kt + B, any);
-        else if (st.template put<true>(kt, kt + B, any)) flags[i & 1] = i;
-    };
     const int n = any > k0 ? (any - k0 + STG - 1) / STG : 0;
-    if (threadIdx.x < 2) flags[threadIdx.x] = -1;
-    __syncthreads();
-    uint32_t there = 0, there_next = 0;
-    if (n > 0) {
-        st.load(a, table, head, k0, any);
-        there = st.there;
-        put(0);
-        if (n > 1) st.load(a, table, head, k0 + STG, any);
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int i = 0; i < n; ++i) {
+
+    // Stage i into the buffer at `to`: keys from `any` on and missing pages arrive as
+    // zeros (they lie past the descriptor's range).  Returns the pages that are there.
+    auto load = [&](int i, char* to) __attribute__((always_inline)) -> uint32_t {
         const int kb = k0 + STG * i;
-        if (i + 1 < n) {
-            there_next = st.there;
-            put(i + 1);
-            if (i + 2 < n) st.load(a, table, head, kb + 2 * STG, any);
+        uint32_t there = 0;
+        Place mine{};
+#pragma unroll
+        for (int x = 0; x < NW; ++x) {
+            const Place p = place(a, table, head, kb + 16 * x, any);
+            there |= (uint32_t)p.there << x;
+            if (x == wave) mine = p;
         }
-        const char *kt = lds + 2 * B * (i & 1), *vt = kt + B;
-        if (kb + STG <= w_all && there == 15u) {
-            wide_block<HD, false>(w, kt, vt, kb, there, a.c, lane);
-        } else if (kb < w_any) {
-            wide_block<HD, true>(w, kt, vt, kb, there, a.c, lane);
-            if (flags[i & 1] == i) {
+        const int rows = mine.there ? min(max(any - (kb + 16 * wave), 0), 16) : 0;
+        to += 16 * wave * Tile::ROW;
+        const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.K + mine.row * HD), (short)0, rows * Tile::ROW, 0x00020000);
+        const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.V + mine.row * HD), (short)0, rows * Tile::ROW, 0x00020000);
+#pragma unroll
+        for (int j = 0; j < Tile::NL; ++j) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lptr_t)(to + 1024 * j), 16, from[j], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lptr_t)(to + B + 1024 * j), 16, from[j], 0, 0, 0);
+        }
+        return there;
+    };
+    // The next stage has landed, and every wave has left this one.
+    auto turn = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    uint32_t there = 0, next = 0;
+    // Stage i from one buffer while the next is loaded into the other: the
+    // __restrict parameters say that they don't overlap (without them the compiler
+    // waits for the loads in flight before the first read).
+    auto whole = [&](char* __restrict to, const char* __restrict kt, int i) __attribute__((always_inline)) {
+        next = i + 1 < n ? load(i + 1, to) : 0;
+        wide_block<HD, false, false>(w, kt, k0 + STG * i, 15u, a.c, hh);
+    };
+    auto part = [&](char* __restrict to, const char* __restrict kt, int i) __attribute__((always_inline)) {
+        const int kb = k0 + STG * i;
+        next = i + 1 < n ? load(i + 1, to) : 0;
+        if (kb >= w_any || !wide_block<HD, true, CAUSAL>(w, kt, kb, there, a.c, hh)) return;
+        // values that are not finite, to the rows that see them
 #pragma unroll 1
-                for (int k = 0; k < STG; ++k) {
-                    if (!(there >> (k / 16) & 1) || kb + k >= any) continue;
-                    const int64_t page = table[(kb + k) >> a.lg_page];
-                    const uint16_t* x = a.V + (((page * a.hk + head) << a.lg_page) + ((kb + k) & ((1 << a.lg_page) - 1))) * HD;
+        for (int k = 0; k < min(STG, any - kb); ++k) {
+            if (!(there >> (k / 16) & 1)) continue;
+            const uint16_t* x = a.V + (place(a, table, head, kb + (k & ~15), any).row + (k & 15)) * HD;
 #pragma unroll
-                    for (int u = 0; u < HD / 32; ++u)
+            for (int u = 0; u < HD / 32; ++u)
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const uint32_t y = x[32 * u + acc_row(v, hh)];
-                            if (not_finite(y) && kb + k < w.lim) w.o[u][v] += bf16_to_f32(y);
-                        }
+                for (int v = 0; v < 16; ++v) {
+                    const uint32_t y = x[32 * u + acc_row(v, hh)];
+                    if (not_finite(y) && kb + k < w.lim) w.o[u][v] += bf16_to_f32(y);
                 }
-            }
         }
-        there = there_next;
-        __syncthreads();
+    };
+    if (n > 0) there = load(0, lds);
+    turn();
+    int i = 0;
+    while (i < n) {
+#pragma unroll 1
+        for (; i < n && k0 + STG * (i + 1) <= w_all && there == 15u; ++i) {
+            whole(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
+            there = next;
+            turn();
+        }
+        if (i < n) {
+            part(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
+            there = next;
+            turn();
+            ++i;
+        }
     }
     // lane (hh, row): elements 32 u + 8 j + 4 hh .. + 3 in o[u][4 j ..]
     const float l = w.l + __shfl_xor(w.l, 32);
@@ -674,7 +731,7 @@ __global__ __launch_bounds__(NTHR, (NP == WIDE ? 2 : 1)) void prefix_attn_kernel
             b /= a.tiles_p;
             const int head = b % a.hk, split = b / a.hk;
             // rows of the batch up to the last that holds a token
-            const int64_t hi = a.start ? min(max((int64_t)a.start[a.n_req], (int64_t)0), a.T) : min((int64_t)a.n_req, a.T);
+            const int64_t hi = a.start ? min(max((int64_t)entry(a.start, a.n_req), (int64_t)0), a.T) : min((int64_t)a.n_req, a.T);
             const int tile0 = tile * 16 * NP, n_rows = (int)hi * a.g;
             if (tile0 < n_rows)
                 any_item<HD, NP, false>(a, lds, a.prefix_table, head, 0, tile0, n_rows, 0, a.prefix, split * a.chunk_p,
