@@ -31,6 +31,7 @@
 // No LDS, no transposing pass, no barrier in the loop: key and value bytes go
 // from memory to the matrix unit.
 #include <math.h>
+#include <stdlib.h>
 
 #include "serve.hpp"
 #include "device_math.hpp"
@@ -67,7 +68,7 @@ struct Args {
     int64_t ldq, ldo, rows, max_pages, n_pages, T;
     int n_req, hq, hk, g, lg_page;
     int prefix, max_kv, max_new;
-    int64_t items, items_p;
+    int64_t blocks, items_p, items_s;     // workgroups' turns, work items of either part
     int tiles_p, splits_p, chunk_p;
     int tiles_s, splits_s, chunk_s;
     int direct;                           // one part in all, of the requests' own keys: the item writes the result
@@ -105,6 +106,12 @@ __device__ __forceinline__ float column_sum(float x) {
 // wait for it is one for the vector loads in flight.
 __device__ __forceinline__ int entry(const int32_t* p, int64_t i) {
     return ((const __attribute__((address_space(4))) int32_t*)p)[i];
+}
+
+// Wave-uniform values kept in scalar registers (a descriptor's parts must be).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
 // Request r, from whatever the arrays hold: its first row and how many (at most
@@ -183,38 +190,62 @@ struct Place {
 };
 __device__ __forceinline__ Place place(const Args& a, const int32_t* table, int head, int k0, int end) {
     const int k = min(k0, (end - 1) & ~15);
-    const int64_t page = entry(table, k >> a.lg_page);
+    const int64_t page = uniform(entry(table, k >> a.lg_page));
     Place p;
     p.there = page >= 0 && page < a.n_pages;
     p.row = (((p.there ? page : 0) * a.hk + head) << a.lg_page) + (k & ((1 << a.lg_page) - 1));
     return p;
 }
 
-// One block of 32 keys from kb on, at the places at[0], at[1].  MASK: some row does
-// not see all of them, or a page is missing; keys from `end` on hold no tokens.
-template <int HD, int NT, bool MASK>
-__device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const Place (&at)[2], int kb, int end, int lane) {
-    constexpr int KK = HD / 32, D = HD / 16;
+// Descriptor of `rows` rows of HD from row `at` on; reads past them give zeros.
+template <int HD>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* base, int64_t at, int rows) {
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(uniform64((int64_t)(base + at * HD))), (short)0,
+                                             uniform(rows) * 2 * HD, 0x00020000);
+}
+
+// The keys and values of one block of 32 keys in a wave's registers; keys from
+// `end` on and those of missing pages are zeros.
+template <int HD>
+struct Keys {
+    static constexpr int KK = HD / 32, D = HD / 16;
     typedef typename VRow<D>::type R;
-    const int g = lane >> 4, c = lane & 15;
-    u32x4 kf[2][KK];
+    bool there[2];
+    u32x4 k[2][KK];
     R v[8];
+
+    __device__ __forceinline__ void load(const Args& a, const int32_t* table, int head, int kb, int end, int lane) {
+        const int g = lane >> 4, c = lane & 15;
+        const int ko = 2 * (c * HD + 8 * g), vo = 2 * (4 * g * HD + D * c);
+        __amdgpu_buffer_rsrc_t rv[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint16_t* p = a.K + at[i].row * HD + c * HD + 8 * g;
+        for (int i = 0; i < 2; ++i) {
+            const Place at = place(a, table, head, kb + 16 * i, end);
+            there[i] = at.there;
+            const int rows = at.there ? min(max(end - (kb + 16 * i), 0), 16) : 0;
+            const __amdgpu_buffer_rsrc_t rk = rows_of<HD>(a.K, at.row, rows);
+            rv[i] = rows_of<HD>(a.V, at.row, rows);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[i][kk] = *reinterpret_cast<const u32x4*>(p + 32 * kk);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint16_t* p = a.V + at[i].row * HD + 4 * g * HD + D * c;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[4 * i + j] = *reinterpret_cast<const R*>(p + j * HD);
-            if constexpr (MASK)
-                if (!at[i].there || kb + 16 * i + 4 * g + j >= end) v[4 * i + j] = R{};
+            for (int kk = 0; kk < KK; ++kk) k[i][kk] = __builtin_amdgcn_raw_buffer_load_b128(rk, ko + 64 * kk, 0, 0);
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (D == 8) v[4 * i + j] = __builtin_amdgcn_raw_buffer_load_b128(rv[i], vo + 2 * HD * j, 0, 0);
+                else v[4 * i + j] = __builtin_amdgcn_raw_buffer_load_b64(rv[i], vo + 2 * HD * j, 0, 0);
+            }
     }
+};
+
+// One block: the keys kb .. kb + 31, those from `end` on without a token.  `part`
+// (wave-uniform): some row does not see all of them, or a page is missing.
+// CAUSAL: the rows see different keys.
+template <int HD, int NT, bool CAUSAL>
+__device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, Keys<HD>& x, const int32_t* table, int head, int kb,
+                                      int end, bool part, int lane) {
+    constexpr int KK = HD / 32, D = HD / 16;
+    const int g = lane >> 4;
     f32x4 s[2][NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -222,23 +253,44 @@ __device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const Plac
         for (int i = 0; i < 2; ++i) {
             s[i][n] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) s[i][n] = mfma16(__builtin_bit_cast(bf16x8, kf[i][kk]), w.q[n][kk], s[i][n]);
+            for (int kk = 0; kk < KK; ++kk) s[i][n] = mfma16(__builtin_bit_cast(bf16x8, x.k[i][kk]), w.q[n][kk], s[i][n]);
         }
+    // A key that some row of the tile sees and another does not must not reach the
+    // second by 0 * inf: values that are not finite leave the product, and go to
+    // the rows that see them by themselves.
+    bool odd = false;
+    if (part) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int first = kb + 16 * i + 4 * g;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int lim = x.there[i] ? w.lim[n] : 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (first + j >= lim) s[i][n][j] = -INFINITY;
+            }
+        }
+        if constexpr (CAUSAL) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int d = 0; d < D / 2; ++d) {
+                    any |= not_finite2(x.v[j][d]);
+                    x.v[j][d] = finite2(x.v[j][d]);
+                }
+            odd = __ballot(any != 0) != 0;
+        }
+    }
     bf16x8 p[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        if constexpr (MASK) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (!at[i].there || kb + 16 * i + 4 * g + j >= w.lim[n]) s[i][n][j] = -INFINITY;
-        }
         float mb = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mb = fmaxf(mb, s[i][n][j]);
+            for (int j = 0; j < 4; j += 2) mb = fmaxf(fmaxf(mb, s[i][n][j]), s[i][n][j + 1]);
         mb = column_max(mb) * a.c;
         if (__ballot(mb > w.m[n] + kSlack) != 0) {
             const float mn = fmaxf(w.m[n], mb);
@@ -262,42 +314,27 @@ __device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, const Plac
         }
         p[n] = __builtin_bit_cast(bf16x8, f);
     }
-    // A key that some row of the tile sees and another does not must not reach the
-    // second by 0 * inf: values that are not finite leave the product, and go to
-    // the rows that see them by themselves.
-    bool odd = false;
-    if constexpr (MASK) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int x = 0; x < D / 2; ++x) {
-                any |= not_finite2(v[j][x]);
-                v[j][x] = finite2(v[j][x]);
-            }
-        odd = __ballot(any != 0) != 0;
-    }
 #pragma unroll
     for (int t = 0; t < D; ++t) {
-        const bf16x8 vf = v_frag<D>(v, t);
+        const bf16x8 vf = v_frag<D>(x.v, t);
 #pragma unroll
         for (int n = 0; n < NT; ++n) w.o[t][n] = mfma16(vf, p[n], w.o[t][n]);
     }
-    if constexpr (MASK) {
+    if constexpr (CAUSAL) {
         if (odd) {
 #pragma unroll 1
-            for (int k = 0; k < KB; ++k) {
-                const int i = k / 16;
-                if (!(i ? at[1].there : at[0].there) || kb + k >= end) continue;
+            for (int k = 0; k < min(KB, end - kb); ++k) {
+                const Place at = place(a, table, head, kb + (k & ~15), end);
+                if (!at.there) continue;
                 // this lane's elements of its rows: 4 D from 4 D g on
-                const uint16_t* x = a.V + ((i ? at[1].row : at[0].row) + k - 16 * i) * HD + 4 * D * g;
+                const uint16_t* y = a.V + (at.row + (k & 15)) * HD + 4 * D * g;
 #pragma unroll
                 for (int e = 0; e < 4 * D; ++e) {
-                    const uint32_t y = x[e];
-                    if (!not_finite(y)) continue;
+                    const uint32_t z = y[e];
+                    if (!not_finite(z)) continue;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        if (kb + k < w.lim[n]) w.o[e % D][n][e / D] += bf16_to_f32(y);
+                        if (kb + k < w.lim[n]) w.o[e % D][n][e / D] += bf16_to_f32(z);
                 }
             }
         }
@@ -345,13 +382,18 @@ __device__ __forceinline__ void take(Wave<HD, NT>& w, const float* buf, int lane
 
 // One work item: rows rho = tile0 .. of the batch's row `row0` on (rho / g tokens
 // further, head rho % g of the group), keys k0 .. of a table that ends at `end`.
-// Row rho sees the keys up to first + rho / g, or all of them.
-template <int HD, int NT, bool CAUSAL>
+// Row rho sees the keys up to first + rho / g, or all of them.  KW = NW: the
+// workgroup's waves share the keys and join through LDS; KW = 1: each wave has an
+// item of its own.
+template <int HD, int NT, int KW, bool CAUSAL>
 __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* table, int head, int row0, int tile0,
                                      int n_rows, int first, int end, int k0, int chunk, int slot) {
     constexpr int KK = HD / 32, D = HD / 16;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int wave = KW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     auto seen = [&](int rho) { return CAUSAL ? (int)min((int64_t)first + 1 + rho / a.g, (int64_t)end) : end; };
+    // keys that the tile's first row sees, and its last
+    const int any = uniform(a.n_pages > 0 ? min(seen(min(tile0 + 16 * NT, n_rows) - 1), k0 + chunk) : 0), all = uniform(min(seen(tile0), any));
     Wave<HD, NT> w;
     w.clear();
     int64_t row[NT];
@@ -373,24 +415,24 @@ __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* t
             w.q[n][kk] = __builtin_bit_cast(bf16x8, x);
         }
     }
-    // keys that the tile's first row sees, and its last
-    const int any = a.n_pages > 0 ? min(seen(min(tile0 + 16 * NT, n_rows) - 1), k0 + chunk) : 0, all = min(seen(tile0), any);
 #pragma unroll 1
-    for (int kb = k0 + KB * wave; kb < any; kb += KB * NW) {
-        const Place at[2] = {place(a, table, head, kb, any), place(a, table, head, kb + 16, any)};
-        if (kb + KB <= all && at[0].there && at[1].there) block<HD, NT, false>(w, a, at, kb, any, lane);
-        else block<HD, NT, true>(w, a, at, kb, any, lane);
+    for (int kb = k0 + KB * wave; kb < any; kb += KB * KW) {
+        Keys<HD> x;
+        x.load(a, table, head, kb, any, lane);
+        block<HD, NT, CAUSAL>(w, a, x, table, head, kb, any, kb + KB > all || !x.there[0] || !x.there[1], lane);
     }
-    // waves 2, 3 into 0, 1, then 1 into 0
-    float* mine = lds + (wave & 1) * kStateFloats<HD, NT>;
-    if (wave >= 2) give<HD, NT>(w, mine, lane);
-    __syncthreads();
-    if (wave < 2) take<HD, NT>(w, mine, lane);
-    __syncthreads();
-    if (wave == 1) give<HD, NT>(w, lds, lane);
-    __syncthreads();
-    if (wave != 0) return;
-    take<HD, NT>(w, lds, lane);
+    if constexpr (KW > 1) {
+        // waves 2, 3 into 0, 1, then 1 into 0
+        float* mine = lds + (wave & 1) * kStateFloats<HD, NT>;
+        if (wave >= 2) give<HD, NT>(w, mine, lane);
+        __syncthreads();
+        if (wave < 2) take<HD, NT>(w, mine, lane);
+        __syncthreads();
+        if (wave == 1) give<HD, NT>(w, lds, lane);
+        __syncthreads();
+        if (wave != 0) return;
+        take<HD, NT>(w, lds, lane);
+    }
     // lane (g, c): row c of each column, elements 4 D g .. 4 D g + 4 D - 1, the
     // element D (4 g + i) + t in o[t][i]
 #pragma unroll
@@ -490,24 +532,24 @@ struct WideWave {
 };
 
 // The keys kb .. of a stage (K at kt, V behind it): one online-softmax step of this
-// lane's row.  MASK: some row does not see all of them.  ODD: and a key that one
-// row sees and another does not may hold values that are not finite; those
-// leave the product (0 * inf), and true is returned if there are any.
-template <int HD, bool MASK, bool ODD>
-__device__ __forceinline__ bool wide_block(WideWave<HD>& w, const char* kt, int kb, uint32_t there, float c, int hh) {
+// lane's row.  `part` (wave-uniform): some row does not see all of them.
+template <int HD>
+__device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, int kb, uint32_t there, bool part, float c, int hh) {
     typedef KeyTile<HD> Tile;
     f32x16 s[2] = {f32x16{}, f32x16{}};
 #pragma unroll
     for (int i = 0; i < HD / 16; ++i)
 #pragma unroll
         for (int b = 0; b < 2; ++b) s[b] = mfma32(lds_frag(kt + w.key[i] + 32 * b * Tile::ROW), w.q[i], s[b]);
-    if constexpr (MASK) {
+    if (part) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int k = 32 * b + acc_row(v, hh);
-                if (!(there >> (2 * b + v / 8) & 1) || kb + k >= w.lim) s[b][v] = -INFINITY;
+            for (int x = 0; x < 2; ++x) {
+                const int lim = there >> (2 * b + x) & 1 ? w.lim - kb - 4 * hh : 0;
+#pragma unroll
+                for (int v = 8 * x; v < 8 * x + 8; ++v)
+                    if (32 * b + acc_row(v, 0) >= lim) s[b][v] = -INFINITY;
             }
     }
     float mb = -INFINITY;
@@ -525,7 +567,6 @@ __device__ __forceinline__ bool wide_block(WideWave<HD>& w, const char* kt, int 
         for (int t = 0; t < HD / 32; ++t) w.o[t] *= alpha;
         w.m = mn;
     }
-    uint32_t odd = 0;
     const char* vt = kt + Tile::BYTES;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -541,26 +582,13 @@ __device__ __forceinline__ bool wide_block(WideWave<HD>& w, const char* kt, int 
             const bf16x8 p = __builtin_bit_cast(bf16x8, f);
             const char* v0 = vt + (32 * b + 16 * i) * Tile::ROW;
 #pragma unroll
-            for (int t = 0; t < HD / 32; ++t) {
-                bf16x8 v = lds_frag_tr(v0 + w.val[t][0], v0 + w.val[t][1]);
-                if constexpr (ODD) {
-                    u32x4 x = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        odd |= not_finite2(x[e]);
-                        x[e] = finite2(x[e]);
-                    }
-                    v = __builtin_bit_cast(bf16x8, x);
-                }
-                w.o[t] = mfma32(v, p, w.o[t]);
-            }
+            for (int t = 0; t < HD / 32; ++t) w.o[t] = mfma32(lds_frag_tr(v0 + w.val[t][0], v0 + w.val[t][1]), p, w.o[t]);
         }
-    return ODD && __ballot(odd != 0) != 0;
 }
 
-// LDS of two stages of keys and values.
+// LDS of two stages of keys and values, and their flags.
 template <int HD>
-constexpr int kWideBytes = 4 * KeyTile<HD>::BYTES;
+constexpr int kWideBytes = 4 * KeyTile<HD>::BYTES + 16;
 
 // item() for a tile of 128 rows: the same rows, keys and results.
 template <int HD, bool CAUSAL>
@@ -596,9 +624,10 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
 #pragma unroll
     for (int j = 0; j < Tile::NL; ++j) from[j] = Tile::from(j, lane);
     // what the tile's last row sees, and what this wave's first and last row see
-    const int any = a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0;
+    const int any = uniform(a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0), all = uniform(min(seen(tile0), any));
     const int w0 = tile0 + 32 * wave;
-    const int w_any = w0 < n_rows ? min(seen(min(w0 + 32, n_rows) - 1), any) : 0, w_all = w0 < n_rows ? min(seen(w0), any) : 0;
+    const int w_any = uniform(w0 < n_rows ? min(seen(min(w0 + 32, n_rows) - 1), any) : 0),
+              w_all = uniform(w0 < n_rows ? min(seen(w0), any) : 0);
     const int n = any > k0 ? (any - k0 + STG - 1) / STG : 0;
 
     // Stage i into the buffer at `to`: keys from `any` on and missing pages arrive as
@@ -615,8 +644,7 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
         }
         const int rows = mine.there ? min(max(any - (kb + 16 * wave), 0), 16) : 0;
         to += 16 * wave * Tile::ROW;
-        const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.K + mine.row * HD), (short)0, rows * Tile::ROW, 0x00020000);
-        const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.V + mine.row * HD), (short)0, rows * Tile::ROW, 0x00020000);
+        const auto rk = rows_of<HD>(a.K, mine.row, rows), rv = rows_of<HD>(a.V, mine.row, rows);
 #pragma unroll
         for (int j = 0; j < Tile::NL; ++j) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lptr_t)(to + 1024 * j), 16, from[j], 0, 0, 0);
@@ -629,47 +657,62 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
     uint32_t there = 0, next = 0;
+    // the last stage of each buffer that held values that are not finite
+    int* odd = reinterpret_cast<int*>(lds + 4 * B);
     // Stage i from one buffer while the next is loaded into the other: the
     // __restrict parameters say that they don't overlap (without them the compiler
     // waits for the loads in flight before the first read).
-    auto whole = [&](char* __restrict to, const char* __restrict kt, int i) __attribute__((always_inline)) {
-        next = i + 1 < n ? load(i + 1, to) : 0;
-        wide_block<HD, false, false>(w, kt, k0 + STG * i, 15u, a.c, hh);
-    };
-    auto part = [&](char* __restrict to, const char* __restrict kt, int i) __attribute__((always_inline)) {
+    auto step = [&](char* __restrict to, char* __restrict kt, int i) __attribute__((always_inline)) {
         const int kb = k0 + STG * i;
         next = i + 1 < n ? load(i + 1, to) : 0;
-        if (kb >= w_any || !wide_block<HD, true, CAUSAL>(w, kt, kb, there, a.c, hh)) return;
-        // values that are not finite, to the rows that see them
-#pragma unroll 1
-        for (int k = 0; k < min(STG, any - kb); ++k) {
-            if (!(there >> (k / 16) & 1)) continue;
-            const uint16_t* x = a.V + (place(a, table, head, kb + (k & ~15), any).row + (k & 15)) * HD;
+        // A key that some row of the tile sees and another does not must not reach
+        // the second by 0 * inf: values that are not finite leave the product,
+        // and go to the rows that see them by themselves.
+        const bool mixed = CAUSAL && kb + STG > all;
+        if (mixed) {
+            char* mine = kt + B + 16 * wave * Tile::ROW + 16 * lane;
+            uint32_t any_odd = 0;
 #pragma unroll
-            for (int u = 0; u < HD / 32; ++u)
+            for (int j = 0; j < Tile::NL; ++j) {
+                u32x4 x = *reinterpret_cast<const u32x4*>(mine + 1024 * j);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const uint32_t y = x[32 * u + acc_row(v, hh)];
-                    if (not_finite(y) && kb + k < w.lim) w.o[u][v] += bf16_to_f32(y);
+                for (int e = 0; e < 4; ++e) {
+                    any_odd |= not_finite2(x[e]);
+                    x[e] = finite2(x[e]);
                 }
+                *reinterpret_cast<u32x4*>(mine + 1024 * j) = x;
+            }
+            if (any_odd) odd[i & 1] = i;
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
+        if (kb < w_any) wide_block<HD>(w, kt, kb, there, kb + STG > w_all || there != 15u, a.c, hh);
+        if (mixed && odd[i & 1] == i) {
+#pragma unroll 1
+            for (int k = 0; k < min(STG, any - kb); ++k) {
+                if (!(there >> (k / 16) & 1)) continue;
+                const uint16_t* x = a.V + (place(a, table, head, kb + (k & ~15), any).row + (k & 15)) * HD;
+#pragma unroll
+                for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const uint32_t y = x[32 * u + acc_row(v, hh)];
+                        if (not_finite(y) && kb + k < w.lim) w.o[u][v] += bf16_to_f32(y);
+                    }
+            }
+        }
+        there = next;
     };
+    if (threadIdx.x < 2) odd[threadIdx.x] = -1;
     if (n > 0) there = load(0, lds);
     turn();
-    int i = 0;
-    while (i < n) {
+    // The queries have arrived, too; said in a way that the compiler sees, or it
+    // waits for "them" (and so for the next stage) in every turn of the loop.
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(w.q[i]));
 #pragma unroll 1
-        for (; i < n && k0 + STG * (i + 1) <= w_all && there == 15u; ++i) {
-            whole(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
-            there = next;
-            turn();
-        }
-        if (i < n) {
-            part(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
-            there = next;
-            turn();
-            ++i;
-        }
+    for (int i = 0; i < n; ++i) {
+        step(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
+        turn();
     }
     // lane (hh, row): elements 32 u + 8 j + 4 hh .. + 3 in o[u][4 j ..]
     const float l = w.l + __shfl_xor(w.l, 32);
@@ -704,18 +747,27 @@ __device__ __forceinline__ int parts_of(const Args& a, int end) {
     return a.splits_s > 0 ? min((end + a.chunk_s - 1) / a.chunk_s, a.splits_s) : 0;
 }
 
-// Rows of a tile whose kind is n: 16 n, keys in registers, or a wide one.
-constexpr int WIDE = 8;
+// Kinds of tiles: 16 or 32 rows whose keys a workgroup's waves share (ONE, TWO); 128
+// rows against keys in LDS (WIDE).  On the requests' own keys, where each has one
+// token, all rows of a tile see the same: ONE becomes FLAT, or SOLO with a tile to
+// a wave.
+enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, WIDE = 8 };
+constexpr int kind_rows(int k) { return k == SOLO || k == FLAT ? 16 : 16 * k; }
 template <int HD, int N>
-constexpr int kLdsBytes = N == WIDE ? kWideBytes<HD> : 8 * kStateFloats<HD, N>;
+constexpr int kLdsBytes = N == WIDE ? kWideBytes<HD> : (N == SOLO ? 16 : 8 * kStateFloats<HD, kind_rows(N) / 16>);
 
 template <int HD, int N, bool CAUSAL>
 __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
                                          int n_rows, int first, int end, int k0, int chunk, int slot) {
     if constexpr (N == WIDE)
         wide_item<HD, CAUSAL>(a, lds, table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+    else if constexpr (N == SOLO)
+        item<HD, 1, 1, false>(a, nullptr, table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0, chunk, slot);
+    else if constexpr (N == FLAT)
+        item<HD, 1, NW, false>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0,
+                               chunk, slot);
     else
-        item<HD, N, CAUSAL>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+        item<HD, N, NW, CAUSAL>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
 }
 
 // NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
@@ -723,7 +775,7 @@ template <int HD, int NP, int NS>
 __global__ __launch_bounds__(NTHR, (NP == WIDE ? 2 : 1)) void prefix_attn_kernel(const Args a) {
     constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
-    for (int64_t at = blockIdx.x; at < a.items; at += gridDim.x) {
+    for (int64_t at = blockIdx.x; at < a.blocks; at += gridDim.x) {
         if (at != blockIdx.x) __syncthreads();          // the item before has left the LDS
         if (at < a.items_p) {
             int b = (int)at;
@@ -732,19 +784,23 @@ __global__ __launch_bounds__(NTHR, (NP == WIDE ? 2 : 1)) void prefix_attn_kernel
             const int head = b % a.hk, split = b / a.hk;
             // rows of the batch up to the last that holds a token
             const int64_t hi = a.start ? min(max((int64_t)entry(a.start, a.n_req), (int64_t)0), a.T) : min((int64_t)a.n_req, a.T);
-            const int tile0 = tile * 16 * NP, n_rows = (int)hi * a.g;
+            const int tile0 = tile * kind_rows(NP), n_rows = (int)hi * a.g;
             if (tile0 < n_rows)
                 any_item<HD, NP, false>(a, lds, a.prefix_table, head, 0, tile0, n_rows, 0, a.prefix, split * a.chunk_p,
                                         a.chunk_p, split);
         } else {
             int64_t b = at - a.items_p;
+            if constexpr (NS == SOLO) {
+                b = b * NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+                if (b >= a.items_s) continue;
+            }
             const int tile = (int)(b % a.tiles_s);
             b /= a.tiles_s;
             const int head = (int)(b % a.hk);
             b /= a.hk;
             const int split = (int)(b % a.splits_s), r = (int)(b / a.splits_s);
             const Span s = span_of(a, r);
-            const int tile0 = tile * 16 * NS, n_rows = s.n * a.g;
+            const int tile0 = tile * kind_rows(NS), n_rows = s.n * a.g;
             if (tile0 < n_rows && (a.direct || split < parts_of(a, s.end)))
                 any_item<HD, NS, true>(a, lds, a.table + r * a.max_pages, head, s.row, tile0, n_rows, s.first, s.end,
                                        split * a.chunk_s, a.chunk_s, a.splits_p + split);
@@ -752,32 +808,61 @@ __global__ __launch_bounds__(NTHR, (NP == WIDE ? 2 : 1)) void prefix_attn_kernel
     }
 }
 
-// The parts of each row joined, in their order: a thread for four elements.
+// The parts of each row joined, in their order: a wave to a row.  Lane p holds the
+// statistics of parts p and p + 64 (there are at most 128) and forms their
+// weights; then LP lanes take four elements each of every 64 / LP-th part.
 template <int HD>
 __global__ __launch_bounds__(NTHR) void prefix_join_kernel(const Args a) {
-    constexpr int TPR = HD / 4;
+    constexpr int LP = HD / 4, PP = 64 / LP;           // lanes of a part, parts at once
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int sub = lane / LP, e = 4 * (lane % LP);
     for (int r = blockIdx.y; r < a.n_req; r += gridDim.y) {
         const Span s = span_of(a, r);
         const int parts = a.splits_p + parts_of(a, s.end);
-        for (int64_t j = (int64_t)blockIdx.x * (NTHR / TPR) + threadIdx.x / TPR; j < (int64_t)s.n * a.hq;
-             j += (int64_t)gridDim.x * (NTHR / TPR)) {
+        for (int64_t j = (int64_t)blockIdx.x * NW + wave; j < (int64_t)s.n * a.hq; j += (int64_t)gridDim.x * NW) {
             const int64_t id = (int64_t)s.row * a.hq + j;
-            const int e = 4 * (threadIdx.x % TPR);
-            float M = kNone;
-            for (int p = 0; p < parts; ++p) M = fmaxf(M, a.ml[2 * (p * a.rows + id)]);
-            float l = 0.0f;
+            float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (lane + 64 * i < parts) {
+                    const float2 x = *reinterpret_cast<const float2*>(a.ml + 2 * ((lane + 64 * i) * a.rows + id));
+                    m[i] = x.x;
+                    l[i] = x.y;
+                }
+            float M = fmaxf(m[0], m[1]);
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+            const float f[2] = {exp2_hw(m[0] - M), exp2_hw(m[1] - M)};
+            float L = f[0] * l[0] + f[1] * l[1];
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) L += __shfl_xor(L, d);
             f32x4 o = {0, 0, 0, 0};
-            for (int p = 0; p < parts; ++p) {
-                const float2 x = *reinterpret_cast<const float2*>(a.ml + 2 * (p * a.rows + id));
-                const float f = exp2_hw(x.x - M);
-                l += f * x.y;
-                o += f * *reinterpret_cast<const f32x4*>(a.part + (p * a.rows + id) * HD + e);
+            const float* from = a.part + id * HD + e;
+            for (int p0 = 0; p0 < parts; p0 += 4 * PP) {
+                f32x4 x[4];
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int p = p0 + i * PP + sub;
+                    const float lo = __shfl(f[0], p & 63), hi = __shfl(f[1], p & 63);
+                    y[i] = p < 64 ? lo : hi;
+                    x[i] = f32x4{0, 0, 0, 0};
+                    if (p < parts) x[i] = *reinterpret_cast<const f32x4*>(from + p * a.rows * HD);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (p0 + i * PP + sub < parts) o += y[i] * x[i];
             }
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+            for (int d = 32; d >= LP; d >>= 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d);
+            const float inv = L == 0.0f ? 0.0f : 1.0f / L;
             const int64_t t = id / a.hq, h = id - t * a.hq;
-            *reinterpret_cast<u32x2*>(a.out + t * a.ldo + h * HD + e) =
-                u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
-            if (a.lse && e == 0) a.lse[h * a.T + t] = l == 0.0f ? -INFINITY : (M + log2f(l)) * kLn2;
+            if (sub == 0)
+                *reinterpret_cast<u32x2*>(a.out + t * a.ldo + h * HD + e) =
+                    u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+            if (a.lse && lane == 0) a.lse[h * a.T + t] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
         }
     }
 }
@@ -797,7 +882,8 @@ Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAtt
     a.tiles_p = p.tiles_p; a.splits_p = p.splits_p; a.chunk_p = (int)p.chunk_p;
     a.tiles_s = p.tiles_s; a.splits_s = p.splits_s; a.chunk_s = (int)p.chunk_s;
     a.items_p = (int64_t)p.splits_p * p.tiles_p * sh.hk;
-    a.items = a.items_p + sh.n_req * p.splits_s * p.tiles_s * sh.hk;
+    a.items_s = sh.n_req * p.splits_s * p.tiles_s * sh.hk;
+    a.blocks = a.items_p + (p.nt_s == SOLO ? (a.items_s + NW - 1) / NW : a.items_s);
     a.direct = p.direct;
     a.c = (float)(sh.scale * (double)kLog2e);
     return a;
@@ -805,16 +891,28 @@ Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAtt
 
 template <int HD>
 hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t s) {
-    if (p.nt_p == 1) prefix_attn_kernel<HD, 1, 1><<<grid, NTHR, 0, s>>>(a);
-    else if (p.nt_p == 2 && p.nt_s == 1) prefix_attn_kernel<HD, 2, 1><<<grid, NTHR, 0, s>>>(a);
-    else if (p.nt_p == 2) prefix_attn_kernel<HD, 2, 2><<<grid, NTHR, 0, s>>>(a);
-    else if (p.nt_s == 1) prefix_attn_kernel<HD, WIDE, 1><<<grid, NTHR, 0, s>>>(a);
-    else if (p.nt_s == 2) prefix_attn_kernel<HD, WIDE, 2><<<grid, NTHR, 0, s>>>(a);
-    else prefix_attn_kernel<HD, WIDE, WIDE><<<grid, NTHR, 0, s>>>(a);
+#define COLA_GO(P, S) \
+    if (p.nt_p == P && p.nt_s == S) prefix_attn_kernel<HD, P, S><<<grid, NTHR, 0, s>>>(a)
+    COLA_GO(ONE, ONE);
+    else COLA_GO(ONE, FLAT);
+    else COLA_GO(ONE, SOLO);
+    else COLA_GO(TWO, ONE);
+    else COLA_GO(TWO, FLAT);
+    else COLA_GO(TWO, SOLO);
+    else COLA_GO(TWO, TWO);
+    else COLA_GO(WIDE, ONE);
+    else COLA_GO(WIDE, FLAT);
+    else COLA_GO(WIDE, SOLO);
+    else COLA_GO(WIDE, TWO);
+    else COLA_GO(WIDE, WIDE);
+    else return hipErrorInvalidValue;
+#undef COLA_GO
     return hipGetLastError();
 }
 
-int columns(int64_t rows) { return rows <= 16 ? 1 : (rows <= 32 ? 2 : WIDE); }
+const int64_t kSoloItems = getenv("PA_SOLO") ? atoi(getenv("PA_SOLO")) : 4096;
+const int64_t kTarget = getenv("PA_TARGET") ? atoi(getenv("PA_TARGET")) : 1024;
+int kind_of(int64_t rows) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : WIDE); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
@@ -824,14 +922,15 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     const int64_t g = sh.hq / sh.hk;
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
     p.rows = sh.T * sh.hq;
-    p.nt_s = columns(new_rows * g);
-    p.nt_p = columns(sh.T * g);                              // never below nt_s
-    p.tiles_p = (int)ceil_div(sh.T * g, 16 * p.nt_p);
-    p.tiles_s = (int)ceil_div(new_rows * g, 16 * p.nt_s);
+    p.nt_s = kind_of(new_rows * g);
+    p.nt_p = kind_of(sh.T * g);                              // never below nt_s
+    p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.nt_p));
+    p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.nt_s));
+    if (p.nt_s == ONE && sh.max_new == 1) p.nt_s = sh.n_req * sh.hk >= kSoloItems ? SOLO : FLAT;
     // Parts of the keys: about a thousand work items in all, none below 256 keys
     const int64_t base_p = (int64_t)p.tiles_p * sh.hk, base_s = sh.n_req * p.tiles_s * sh.hk;
     const int64_t blocks = base_p * ceil_div(sh.prefix, KB) + base_s * ceil_div(sh.max_kv, KB);
-    int64_t chunk = ceil_div(blocks, 1024);
+    int64_t chunk = ceil_div(blocks, kTarget);
     if (chunk < 8) chunk = 8;
     // as many parts as that gives, of equal length
     auto parts = [&](int64_t keys, int* n, int64_t* len) {
@@ -856,8 +955,8 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
 hipError_t launch_prefix_attn(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAttnPtrs& t,
                               hipStream_t s) {
     const Args a = args_of(sh, p, t);
-    if (a.items == 0) return hipSuccess;
-    const int64_t grid = a.items < (1 << 22) ? a.items : (1 << 22);
+    if (a.blocks == 0) return hipSuccess;
+    const int64_t grid = a.blocks < (1 << 22) ? a.blocks : (1 << 22);
     return sh.hd == 64 ? go<64>(p, a, (unsigned)grid, s) : go<128>(p, a, (unsigned)grid, s);
 }
 
@@ -866,7 +965,7 @@ hipError_t launch_prefix_join(const PrefixAttnShape& sh, const PrefixAttnPlan& p
     if (p.direct) return hipSuccess;
     const Args a = args_of(sh, p, t);
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
-    int64_t gx = ceil_div(new_rows * sh.hq, NTHR / (sh.hd / 4));
+    int64_t gx = ceil_div(new_rows * sh.hq, NW);
     if (gx > 4096) gx = 4096;
     const dim3 grid((unsigned)gx, (unsigned)sh.n_req);
     if (sh.hd == 64) prefix_join_kernel<64><<<grid, NTHR, 0, s>>>(a);
