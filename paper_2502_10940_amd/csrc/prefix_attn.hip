@@ -31,7 +31,8 @@
 // No LDS, no transposing pass, no barrier in the loop: key and value bytes go
 // from memory to the matrix unit.
 #include <math.h>
-#include <stdlib.h>
+
+#include <type_traits>
 
 #include "serve.hpp"
 #include "device_math.hpp"
@@ -68,7 +69,8 @@ struct Args {
     int64_t ldq, ldo, rows, max_pages, n_pages, T;
     int n_req, hq, hk, g, lg_page;
     int prefix, max_kv, max_new;
-    int64_t blocks, items_p, items_s;     // workgroups' turns, work items of either part
+    int64_t blocks, items_p, base;        // workgroups' turns, those on the prefix, the launch's first
+    int64_t units_p, units_s;             // (head, part) pairs of the prefix; (request, head, part) of the own keys
     int tiles_p, splits_p, chunk_p;
     int tiles_s, splits_s, chunk_s;
     int direct;                           // one part in all, of the requests' own keys: the item writes the result
@@ -180,21 +182,20 @@ __device__ __forceinline__ bf16x8 v_frag(const R (&v)[8], int t) {
     return __builtin_bit_cast(bf16x8, f);
 }
 
-// Where 16 keys from k0 on lie: the place of the first in K and V, in rows of HD,
-// and whether their page is in the cache.  Tiles that begin at or past `end` are
-// looked up at the last one before it, missing pages at page 0: what is read
-// there is memory of the cache and is masked.
-struct Place {
-    int64_t row;
-    bool there;
-};
-__device__ __forceinline__ Place place(const Args& a, const int32_t* table, int head, int k0, int end) {
+// The page of the 16 keys from k0 on; tiles that begin at or past `end` are looked
+// up at the last one before it (their table entry may not exist).
+__device__ __forceinline__ int page_of(const Args& a, const int32_t* table, int k0, int end) {
     const int k = min(k0, (end - 1) & ~15);
-    const int64_t page = uniform(entry(table, k >> a.lg_page));
-    Place p;
-    p.there = page >= 0 && page < a.n_pages;
-    p.row = (((p.there ? page : 0) * a.hk + head) << a.lg_page) + (k & ((1 << a.lg_page) - 1));
-    return p;
+    return uniform(entry(table, k >> a.lg_page));
+}
+__device__ __forceinline__ bool in_cache(const Args& a, int page) { return (uint32_t)page < (uint32_t)a.n_pages; }
+// Row of K and V (in units of HD) at which key k of a page lies.
+__device__ __forceinline__ int64_t row_of(const Args& a, int page, int head, int k) {
+    return (((int64_t)page * a.hk + head) << a.lg_page) + (k & ((1 << a.lg_page) - 1));
+}
+// Keys from k0 on, of 16, that lie in the cache and before `end`.
+__device__ __forceinline__ int rows_in(bool there, int k0, int end) {
+    return there && k0 < end ? (end - k0 < 16 ? end - k0 : 16) : 0;
 }
 
 // Descriptor of `rows` rows of HD from row `at` on; reads past them give zeros.
@@ -220,11 +221,12 @@ struct Keys {
         __amdgpu_buffer_rsrc_t rv[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const Place at = place(a, table, head, kb + 16 * i, end);
-            there[i] = at.there;
-            const int rows = at.there ? min(max(end - (kb + 16 * i), 0), 16) : 0;
-            const __amdgpu_buffer_rsrc_t rk = rows_of<HD>(a.K, at.row, rows);
-            rv[i] = rows_of<HD>(a.V, at.row, rows);
+            const int page = page_of(a, table, kb + 16 * i, end);
+            there[i] = in_cache(a, page);
+            const int rows = rows_in(there[i], kb + 16 * i, end);
+            const int64_t at = row_of(a, page, head, kb + 16 * i);
+            const __amdgpu_buffer_rsrc_t rk = rows_of<HD>(a.K, at, rows);
+            rv[i] = rows_of<HD>(a.V, at, rows);
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) k[i][kk] = __builtin_amdgcn_raw_buffer_load_b128(rk, ko + 64 * kk, 0, 0);
         }
@@ -324,17 +326,16 @@ __device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, Keys<HD>& 
         if (odd) {
 #pragma unroll 1
             for (int k = 0; k < min(KB, end - kb); ++k) {
-                const Place at = place(a, table, head, kb + (k & ~15), end);
-                if (!at.there) continue;
+                const int page = page_of(a, table, kb + k, end);
+                if (!in_cache(a, page)) continue;
                 // this lane's elements of its rows: 4 D from 4 D g on
-                const uint16_t* y = a.V + (at.row + (k & 15)) * HD + 4 * D * g;
+                const uint16_t* y = a.V + row_of(a, page, head, kb + k) * HD + 4 * D * g;
 #pragma unroll
                 for (int e = 0; e < 4 * D; ++e) {
                     const uint32_t z = y[e];
-                    if (!not_finite(z)) continue;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        if (kb + k < w.lim[n]) w.o[e % D][n][e / D] += bf16_to_f32(z);
+                        w.o[e % D][n][e / D] += not_finite(z) && kb + k < w.lim[n] ? bf16_to_f32(z) : 0.0f;
                 }
             }
         }
@@ -384,8 +385,9 @@ __device__ __forceinline__ void take(Wave<HD, NT>& w, const float* buf, int lane
 // further, head rho % g of the group), keys k0 .. of a table that ends at `end`.
 // Row rho sees the keys up to first + rho / g, or all of them.  KW = NW: the
 // workgroup's waves share the keys and join through LDS; KW = 1: each wave has an
-// item of its own.
-template <int HD, int NT, int KW, bool CAUSAL>
+// item of its own.  ALONG: the prefix's keys come before them.  AHEAD: the next
+// block's keys are on their way while one is used.
+template <int HD, int NT, int KW, bool CAUSAL, bool ALONG, bool AHEAD>
 __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* table, int head, int row0, int tile0,
                                      int n_rows, int first, int end, int k0, int chunk, int slot) {
     constexpr int KK = HD / 32, D = HD / 16;
@@ -415,12 +417,39 @@ __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* t
             w.q[n][kk] = __builtin_bit_cast(bf16x8, x);
         }
     }
+    // The blocks kb, kb + KB KW, .. of one table.
+    auto walk = [&](auto causal, const int32_t* tab, int kb, int end_k, int all_k) __attribute__((always_inline)) {
+        constexpr bool C = decltype(causal)::value;
+        Keys<HD> x, y;
+        if (AHEAD && kb < end_k) x.load(a, tab, head, kb, end_k, lane);
+        auto step = [&](Keys<HD>& now, Keys<HD>& next) __attribute__((always_inline)) {
+            const int nb = kb + KB * KW;
+            if (!AHEAD) now.load(a, tab, head, kb, end_k, lane);
+            else if (nb < end_k) next.load(a, tab, head, nb, end_k, lane);
+            block<HD, NT, C>(w, a, now, tab, head, kb, end_k, kb + KB > all_k || !now.there[0] || !now.there[1], lane);
+            kb = nb;
+        };
 #pragma unroll 1
-    for (int kb = k0 + KB * wave; kb < any; kb += KB * KW) {
-        Keys<HD> x;
-        x.load(a, table, head, kb, any, lane);
-        block<HD, NT, CAUSAL>(w, a, x, table, head, kb, any, kb + KB > all || !x.there[0] || !x.there[1], lane);
+        while (kb < end_k) {
+            step(x, y);
+            if (AHEAD && kb < end_k) step(y, x);
+        }
+    };
+    int turn = wave;                                    // whose block is the first
+    if constexpr (ALONG) {
+        const int end_p = a.n_pages > 0 ? a.prefix : 0;
+        int lim[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            lim[n] = w.lim[n];
+            w.lim[n] = live[n] ? end_p : 0;
+        }
+        walk(std::false_type{}, a.prefix_table, KB * wave, end_p, end_p);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) w.lim[n] = lim[n];
+        turn = (wave + KW - (end_p + KB - 1) / KB % KW) % KW;
     }
+    walk(std::integral_constant<bool, CAUSAL>{}, table, k0 + KB * turn, any, all);
     if constexpr (KW > 1) {
         // waves 2, 3 into 0, 1, then 1 into 0
         float* mine = lds + (wave & 1) * kStateFloats<HD, NT>;
@@ -479,25 +508,27 @@ __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* t
 // order, which the transposing LDS reads give.
 
 constexpr int WROWS = 32 * NW;            // rows of a wide tile
-constexpr int STG = 16 * NW;              // keys of a stage
+constexpr int STG = 64;                   // keys of a stage (32: 5 to 10 % slower)
 
 // A stage's keys or values in LDS: [STG][HD] bf16, 16-byte chunk c of row r at chunk
 // c ^ swz(r).  The swizzle gives 16 rows of one chunk, and four neighbouring rows of
 // 64 bytes, all 64 banks once: the reads of the two products.
 template <int HD>
 struct KeyTile {
+    static constexpr int NB = STG / 32, TILES = STG / 16;
     static constexpr int ROW = 2 * HD, BYTES = STG * ROW;
     static constexpr int CPR = HD / 8;                 // chunks per row
     static constexpr int RPI = 64 / CPR;               // rows of a 1 KB load
-    static constexpr int NL = 16 / RPI;                // loads of 16 rows
+    static constexpr int RW = STG / NW;                // rows that a wave loads, in NL loads
+    static constexpr int NL = RW / RPI;
     __device__ static __forceinline__ int swz(int row) {
         const int x = HD == 128 ? row & 15 : (row >> 1) & 7;
         return HD == 128 ? ((x & 3) << 2) | (x >> 2) : ((x & 1) << 2) | (x >> 1);
     }
     __device__ static __forceinline__ int off(int row, int chunk) { return row * ROW + ((chunk ^ swz(row)) << 4); }
-    // Load j of a tile of 16 rows: where this lane reads, from the tile's first byte.
-    __device__ static __forceinline__ uint32_t from(int j, int lane) {
-        const int row = RPI * j + lane / CPR;
+    // Load j of a wave: where this lane reads, from the first byte of its tile of 16.
+    __device__ static __forceinline__ uint32_t from(int j, int wave, int lane) {
+        const int row = RW * wave % 16 + RPI * j + lane / CPR;
         return row * ROW + (((lane % CPR) ^ swz(row)) << 4);
     }
     // K operand, step i: elements 16 i + 8 (lane / 32) .. of row lane % 32.
@@ -536,14 +567,15 @@ struct WideWave {
 template <int HD>
 __device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, int kb, uint32_t there, bool part, float c, int hh) {
     typedef KeyTile<HD> Tile;
-    f32x16 s[2] = {f32x16{}, f32x16{}};
+    constexpr int NB = Tile::NB;
+    f32x16 s[NB] = {};
 #pragma unroll
     for (int i = 0; i < HD / 16; ++i)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) s[b] = mfma32(lds_frag(kt + w.key[i] + 32 * b * Tile::ROW), w.q[i], s[b]);
+        for (int b = 0; b < NB; ++b) s[b] = mfma32(lds_frag(kt + w.key[i] + 32 * b * Tile::ROW), w.q[i], s[b]);
     if (part) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const int lim = there >> (2 * b + x) & 1 ? w.lim - kb - 4 * hh : 0;
@@ -554,7 +586,7 @@ __device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, int 
     }
     float mb = -INFINITY;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int v = 0; v < 16; v += 2) mb = fmaxf(fmaxf(mb, s[b][v]), s[b][v + 1]);
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
@@ -569,7 +601,7 @@ __device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, int 
     }
     const char* vt = kt + Tile::BYTES;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             u32x4 f;
@@ -622,7 +654,7 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
     }
     uint32_t from[Tile::NL];
 #pragma unroll
-    for (int j = 0; j < Tile::NL; ++j) from[j] = Tile::from(j, lane);
+    for (int j = 0; j < Tile::NL; ++j) from[j] = Tile::from(j, wave, lane);
     // what the tile's last row sees, and what this wave's first and last row see
     const int any = uniform(a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0), all = uniform(min(seen(tile0), any));
     const int w0 = tile0 + 32 * wave;
@@ -630,21 +662,34 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
               w_all = uniform(w0 < n_rows ? min(seen(w0), any) : 0);
     const int n = any > k0 ? (any - k0 + STG - 1) / STG : 0;
 
+    // The pages of stage i's tiles of 16, looked up a turn before they are used.
+    int page[Tile::TILES] = {};
+    auto look = [&](int i) __attribute__((always_inline)) {
+        const int kb = k0 + STG * i;
+        if (1 << a.lg_page >= STG) {                   // the stage lies in one page
+            const int p = page_of(a, table, kb, any);
+#pragma unroll
+            for (int x = 0; x < Tile::TILES; ++x) page[x] = p;
+        } else {
+#pragma unroll
+            for (int x = 0; x < Tile::TILES; ++x) page[x] = page_of(a, table, kb + 16 * x, any);
+        }
+    };
+    constexpr uint32_t ALL = (1u << Tile::TILES) - 1;
     // Stage i into the buffer at `to`: keys from `any` on and missing pages arrive as
     // zeros (they lie past the descriptor's range).  Returns the pages that are there.
     auto load = [&](int i, char* to) __attribute__((always_inline)) -> uint32_t {
-        const int kb = k0 + STG * i;
         uint32_t there = 0;
-        Place mine{};
+        int mine = page[0];
 #pragma unroll
-        for (int x = 0; x < NW; ++x) {
-            const Place p = place(a, table, head, kb + 16 * x, any);
-            there |= (uint32_t)p.there << x;
-            if (x == wave) mine = p;
+        for (int x = 0; x < Tile::TILES; ++x) {
+            there |= (uint32_t)in_cache(a, page[x]) << x;
+            if (x == Tile::RW * wave / 16) mine = page[x];
         }
-        const int rows = mine.there ? min(max(any - (kb + 16 * wave), 0), 16) : 0;
-        to += 16 * wave * Tile::ROW;
-        const auto rk = rows_of<HD>(a.K, mine.row, rows), rv = rows_of<HD>(a.V, mine.row, rows);
+        const int kb = k0 + STG * i + (Tile::RW * wave & ~15), rows = rows_in(in_cache(a, mine), kb, any);
+        const int64_t at = row_of(a, mine, head, kb);
+        to += Tile::RW * wave * Tile::ROW;
+        const auto rk = rows_of<HD>(a.K, at, rows), rv = rows_of<HD>(a.V, at, rows);
 #pragma unroll
         for (int j = 0; j < Tile::NL; ++j) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lptr_t)(to + 1024 * j), 16, from[j], 0, 0, 0);
@@ -670,7 +715,7 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
         // and go to the rows that see them by themselves.
         const bool mixed = CAUSAL && kb + STG > all;
         if (mixed) {
-            char* mine = kt + B + 16 * wave * Tile::ROW + 16 * lane;
+            char* mine = kt + B + Tile::RW * wave * Tile::ROW + 16 * lane;
             uint32_t any_odd = 0;
 #pragma unroll
             for (int j = 0; j < Tile::NL; ++j) {
@@ -685,25 +730,30 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
             if (any_odd) odd[i & 1] = i;
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
-        if (kb < w_any) wide_block<HD>(w, kt, kb, there, kb + STG > w_all || there != 15u, a.c, hh);
+        if (kb < w_any) wide_block<HD>(w, kt, kb, there, kb + STG > w_all || there != ALL, a.c, hh);
         if (mixed && odd[i & 1] == i) {
 #pragma unroll 1
             for (int k = 0; k < min(STG, any - kb); ++k) {
                 if (!(there >> (k / 16) & 1)) continue;
-                const uint16_t* x = a.V + (place(a, table, head, kb + (k & ~15), any).row + (k & 15)) * HD;
+                const uint16_t* x = a.V + row_of(a, page_of(a, table, kb + k, any), head, kb + k) * HD;
 #pragma unroll
                 for (int u = 0; u < HD / 32; ++u)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const uint32_t y = x[32 * u + acc_row(v, hh)];
-                        if (not_finite(y) && kb + k < w.lim) w.o[u][v] += bf16_to_f32(y);
+                        w.o[u][v] += not_finite(y) && kb + k < w.lim ? bf16_to_f32(y) : 0.0f;
                     }
             }
         }
         there = next;
+        if (i + 2 < n) look(i + 2);
     };
     if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-    if (n > 0) there = load(0, lds);
+    if (n > 0) {
+        look(0);
+        there = load(0, lds);
+        if (n > 1) look(1);
+    }
     turn();
     // The queries have arrived, too; said in a way that the compiler sees, or it
     // waits for "them" (and so for the next stage) in every turn of the loop.
@@ -714,31 +764,37 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
         step(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
         turn();
     }
-    // lane (hh, row): elements 32 u + 8 j + 4 hh .. + 3 in o[u][4 j ..]
-    const float l = w.l + __shfl_xor(w.l, 32);
-    if (!live) return;
+    // Lane (hh, row) has the elements 32 u + 8 j + 4 hh .. + 3 in o[u][4 j ..].  They go
+    // out by way of LDS, a region for each wave, so that a store covers whole rows:
+    // four elements at chunk c of row r lie at chunk c ^ (r % 16).
+    constexpr int CH = HD / 4, RS = 64 / CH;           // chunks of a row, rows of a store
+    float l = w.l + __shfl_xor(w.l, 32);
+    f32x4* mine = reinterpret_cast<f32x4*>(lds) + 32 * CH * wave;
+    const int rr = lane & 31;
+    const float scale = a.direct ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+#pragma unroll
+    for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            mine[CH * rr + ((8 * u + 2 * j + hh) ^ (rr & 15))] =
+                f32x4{w.o[u][4 * j], w.o[u][4 * j + 1], w.o[u][4 * j + 2], w.o[u][4 * j + 3]} * scale;
     const int64_t id = row * a.hq + h;
-    if (a.direct) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        uint16_t* y = a.out + row * a.ldo + h * HD + 4 * hh;
+    if (live && hh == 0) {
+        if (!a.direct) *reinterpret_cast<float2*>(a.ml + 2 * (slot * a.rows + id)) = make_float2(w.m, l);
+        else if (a.lse) a.lse[h * a.T + row] = l == 0.0f ? -INFINITY : (w.m + log2f(l)) * kLn2;
+    }
+    const int c = lane % CH;
 #pragma unroll
-        for (int u = 0; u < HD / 32; ++u)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const u32x2 x = {pack_bf16x2(w.o[u][4 * j] * inv, w.o[u][4 * j + 1] * inv),
-                                 pack_bf16x2(w.o[u][4 * j + 2] * inv, w.o[u][4 * j + 3] * inv)};
-                *reinterpret_cast<u32x2*>(y + 32 * u + 8 * j) = x;
-            }
-        if (a.lse && hh == 0) a.lse[h * a.T + row] = l == 0.0f ? -INFINITY : (w.m + log2f(l)) * kLn2;
-    } else {
-        float* y = a.part + (slot * a.rows + id) * HD + 4 * hh;
-#pragma unroll
-        for (int u = 0; u < HD / 32; ++u)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<f32x4*>(y + 32 * u + 8 * j) =
-                    f32x4{w.o[u][4 * j], w.o[u][4 * j + 1], w.o[u][4 * j + 2], w.o[u][4 * j + 3]};
-        if (hh == 0) *reinterpret_cast<float2*>(a.ml + 2 * (slot * a.rows + id)) = make_float2(w.m, l);
+    for (int i = 0; i < 32; i += RS) {
+        const int r = i + lane / CH;
+        if (w0 + r >= n_rows) continue;
+        const f32x4 x = mine[CH * r + (c ^ (r & 15))];
+        const int t = (w0 + r) / a.g, hd = head * a.g + (w0 + r - t * a.g);
+        if (a.direct)
+            *reinterpret_cast<u32x2*>(a.out + (row0 + t) * a.ldo + hd * HD + 4 * c) =
+                u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        else
+            *reinterpret_cast<f32x4*>(a.part + (slot * a.rows + (int64_t)(row0 + t) * a.hq + hd) * HD + 4 * c) = x;
     }
 }
 
@@ -751,64 +807,133 @@ __device__ __forceinline__ int parts_of(const Args& a, int end) {
 // rows against keys in LDS (WIDE).  On the requests' own keys, where each has one
 // token, all rows of a tile see the same: ONE becomes FLAT, or SOLO with a tile to
 // a wave.
-enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, WIDE = 8 };
+// Behind a short prefix there are no tiles for it: each request's own items take its
+// keys ALONG, and nothing is left to join.
+enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, ALONG = 5, WIDE = 8 };
 constexpr int kind_rows(int k) { return k == SOLO || k == FLAT ? 16 : 16 * k; }
 template <int HD, int N>
-constexpr int kLdsBytes = N == WIDE ? kWideBytes<HD> : (N == SOLO ? 16 : 8 * kStateFloats<HD, kind_rows(N) / 16>);
+constexpr int kLdsBytes = N == WIDE ? kWideBytes<HD> : (N == SOLO || N == ALONG ? 16 : 8 * kStateFloats<HD, kind_rows(N) / 16>);
 
-template <int HD, int N, bool CAUSAL>
+// AHEAD costs registers: heads of 128 with 32 rows have none to spare, and beside
+// wide tiles, which leave two workgroups a CU, the plain loop is faster (64 requests
+// behind 32768 tokens 101 us against 114, 200 of 32 heads 123 against 140; one request
+// behind 100 tokens 4.9 against 4.7, behind 1024 8.7 against 7.8).
+template <int HD, int N, int NP>
+constexpr bool kAhead = NP != WIDE && !(HD == 128 && N == TWO);
+
+template <int HD, int N, int NP, bool CAUSAL>
 __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
                                          int n_rows, int first, int end, int k0, int chunk, int slot) {
+    constexpr bool ALONG_P = NP == ALONG;
     if constexpr (N == WIDE)
         wide_item<HD, CAUSAL>(a, lds, table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
     else if constexpr (N == SOLO)
-        item<HD, 1, 1, false>(a, nullptr, table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0, chunk, slot);
+        item<HD, 1, 1, false, false, kAhead<HD, N, NP>>(a, nullptr, table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0, chunk, slot);
     else if constexpr (N == FLAT)
-        item<HD, 1, NW, false>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0,
+        item<HD, 1, NW, false, ALONG_P, kAhead<HD, N, NP>>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0,
                                chunk, slot);
     else
-        item<HD, N, NW, CAUSAL>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+        item<HD, N, NW, CAUSAL, ALONG_P, kAhead<HD, N, NP>>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
 }
+
+// Tile `tile` of unit `unit` (a head and a part of the keys) from turn b of a range
+// whose tiles of a unit read the same keys.  Workgroups go to the XCDs in turn, each
+// of which has an L2 of its own: a unit's tiles are eight turns apart.  False past
+// the last unit.
+struct Turn {
+    int64_t unit;
+    int tile;
+};
+__device__ __forceinline__ Turn turn_of(int64_t b, int tiles) {
+    const int64_t j = b >> 3;
+    return {j / tiles * 8 + (b & 7), (int)(j % tiles)};
+}
+// Turns that `units` units of `tiles` tiles take.
+__host__ __device__ constexpr int64_t turns(int64_t units, int tiles) { return tiles == 1 ? units : (units + 7) / 8 * 8 * tiles; }
 
 // NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
 template <int HD, int NP, int NS>
 __global__ __launch_bounds__(NTHR, (NP == WIDE ? 2 : 1)) void prefix_attn_kernel(const Args a) {
     constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
-    for (int64_t at = blockIdx.x; at < a.blocks; at += gridDim.x) {
-        if (at != blockIdx.x) __syncthreads();          // the item before has left the LDS
-        if (at < a.items_p) {
-            int b = (int)at;
-            const int tile = b % a.tiles_p;
-            b /= a.tiles_p;
-            const int head = b % a.hk, split = b / a.hk;
-            // rows of the batch up to the last that holds a token
-            const int64_t hi = a.start ? min(max((int64_t)entry(a.start, a.n_req), (int64_t)0), a.T) : min((int64_t)a.n_req, a.T);
-            const int tile0 = tile * kind_rows(NP), n_rows = (int)hi * a.g;
+    const int64_t at = a.base + blockIdx.x;
+    if (NP != ALONG && at < a.items_p) {
+        const Turn t = a.tiles_p == 1 ? Turn{at, 0} : turn_of(at, a.tiles_p);
+        if (t.unit >= a.units_p) return;
+        const int tile = t.tile, head = (int)t.unit % a.hk, split = (int)t.unit / a.hk;
+        // rows of the batch up to the last that holds a token
+        const int64_t hi = a.start ? min(max((int64_t)entry(a.start, a.n_req), (int64_t)0), a.T) : min((int64_t)a.n_req, a.T);
+        const int tile0 = tile * kind_rows(NP), n_rows = (int)hi * a.g;
+        if constexpr (NP != ALONG)
             if (tile0 < n_rows)
-                any_item<HD, NP, false>(a, lds, a.prefix_table, head, 0, tile0, n_rows, 0, a.prefix, split * a.chunk_p,
+                any_item<HD, NP, NP, false>(a, lds, a.prefix_table, head, 0, tile0, n_rows, 0, a.prefix, split * a.chunk_p,
                                         a.chunk_p, split);
-        } else {
-            int64_t b = at - a.items_p;
-            if constexpr (NS == SOLO) {
-                b = b * NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-                if (b >= a.items_s) continue;
+    } else {
+        int64_t b = at - a.items_p;
+        if constexpr (NS == SOLO) b = b * NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const Turn t = a.tiles_s == 1 ? Turn{b, 0} : turn_of(b, a.tiles_s);
+        if (t.unit >= a.units_s) return;
+        const int tile = t.tile, head = (int)(t.unit % a.hk);
+        b = t.unit / a.hk;
+        const int split = (int)(b % a.splits_s), r = (int)(b / a.splits_s);
+        const Span s = span_of(a, r);
+        const int tile0 = tile * kind_rows(NS), n_rows = s.n * a.g;
+        if (tile0 < n_rows && (a.direct || split < parts_of(a, s.end)))
+            any_item<HD, NS, NP, true>(a, lds, a.table + r * a.max_pages, head, s.row, tile0, n_rows, s.first, s.end,
+                                   split * a.chunk_s, a.chunk_s, a.splits_p + split);
+    }
+}
+
+// The parts of each row joined, in their order, where they are few: a thread for
+// four elements of a row, kFew parts in flight.
+constexpr int kFew = 4;
+template <int HD>
+__global__ __launch_bounds__(NTHR) void prefix_join_few_kernel(const Args a) {
+    constexpr int TPR = HD / 4;
+    const int e = 4 * (threadIdx.x % TPR);
+    for (int r = blockIdx.y; r < a.n_req; r += gridDim.y) {
+        const Span s = span_of(a, r);
+        const int parts = a.splits_p + parts_of(a, s.end);
+        for (int64_t j = (int64_t)blockIdx.x * (NTHR / TPR) + threadIdx.x / TPR; j < (int64_t)s.n * a.hq;
+             j += (int64_t)gridDim.x * (NTHR / TPR)) {
+            const int64_t id = (int64_t)s.row * a.hq + j;
+            float M = kNone, l = 0.0f;
+            f32x4 o = {0, 0, 0, 0};
+            for (int p0 = 0; p0 < parts; p0 += kFew) {
+                float2 x[kFew];
+                f32x4 y[kFew];
+                float m = M;
+#pragma unroll
+                for (int i = 0; i < kFew; ++i) {
+                    x[i] = make_float2(kNone, 0.0f);
+                    y[i] = f32x4{0, 0, 0, 0};
+                    if (p0 + i < parts) {
+                        x[i] = *reinterpret_cast<const float2*>(a.ml + 2 * ((p0 + i) * a.rows + id));
+                        y[i] = *reinterpret_cast<const f32x4*>(a.part + ((p0 + i) * a.rows + id) * HD + e);
+                    }
+                    m = fmaxf(m, x[i].x);
+                }
+                const float f = exp2_hw(M - m);
+                l *= f;
+                o *= f;
+                M = m;
+#pragma unroll
+                for (int i = 0; i < kFew; ++i) {
+                    const float g = exp2_hw(x[i].x - m);
+                    l += g * x[i].y;
+                    o += g * y[i];
+                }
             }
-            const int tile = (int)(b % a.tiles_s);
-            b /= a.tiles_s;
-            const int head = (int)(b % a.hk);
-            b /= a.hk;
-            const int split = (int)(b % a.splits_s), r = (int)(b / a.splits_s);
-            const Span s = span_of(a, r);
-            const int tile0 = tile * kind_rows(NS), n_rows = s.n * a.g;
-            if (tile0 < n_rows && (a.direct || split < parts_of(a, s.end)))
-                any_item<HD, NS, true>(a, lds, a.table + r * a.max_pages, head, s.row, tile0, n_rows, s.first, s.end,
-                                       split * a.chunk_s, a.chunk_s, a.splits_p + split);
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const uint32_t t = (uint32_t)id / (uint32_t)a.hq, h = (uint32_t)id - t * (uint32_t)a.hq;
+            *reinterpret_cast<u32x2*>(a.out + (int64_t)t * a.ldo + h * HD + e) =
+                u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+            if (a.lse && e == 0) a.lse[h * a.T + t] = l == 0.0f ? -INFINITY : (M + log2f(l)) * kLn2;
         }
     }
 }
 
-// The parts of each row joined, in their order: a wave to a row.  Lane p holds the
+// The same where they are many: a wave to a row.  Lane p holds the
 // statistics of parts p and p + 64 (there are at most 128) and forms their
 // weights; then LP lanes take four elements each of every 64 / LP-th part.
 template <int HD>
@@ -881,9 +1006,10 @@ Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAtt
     a.prefix = (int)sh.prefix; a.max_kv = (int)sh.max_kv; a.max_new = (int)sh.max_new;
     a.tiles_p = p.tiles_p; a.splits_p = p.splits_p; a.chunk_p = (int)p.chunk_p;
     a.tiles_s = p.tiles_s; a.splits_s = p.splits_s; a.chunk_s = (int)p.chunk_s;
-    a.items_p = (int64_t)p.splits_p * p.tiles_p * sh.hk;
-    a.items_s = sh.n_req * p.splits_s * p.tiles_s * sh.hk;
-    a.blocks = a.items_p + (p.nt_s == SOLO ? (a.items_s + NW - 1) / NW : a.items_s);
+    a.units_p = (int64_t)p.splits_p * sh.hk;
+    a.units_s = sh.n_req * p.splits_s * sh.hk;
+    a.items_p = turns(a.units_p, p.tiles_p);
+    a.blocks = a.items_p + (p.nt_s == SOLO ? (a.units_s + NW - 1) / NW : turns(a.units_s, p.tiles_s));
     a.direct = p.direct;
     a.c = (float)(sh.scale * (double)kLog2e);
     return a;
@@ -893,7 +1019,10 @@ template <int HD>
 hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t s) {
 #define COLA_GO(P, S) \
     if (p.nt_p == P && p.nt_s == S) prefix_attn_kernel<HD, P, S><<<grid, NTHR, 0, s>>>(a)
-    COLA_GO(ONE, ONE);
+    COLA_GO(ALONG, ONE);
+    else COLA_GO(ALONG, TWO);
+    else COLA_GO(ALONG, FLAT);
+    else COLA_GO(ONE, ONE);
     else COLA_GO(ONE, FLAT);
     else COLA_GO(ONE, SOLO);
     else COLA_GO(TWO, ONE);
@@ -910,8 +1039,20 @@ hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t
     return hipGetLastError();
 }
 
-const int64_t kSoloItems = getenv("PA_SOLO") ? atoi(getenv("PA_SOLO")) : 4096;
-const int64_t kTarget = getenv("PA_TARGET") ? atoi(getenv("PA_TARGET")) : 1024;
+// Batches of so many (request, key head) pairs keep the chip busy with a wave to
+// each: 200 requests of 32 heads 97 us against 105 with four waves to a pair; 1024
+// pairs 36 us against 23, 512 pairs of 2000 keys 79 against 67.
+constexpr int64_t kSoloItems = 4096;
+// Parts up to which a thread reads all of a row's four elements (2 to 8 parts: the
+// same time as a wave to a row, or less; 3 parts of 70112 rows 13 us against 83).
+constexpr int64_t kJoinFew = 8;
+// Keys that a request's item takes along at most, and bytes of prefix that all
+// requests read again.  One request of 8 heads of 64 with 200 keys of its own: 5.1
+// us against 8.0 behind 64 keys, 7.4 against 8.1 behind 512, 10.0 against 8.5 behind
+// 1024; 64 requests: 9.4 against 12.1 at 34 MB, 12.0 against 12.4 at 67 MB.
+constexpr int64_t kAlongKeys = 640, kAlongBytes = 40000000;
+constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
+constexpr int kRound = 64;                 // parts end where a stage of any kernel does
 int kind_of(int64_t rows) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : WIDE); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -927,10 +1068,26 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.nt_p));
     p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.nt_s));
     if (p.nt_s == ONE && sh.max_new == 1) p.nt_s = sh.n_req * sh.hk >= kSoloItems ? SOLO : FLAT;
-    // Parts of the keys: about a thousand work items in all, none below 256 keys
+    // Short prefixes and few requests: the prefix's bytes come from L2 for each of them,
+    // which costs less than a launch that joins.
+    if (sh.prefix > 0 && sh.prefix + sh.max_kv <= kAlongKeys && p.nt_s != SOLO && p.nt_s != WIDE &&
+        sh.n_req * p.tiles_s * sh.prefix * sh.hk * sh.hd * 4 <= kAlongBytes) {
+        p.nt_p = ALONG;
+        p.tiles_p = 1;
+        p.chunk_p = kRound;
+        p.splits_s = 1;
+        p.chunk_s = ceil_div(sh.max_kv < 1 ? 1 : sh.max_kv, kRound) * kRound;
+        p.direct = true;
+        return p;
+    }
+    // Parts of the keys: as many work items in all as the chip holds at once of the
+    // wide kernels (two workgroups a CU at 128, four at 64), none below 256 keys.
+    // More parts cost more partial rows: 64 requests behind 32768 tokens take 100 us
+    // with 512 items, 106 with 768, 116 with 1024; chunks of heads of 64 take 154, 151
+    // and 141.
     const int64_t base_p = (int64_t)p.tiles_p * sh.hk, base_s = sh.n_req * p.tiles_s * sh.hk;
     const int64_t blocks = base_p * ceil_div(sh.prefix, KB) + base_s * ceil_div(sh.max_kv, KB);
-    int64_t chunk = ceil_div(blocks, kTarget);
+    int64_t chunk = ceil_div(blocks, sh.hd == 128 ? 512 : 1024);
     if (chunk < 8) chunk = 8;
     // as many parts as that gives, of equal length
     auto parts = [&](int64_t keys, int* n, int64_t* len) {
@@ -941,7 +1098,7 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
         }
         int64_t k = ceil_div(ceil_div(keys, KB), chunk);
         if (k > 64) k = 64;
-        *len = ceil_div(ceil_div(keys, k), STG) * STG;
+        *len = ceil_div(ceil_div(keys, k), kRound) * kRound;
         *n = (int)ceil_div(keys, *len);
     };
     parts(sh.prefix, &p.splits_p, &p.chunk_p);
@@ -954,10 +1111,14 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
 
 hipError_t launch_prefix_attn(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAttnPtrs& t,
                               hipStream_t s) {
-    const Args a = args_of(sh, p, t);
-    if (a.blocks == 0) return hipSuccess;
-    const int64_t grid = a.blocks < (1 << 22) ? a.blocks : (1 << 22);
-    return sh.hd == 64 ? go<64>(p, a, (unsigned)grid, s) : go<128>(p, a, (unsigned)grid, s);
+    Args a = args_of(sh, p, t);
+    // more turns than a grid may have go into launches one after the other
+    for (a.base = 0; a.base < a.blocks; a.base += kMaxGrid) {
+        const unsigned grid = (unsigned)(a.blocks - a.base < kMaxGrid ? a.blocks - a.base : kMaxGrid);
+        const hipError_t e = sh.hd == 64 ? go<64>(p, a, grid, s) : go<128>(p, a, grid, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_prefix_join(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAttnPtrs& t,
@@ -965,11 +1126,19 @@ hipError_t launch_prefix_join(const PrefixAttnShape& sh, const PrefixAttnPlan& p
     if (p.direct) return hipSuccess;
     const Args a = args_of(sh, p, t);
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
-    int64_t gx = ceil_div(new_rows * sh.hq, NW);
+    // A thread for four elements while its loads of all parts fit a few rounds; a
+    // wave to a row beyond.
+    const bool few = p.splits_p + p.splits_s <= kJoinFew;
+    int64_t gx = ceil_div(new_rows * sh.hq, few ? NTHR / (sh.hd / 4) : NW);
     if (gx > 4096) gx = 4096;
     const dim3 grid((unsigned)gx, (unsigned)sh.n_req);
-    if (sh.hd == 64) prefix_join_kernel<64><<<grid, NTHR, 0, s>>>(a);
-    else prefix_join_kernel<128><<<grid, NTHR, 0, s>>>(a);
+    if (few) {
+        if (sh.hd == 64) prefix_join_few_kernel<64><<<grid, NTHR, 0, s>>>(a);
+        else prefix_join_few_kernel<128><<<grid, NTHR, 0, s>>>(a);
+    } else {
+        if (sh.hd == 64) prefix_join_kernel<64><<<grid, NTHR, 0, s>>>(a);
+        else prefix_join_kernel<128><<<grid, NTHR, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 

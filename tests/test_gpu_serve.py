@@ -664,8 +664,10 @@ def test_two_streams_at_once():
     assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
 
 
-def test_timing_classes_count_the_launches():
-    s = Server(2, 2, 2, 64, 16, 20, 4)
+@pytest.mark.parametrize("L, launches", [(20, 1), (1000, 2)])
+def test_timing_classes_count_the_launches(L, launches):
+    """A short prefix goes along with the requests' own keys; a long one has parts to join."""
+    s = Server(2, 2, 2, 64, 16, L, 4)
     s.feed([1, 1], 3)
     cola.timing_enable(True)
     cola.timing_reset()
@@ -676,4 +678,4 @@ def test_timing_classes_count_the_launches():
     finally:
         cola.timing_enable(False)
         cola.timing_reset()
-    assert n["pointwise"] == 3 and n["attn_fwd"] == 2 and sum(n.values()) == 5
+    assert n["pointwise"] == 3 and n["attn_fwd"] == launches and sum(n.values()) == 3 + launches
