@@ -7,14 +7,15 @@
 // the backward is the transpose, the same with -s.  HBM bound: each element is
 // read once and written once, 3 operations between.
 //
-// A thread owns one unit of a head, PV pairs in two vectors of PV elements: with
-// the half layout elements u PV .. and rot/2 + u PV .., interleaved the 2 PV
-// elements from 2 u PV on; units past the rotated part copy two vectors.  It
-// forms the unit's cosines and sines once and walks over heads of its row with
-// them.  The angle is taken in turns, pos * (f / 2 pi) in 64 bits, and only its
-// fraction goes to 32 bits: positions of 2^31 lose nothing.  Vectors are loaded
-// and stored at the elements' own alignment (gfx950 takes any address), so odd
-// pitches need no other path.
+// A thread owns one unit of a head and walks over heads of its row with it: with the
+// half layout PV pairs in two vectors of PV elements, u PV .. and rot/2 + u PV ..;
+// interleaved PV/2 pairs in one.  Units past the rotated part copy.  Neighbouring
+// threads own neighbouring vectors, so each load and store of a wave covers whole
+// runs.  The first heads' loads are issued before the cosines and sines are formed,
+// which every head of the row shares.  The angle is taken in turns, pos * (f / 2 pi)
+// in 64 bits, and only its fraction goes to 32 bits: positions of 2^31 lose nothing.
+// Vectors are loaded and stored at the elements' own alignment (gfx950 takes any
+// address), so odd pitches need no other path.
 #include <type_traits>
 
 #include "serve.hpp"
@@ -24,7 +25,6 @@ namespace cola {
 namespace {
 
 constexpr int NTHR = 256;
-constexpr int CH = 4;                 // heads whose loads a thread has in flight
 
 // PV elements, loaded and stored at the alignment of one of them.
 template <bool BF16, int PV>
@@ -39,6 +39,15 @@ struct Vec {
     Raw r;
     __device__ __forceinline__ void load(const E* p) { r = *reinterpret_cast<const Loose*>(p); }
     __device__ __forceinline__ void store(G p) const { *(__attribute__((address_space(1))) Loose*)p = r; }
+    // the first element alone
+    __device__ __forceinline__ void load_first(const E* p) {
+        if constexpr (sizeof(W) == sizeof(E)) r[0] = reinterpret_cast<const W*>(p)[0];
+        else r[0] = p[0];
+    }
+    __device__ __forceinline__ void store_first(G p) const {
+        if constexpr (sizeof(W) == sizeof(E)) ((__attribute__((address_space(1))) W*)p)[0] = r[0];
+        else p[0] = (E)r[0];
+    }
     __device__ __forceinline__ void get(float (&f)[PV]) const {
 #pragma unroll
         for (int i = 0; i < PV; ++i) {
@@ -70,10 +79,23 @@ __device__ __forceinline__ void turn(float x, float& c, float& s) {
     }
 }
 
+// Row t's place of head h: q, then k, then (with a cache) v.
+template <class E, bool CACHE>
+__device__ __forceinline__ const E* source(const RopeArgs& a, int64_t t, int h) {
+    if (h < a.hq) return (const E*)a.q + t * a.ldq + (int64_t)h * a.hd;
+    const int hk = h - a.hq;
+    if (CACHE && hk >= a.hk) return (const E*)a.v + t * a.ldv + (int64_t)(hk - a.hk) * a.hd;
+    return (const E*)a.k + t * a.ldk + (int64_t)hk * a.hd;
+}
+
 template <bool BF16, int PV, bool INTER, bool CACHE>
 __global__ __launch_bounds__(NTHR) void rope_kernel(const RopeArgs a) {
     typedef Vec<BF16, PV> V;
     typedef typename V::E E;
+    typedef typename V::G G;
+    constexpr int NV = INTER ? 1 : 2;                   // vectors of a unit
+    constexpr int NP = INTER ? PV / 2 : PV;             // its pairs
+    constexpr int CH = 8 / NV;                          // heads whose loads a thread has in flight
     const int per = a.lanes * a.units;                  // threads of one row
     int tl = 0, rem = (int)(blockIdx.y * NTHR + threadIdx.x);
     if (per < NTHR) {
@@ -84,112 +106,110 @@ __global__ __launch_bounds__(NTHR) void rope_kernel(const RopeArgs a) {
     const int hl = rem / a.units, u = rem - hl * a.units;
 
     const bool turning = u < a.turning;
-    const int half = a.rot / 2;
-    int A, B;                                           // the unit's two vectors in a head
-    if (!turning) {
-        A = a.rot + 2 * PV * (u - a.turning);
-        B = A + PV;
-    } else if (INTER) {
-        A = 2 * PV * u;
-        B = A + PV;
+    int at[2];                                          // the unit's vectors in a head
+    if (INTER) {
+        at[0] = PV * u;
+        at[1] = a.hd;
+    } else if (turning) {
+        at[0] = PV * u;
+        at[1] = at[0] + a.rot / 2;
     } else {
-        A = PV * u;
-        B = A + half;
+        at[0] = a.rot + PV * (u - a.turning);
+        at[1] = at[0] + PV * (a.units - a.turning);
     }
-    const bool two = B < a.hd;
+    // A vector past the head's end is left out; one across it (an odd head, pairs
+    // interleaved) has its first element alone.
+    const bool two = at[1] < a.hd, whole = at[0] + PV <= a.hd;
 
     const int H = a.hq + a.hk + (CACHE ? a.hk : 0);
     for (int64_t t = (int64_t)blockIdx.x * a.tpw + tl; t < a.T; t += (int64_t)gridDim.x * a.tpw) {
-        float c[PV], s[PV];
+        V x[CH][NV];
+        auto load = [&](int h0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int h = h0 + j * a.lanes;
+                if (h >= H) continue;
+                const E* src = source<E, CACHE>(a, t, h);
+                if (PV == 1 || !INTER || whole) x[j][0].load(src + at[0]);
+                else x[j][0].load_first(src + at[0]);
+                if (NV == 2 && two) x[j][NV - 1].load(src + at[1]);
+            }
+        };
+        load(hl);
+        float c[NP], s[NP];
         if (turning) {
             const int64_t p = a.pos ? (int64_t)a.pos[t] : (a.seq_len > 0 ? t % a.seq_len : t);
 #pragma unroll
-            for (int e = 0; e < PV; ++e) {
-                const double turns = (double)p * a.rev[PV * u + e];
+            for (int e = 0; e < NP; ++e) {
+                const double turns = (double)p * a.rev[NP * u + e];
                 turn<BF16>((float)(turns - rint(turns)), c[e], s[e]);
                 c[e] *= a.mscale;
                 s[e] *= a.mscale * a.sign;
             }
         }
-        int64_t at = -1;                                // this row's place in the cache, less the head's part
+        int64_t place = -1;                             // this row's place in the cache, less the head's part
         if constexpr (CACHE) {
             const int64_t slot = a.slots[t];
             if (slot >= 0 && slot < a.n_slots) {
                 const int64_t page = slot >> a.lg_page, off = slot & ((int64_t(1) << a.lg_page) - 1);
-                at = ((page * a.hk) << a.lg_page) + off;
+                place = ((page * a.hk) << a.lg_page) + off;
             }
         }
         for (int h0 = hl; h0 < H; h0 += CH * a.lanes) {
-            V x[CH], y[CH];
-            typename V::G dst[CH];
-            bool on[CH];
+            if (h0 != hl) load(h0);
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
                 const int h = h0 + j * a.lanes;
-                on[j] = h < H;
-                if (!on[j]) continue;
-                const E* src;
-                if (h < a.hq) {
-                    src = (const E*)a.q + t * a.ldq + (int64_t)h * a.hd;
-                    dst[j] = (typename V::G)a.qo + t * a.ldqo + (int64_t)h * a.hd;
-                } else {
-                    const int hk = h - a.hq;
-                    if constexpr (CACHE) {
-                        const bool val = hk >= a.hk;
-                        const int hh = val ? hk - a.hk : hk;
-                        src = (val ? (const E*)a.v + t * a.ldv : (const E*)a.k + t * a.ldk) + (int64_t)hh * a.hd;
-                        dst[j] = (typename V::G)(val ? a.V : a.K) + (at + ((int64_t)hh << a.lg_page)) * a.hd;
-                        on[j] = at >= 0;
-                    } else {
-                        src = (const E*)a.k + t * a.ldk + (int64_t)hk * a.hd;
-                        dst[j] = (typename V::G)a.ko + t * a.ldko + (int64_t)hk * a.hd;
-                    }
-                }
-                if (on[j]) {
-                    x[j].load(src + A);
-                    if (two) y[j].load(src + B);
-                }
-            }
+                if (h >= H) continue;
+                if (turning && h < a.hq + a.hk) {
+                    float p[PV];
+                    x[j][0].get(p);
+                    if constexpr (INTER) {
 #pragma unroll
-            for (int j = 0; j < CH; ++j) {
-                if (!on[j]) continue;
-                if (turning && h0 + j * a.lanes < a.hq + a.hk) {
-                    float p[PV], q[PV];
-                    x[j].get(p);
-                    y[j].get(q);
-                    if constexpr (INTER && PV > 1) {
-                        // pairs 0 .. PV/2 - 1 in the first vector, the others in the second
-#pragma unroll
-                        for (int e = 0; e < PV / 2; ++e) {
-                            const float p0 = p[2 * e], q0 = q[2 * e];
+                        for (int e = 0; e < NP; ++e) {
+                            const float p0 = p[2 * e];
                             p[2 * e] = p0 * c[e] - p[2 * e + 1] * s[e];
                             p[2 * e + 1] = p[2 * e + 1] * c[e] + p0 * s[e];
-                            q[2 * e] = q0 * c[e + PV / 2] - q[2 * e + 1] * s[e + PV / 2];
-                            q[2 * e + 1] = q[2 * e + 1] * c[e + PV / 2] + q0 * s[e + PV / 2];
                         }
                     } else {
+                        float q[PV];
+                        x[j][NV - 1].get(q);
 #pragma unroll
-                        for (int e = 0; e < PV; ++e) {
+                        for (int e = 0; e < NP; ++e) {
                             const float p0 = p[e];
                             p[e] = p0 * c[e] - q[e] * s[e];
                             q[e] = q[e] * c[e] + p0 * s[e];
                         }
+                        x[j][NV - 1].put(q);
                     }
-                    x[j].put(p);
-                    y[j].put(q);
+                    x[j][0].put(p);
                 }
-                x[j].store(dst[j] + A);
-                if (two) y[j].store(dst[j] + B);
+                G dst;
+                if (h < a.hq) {
+                    dst = (G)a.qo + t * a.ldqo + (int64_t)h * a.hd;
+                } else if constexpr (CACHE) {
+                    if (place < 0) continue;
+                    const int hk = h - a.hq;
+                    const bool val = hk >= a.hk;
+                    dst = (G)(val ? a.V : a.K) + (place + ((int64_t)(val ? hk - a.hk : hk) << a.lg_page)) * a.hd;
+                } else {
+                    dst = (G)a.ko + t * a.ldko + (int64_t)(h - a.hq) * a.hd;
+                }
+                if (PV == 1 || !INTER || whole) x[j][0].store(dst + at[0]);
+                else x[j][0].store_first(dst + at[0]);
+                if (NV == 2 && two) x[j][NV - 1].store(dst + at[1]);
             }
         }
     }
 }
 
 template <bool BF16, int PV>
-hipError_t go(bool inter, bool cache, const RopeArgs& a, dim3 grid, hipStream_t s) {
-    if (inter) {
-        if (cache) rope_kernel<BF16, PV, true, true><<<grid, NTHR, 0, s>>>(a);
-        else rope_kernel<BF16, PV, true, false><<<grid, NTHR, 0, s>>>(a);
+hipError_t go(bool cache, const RopeArgs& a, dim3 grid, hipStream_t s) {
+    if (a.interleaved) {
+        if constexpr (PV > 1) {
+            if (cache) rope_kernel<BF16, PV, true, true><<<grid, NTHR, 0, s>>>(a);
+            else rope_kernel<BF16, PV, true, false><<<grid, NTHR, 0, s>>>(a);
+        }
     } else {
         if (cache) rope_kernel<BF16, PV, false, true><<<grid, NTHR, 0, s>>>(a);
         else rope_kernel<BF16, PV, false, false><<<grid, NTHR, 0, s>>>(a);
@@ -200,17 +220,19 @@ hipError_t go(bool inter, bool cache, const RopeArgs& a, dim3 grid, hipStream_t 
 }  // namespace
 
 hipError_t launch_rope(bool bf16, bool cache, RopeArgs& a, hipStream_t s) {
-    // the widest vector that divides the rotated half and the head
-    const int top = bf16 ? 8 : 4;
-    int pv = top;
-    while (pv > 1 && ((a.rot / 2) % pv != 0 || a.hd % pv != 0)) pv /= 2;
-    a.turning = a.rot / 2 / pv;
-    a.units = a.turning + (a.hd - a.rot + 2 * pv - 1) / (2 * pv);
-    const int H = a.hq + (cache ? 2 : 1) * a.hk;
-    // Threads of a row share its heads out: about eight heads each where there
-    // are rows enough to fill the chip, down to one each where there are few.
+    // The widest vector that divides the rotated part's vectors and the head;
+    // interleaved pairs need two elements, and an odd head then ends in half of one.
+    int pv = bf16 ? 8 : 4;
+    const int turned = a.interleaved ? a.rot : a.rot / 2, least = a.interleaved ? 2 : 1;
+    while (pv > least && (turned % pv != 0 || a.hd % pv != 0)) pv /= 2;
+    a.turning = turned / pv;
+    const int copied = (a.hd - a.rot + pv - 1) / pv;
+    a.units = a.turning + (a.interleaved ? copied : (copied + 1) / 2);
+    const int H = a.hq + (cache ? 2 : 1) * a.hk, CH = a.interleaved ? 8 : 4;
+    // Threads of a row share its heads out: as many heads each as it has loads in
+    // flight, down to one each where rows are few (2^18 threads fill the chip).
     int64_t lanes = (int64_t(1) << 18) / (a.T * a.units) + 1;
-    if (lanes < (H + 7) / 8) lanes = (H + 7) / 8;
+    if (lanes < (H + CH - 1) / CH) lanes = (H + CH - 1) / CH;
     if (lanes > H) lanes = H;
     a.lanes = (int)lanes;
     const int per = a.lanes * a.units;
@@ -219,14 +241,14 @@ hipError_t launch_rope(bool bf16, bool cache, RopeArgs& a, hipStream_t s) {
     if (gx > (1 << 20)) gx = 1 << 20;
     const dim3 grid((unsigned)gx, (unsigned)(per < NTHR ? 1 : (per + NTHR - 1) / NTHR));
     if (bf16) {
-        if (pv == 8) return go<true, 8>(a.interleaved, cache, a, grid, s);
-        if (pv == 4) return go<true, 4>(a.interleaved, cache, a, grid, s);
-        if (pv == 2) return go<true, 2>(a.interleaved, cache, a, grid, s);
-        return go<true, 1>(a.interleaved, cache, a, grid, s);
+        if (pv == 8) return go<true, 8>(cache, a, grid, s);
+        if (pv == 4) return go<true, 4>(cache, a, grid, s);
+        if (pv == 2) return go<true, 2>(cache, a, grid, s);
+        return go<true, 1>(cache, a, grid, s);
     }
-    if (pv == 4) return go<false, 4>(a.interleaved, cache, a, grid, s);
-    if (pv == 2) return go<false, 2>(a.interleaved, cache, a, grid, s);
-    return go<false, 1>(a.interleaved, cache, a, grid, s);
+    if (pv == 4) return go<false, 4>(cache, a, grid, s);
+    if (pv == 2) return go<false, 2>(cache, a, grid, s);
+    return go<false, 1>(cache, a, grid, s);
 }
 
 }  // namespace cola
