@@ -1027,7 +1027,6 @@ hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t
     else COLA_GO(ONE, SOLO);
     else COLA_GO(TWO, ONE);
     else COLA_GO(TWO, FLAT);
-    else COLA_GO(TWO, SOLO);
     else COLA_GO(TWO, TWO);
     else COLA_GO(WIDE, ONE);
     else COLA_GO(WIDE, FLAT);
@@ -1067,7 +1066,10 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     p.nt_p = kind_of(sh.T * g);                              // never below nt_s
     p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.nt_p));
     p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.nt_s));
-    if (p.nt_s == ONE && sh.max_new == 1) p.nt_s = sh.n_req * sh.hk >= kSoloItems ? SOLO : FLAT;
+    if (p.nt_s == ONE && sh.max_new == 1)
+        p.nt_s = sh.n_req * sh.hk >= kSoloItems && (sh.prefix == 0 || p.nt_p == WIDE) ? SOLO : FLAT;
+    // without a prefix, the kernel whose prefix part asks for least
+    if (sh.prefix == 0) p.nt_p = p.nt_s == TWO || p.nt_s == WIDE ? p.nt_s : ONE;
     // Short prefixes and few requests: the prefix's bytes come from L2 for each of them,
     // which costs less than a launch that joins.
     if (sh.prefix > 0 && sh.prefix + sh.max_kv <= kAlongKeys && p.nt_s != SOLO && p.nt_s != WIDE &&

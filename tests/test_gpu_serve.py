@@ -178,6 +178,31 @@ def test_append(case, dtype):
     assert torch.equal(K, K0) and torch.equal(V, V0)
 
 
+@pytest.mark.parametrize("layout", ("half", "interleaved"))
+def test_large_results_are_the_small_ones(layout):
+    """Results of more than 48 MB leave by other stores: the bits of the same rows in parts."""
+    T, hq, hk, hd, page = 6300, 32, 8, 128, 16
+    q, k, v = (rand(s, (T, h * hd), "bf16") for s, h in ((1, hq), (2, hk), (3, hk)))
+    pos = torch.arange(T, dtype=torch.int32, device=DEV) * 7
+    slots = torch.randperm(T, device=DEV).int()
+    pages = -(-T // page)
+    c = cola.cache_desc(pages, page, hk, hd)
+    got, want = ([torch.zeros_like(q), torch.zeros_like(k)] + [torch.zeros((pages, hk, page, hd), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+                 for _ in range(2))
+    for res, step in ((got, T), (want, 1575)):
+        for at in range(0, T, step):
+            n = slice(at, at + step)
+            d = cola.rope_desc(step, hq, hk, hd, 64, layout=layout)
+            cola.rope_bwd(d, q[n], k[n], pos[n], res[0][n], res[1][n])
+            cola.cache_append(d, c, q[n], k[n], v[n], pos[n], slots[n], torch.empty_like(q[n]), res[2], res[3])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    qo = torch.empty_like(q)
+    cola.cache_append(cola.rope_desc(T, hq, hk, hd, 64, layout=layout), c, q, k, v, pos, slots, qo, got[2], got[3])
+    back = torch.empty_like(q)
+    cola.rope_fwd(cola.rope_desc(T, hq, 0, hd, 64, layout=layout), q, None, pos, back, None)
+    assert torch.equal(qo, back)
+
+
 def test_append_past_4_gib():
     """Slots whose bytes lie past 2^32 of the cache."""
     hk, hd, page = 8, 128, 64
@@ -372,6 +397,32 @@ ATTN = {
 }
 
 
+# Each kernel of the launch plan: how the prefix's rows are tiled (along with the
+# requests, 16, 32 or 128 to a tile), and a request's own (one token: four waves or
+# one to a tile; 16, 32 or 128 rows).  (new, kv, L, hq, hk)
+KERNELS = {
+    "along-flat": ([1, 1], [30, 70], 90, 2, 1), "along-one": ([5, 2], [30, 70], 90, 2, 1), "along-two": ([12, 3], [30, 70], 90, 2, 1),
+    "along-no-own": ([1, 1, 1], [0, 0, 0], 90, 2, 1),
+    "one-one": ([3, 2], [50, 9], 700, 2, 1), "one-flat": ([1, 1], [50, 9], 700, 4, 2),
+    "one-solo": ([1] * 514, [(7 * i) % 50 for i in range(514)], 0, 8, 8),
+    "two-one": ([4] * 6, [4, 10, 33, 50, 7, 64], 700, 2, 2), "two-flat": ([1] * 12, [5 * i for i in range(12)], 700, 4, 2),
+    "two-two": ([20, 5], [30, 100], 700, 2, 2), "two-no-prefix": ([20, 5], [30, 100], 0, 2, 2),
+    "wide-one": ([3] * 20, [3 + 9 * i for i in range(20)], 700, 2, 2), "wide-flat": ([1] * 40, [7 * i for i in range(40)], 700, 4, 2),
+    "wide-solo": ([1] * 513, [(5 * i) % 40 for i in range(513)], 650, 8, 8),
+    "wide-two": ([20] * 3, [20, 50, 131], 700, 2, 2), "wide-wide": ([50, 40], [50, 333], 700, 2, 2),
+    # many parts of the keys, of the requests' own and of the prefix
+    "parts": ([1, 1], [5000, 3], 3000, 2, 1), "parts-own": ([40], [3000], 0, 2, 2), "parts-chunk": ([9, 30], [2000, 30], 2500, 2, 1),
+}
+
+
+@pytest.mark.parametrize("hd", (64, 128))
+@pytest.mark.parametrize("name", sorted(KERNELS))
+def test_attention_kernels(name, hd):
+    new, kv, L, hq, hk = KERNELS[name]
+    print("kernels", name, hd, flush=True)
+    Batch(len(name) + hd, new, kv, L, hq, hk, hd, 16 if hd == 64 else 64, pad=2).check()
+
+
 @pytest.mark.parametrize("name", sorted(ATTN))
 def test_attention(name):
     print("attention", name, ATTN[name], flush=True)
@@ -431,7 +482,8 @@ def test_attention_masked_values_do_not_reach_a_row(value):
     """A later token whose key or value is not finite changes the rows that see it
     and no other."""
     kw = dict(new=[12, 1], kv=[40, 20], L=20, hq=4, hk=2, hd=64, page=16)
-    for seed, kw in ((11, kw), (12, dict(kw, hd=128)), (13, dict(kw, new=[40, 1], L=0))):
+    for seed, kw in ((11, kw), (12, dict(kw, hd=128)), (13, dict(kw, new=[40, 1], L=0)), (14, dict(kw, new=[40, 1], hd=128, L=700)),
+                     (15, dict(kw, new=[5, 1])), (16, dict(kw, new=[3, 1], hd=128, L=900))):
         b = Batch(seed, **kw)
         clean, cl = b.run()
         n = kw["new"][0]
