@@ -623,7 +623,7 @@ template <int HD>
 constexpr int kWideBytes = 4 * KeyTile<HD>::BYTES + 16;
 
 // item() for a tile of 128 rows: the same rows, keys and results.
-template <int HD, bool CAUSAL>
+template <int HD, bool CAUSAL, bool ALONG>
 __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
                                           int n_rows, int first, int end, int k0, int chunk, int slot) {
     typedef KeyTile<HD> Tile;
@@ -655,11 +655,18 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
     uint32_t from[Tile::NL];
 #pragma unroll
     for (int j = 0; j < Tile::NL; ++j) from[j] = Tile::from(j, wave, lane);
-    // what the tile's last row sees, and what this wave's first and last row see
-    const int any = uniform(a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0), all = uniform(min(seen(tile0), any));
     const int w0 = tile0 + 32 * wave;
-    const int w_any = uniform(w0 < n_rows ? min(seen(min(w0 + 32, n_rows) - 1), any) : 0),
-              w_all = uniform(w0 < n_rows ? min(seen(w0), any) : 0);
+    // the last stage of each buffer that held values that are not finite
+    int* odd = reinterpret_cast<int*>(lds + 4 * B);
+    // The next stage has landed, and every wave has left this one.
+    auto turn = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    // The keys k0 .. of one table: the tile's last row sees those up to `any`, its
+    // first those up to `all`; this wave's rows up to w_any and w_all.
+    auto walk = [&](auto causal, const int32_t* table, int k0, int any, int all, int w_any, int w_all)
+                    __attribute__((always_inline)) {
+    constexpr bool C = decltype(causal)::value;
     const int n = any > k0 ? (any - k0 + STG - 1) / STG : 0;
 
     // The pages of stage i's tiles of 16, looked up a turn before they are used.
@@ -697,13 +704,7 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
         }
         return there;
     };
-    // The next stage has landed, and every wave has left this one.
-    auto turn = [&]() __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    };
     uint32_t there = 0, next = 0;
-    // the last stage of each buffer that held values that are not finite
-    int* odd = reinterpret_cast<int*>(lds + 4 * B);
     // Stage i from one buffer while the next is loaded into the other: the
     // __restrict parameters say that they don't overlap (without them the compiler
     // waits for the loads in flight before the first read).
@@ -713,7 +714,7 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
         // A key that some row of the tile sees and another does not must not reach
         // the second by 0 * inf: values that are not finite leave the product,
         // and go to the rows that see them by themselves.
-        const bool mixed = CAUSAL && kb + STG > all;
+        const bool mixed = C && kb + STG > all;
         if (mixed) {
             char* mine = kt + B + Tile::RW * wave * Tile::ROW + 16 * lane;
             uint32_t any_odd = 0;
@@ -763,6 +764,21 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
     for (int i = 0; i < n; ++i) {
         step(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
         turn();
+    }
+    };
+    if constexpr (ALONG) {
+        const int end_p = uniform(a.n_pages > 0 ? a.prefix : 0), w_end = w0 < n_rows ? end_p : 0;
+        const int lim = w.lim;
+        w.lim = live ? end_p : 0;
+        walk(std::false_type{}, a.prefix_table, 0, end_p, end_p, w_end, w_end);
+        w.lim = lim;
+    }
+    {
+        const int any = uniform(a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0);
+        const int all = uniform(min(seen(tile0), any));
+        const int w_any = uniform(w0 < n_rows ? min(seen(min(w0 + 32, n_rows) - 1), any) : 0);
+        const int w_all = uniform(w0 < n_rows ? min(seen(w0), any) : 0);
+        walk(std::integral_constant<bool, CAUSAL>{}, table, k0, any, all, w_any, w_all);
     }
     // Lane (hh, row) has the elements 32 u + 8 j + 4 hh .. + 3 in o[u][4 j ..].  They go
     // out by way of LDS, a region for each wave, so that a store covers whole rows:
@@ -826,7 +842,7 @@ __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t
                                          int n_rows, int first, int end, int k0, int chunk, int slot) {
     constexpr bool ALONG_P = NP == ALONG;
     if constexpr (N == WIDE)
-        wide_item<HD, CAUSAL>(a, lds, table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+        wide_item<HD, CAUSAL, ALONG_P>(a, lds, table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
     else if constexpr (N == SOLO)
         item<HD, 1, 1, false, false, kAhead<HD, N, NP>>(a, nullptr, table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0, chunk, slot);
     else if constexpr (N == FLAT)
@@ -853,7 +869,7 @@ __host__ __device__ constexpr int64_t turns(int64_t units, int tiles) { return t
 
 // NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
 template <int HD, int NP, int NS>
-__global__ __launch_bounds__(NTHR, (NP == WIDE ? 2 : 1)) void prefix_attn_kernel(const Args a) {
+__global__ __launch_bounds__(NTHR, (NP == WIDE || NS == WIDE ? 2 : 1)) void prefix_attn_kernel(const Args a) {
     constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     const int64_t at = a.base + blockIdx.x;
@@ -1022,6 +1038,7 @@ hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t
     COLA_GO(ALONG, ONE);
     else COLA_GO(ALONG, TWO);
     else COLA_GO(ALONG, FLAT);
+    else COLA_GO(ALONG, WIDE);
     else COLA_GO(ONE, ONE);
     else COLA_GO(ONE, FLAT);
     else COLA_GO(ONE, SOLO);
@@ -1050,6 +1067,12 @@ constexpr int64_t kJoinFew = 8;
 // us against 8.0 behind 64 keys, 7.4 against 8.1 behind 512, 10.0 against 8.5 behind
 // 1024; 64 requests: 9.4 against 12.1 at 34 MB, 12.0 against 12.4 at 67 MB.
 constexpr int64_t kAlongKeys = 640, kAlongBytes = 40000000;
+// The same of tiles of 128 rows, whose partial rows are more.  64 requests with 64
+// queries of 16 heads over 2, 256 + 256 keys: 18.3 us against 37.6; of 16 over 4, 200
+// + 700 keys: 27.9 against 39.0; of 8 heads of 128, 512 + 64 keys, 134 MB: 25.1
+// against 31.9.  1000 + 100 keys take 23.0 against 18.2, 512 + 1000 keys 32.1 against
+// 28.8.
+constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
 int kind_of(int64_t rows) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : WIDE); }
@@ -1072,8 +1095,9 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     if (sh.prefix == 0) p.nt_p = p.nt_s == TWO || p.nt_s == WIDE ? p.nt_s : ONE;
     // Short prefixes and few requests: the prefix's bytes come from L2 for each of them,
     // which costs less than a launch that joins.
-    if (sh.prefix > 0 && sh.prefix + sh.max_kv <= kAlongKeys && p.nt_s != SOLO && p.nt_s != WIDE &&
-        sh.n_req * p.tiles_s * sh.prefix * sh.hk * sh.hd * 4 <= kAlongBytes) {
+    const bool wide = p.nt_s == WIDE;
+    if (sh.prefix > 0 && sh.prefix + sh.max_kv <= (wide ? kWideAlongKeys : kAlongKeys) && p.nt_s != SOLO &&
+        sh.n_req * p.tiles_s * sh.prefix * sh.hk * sh.hd * 4 <= (wide ? kWideAlongBytes : kAlongBytes)) {
         p.nt_p = ALONG;
         p.tiles_p = 1;
         p.chunk_p = kRound;
@@ -1091,20 +1115,24 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     const int64_t blocks = base_p * ceil_div(sh.prefix, KB) + base_s * ceil_div(sh.max_kv, KB);
     int64_t chunk = ceil_div(blocks, sh.hd == 128 ? 512 : 1024);
     if (chunk < 8) chunk = 8;
-    // as many parts as that gives, of equal length
-    auto parts = [&](int64_t keys, int* n, int64_t* len) {
+    // As many parts as that gives, of equal length.  Without a prefix, less than two
+    // parts' worth of own keys is one: a call without a join (111 requests of up to 538
+    // keys, 52 queries of 16 heads over 2: 25.7 us against 42.6; 7 requests of up to 353
+    // keys, 29 queries: 7.0 against 9.7).
+    auto parts = [&](int64_t keys, bool one, int* n, int64_t* len) {
         if (keys == 0) {
             *n = 0;
             *len = KB;
             return;
         }
         int64_t k = ceil_div(ceil_div(keys, KB), chunk);
+        if (one && k == 2) k = 1;
         if (k > 64) k = 64;
         *len = ceil_div(ceil_div(keys, k), kRound) * kRound;
         *n = (int)ceil_div(keys, *len);
     };
-    parts(sh.prefix, &p.splits_p, &p.chunk_p);
-    parts(sh.max_kv, &p.splits_s, &p.chunk_s);
+    parts(sh.prefix, false, &p.splits_p, &p.chunk_p);
+    parts(sh.max_kv, sh.prefix == 0, &p.splits_s, &p.chunk_s);
     const int64_t n = (p.splits_p + p.splits_s) * p.rows;
     p.direct = p.splits_p == 0 && p.splits_s == 1;
     p.ws_bytes = p.direct || n == 0 ? 0 : (size_t)((2 * n + 63) / 64 * 64 + n * sh.hd) * 4;

@@ -402,6 +402,8 @@ ATTN = {
 # one to a tile; 16, 32 or 128 rows).  (new, kv, L, hq, hk)
 KERNELS = {
     "along-flat": ([1, 1], [30, 70], 90, 2, 1), "along-one": ([5, 2], [30, 70], 90, 2, 1), "along-two": ([12, 3], [30, 70], 90, 2, 1),
+    "along-wide": ([50, 5], [70, 20], 90, 2, 1), "along-wide-tiles": ([150, 1, 90], [300, 40, 90], 333, 4, 2),
+    "along-wide-no-own": ([70, 130], [0, 0], 90, 2, 1),
     "along-no-own": ([1, 1, 1], [0, 0, 0], 90, 2, 1),
     "one-one": ([3, 2], [50, 9], 700, 2, 1), "one-flat": ([1, 1], [50, 9], 700, 4, 2),
     "one-solo": ([1] * 514, [(7 * i) % 50 for i in range(514)], 0, 8, 8),
