@@ -424,7 +424,7 @@ typedef struct {
     double base;              /* > 1 */
     double factor;            /* >= 1 (NONE: not read) */
     double low, high;         /* YARN, WAVELENGTH: 0 < low < high */
-    double mscale;            /* factor on cosine and sine, 0 = 1 (YARN: 1 + 0.1 ln factor) */
+    double mscale;            /* factor on cosine and sine, up to 1e30; 0 = 1 (YARN: 1 + 0.1 ln factor) */
     int64_t orig_len;         /* YARN, WAVELENGTH: >= 1 */
 } cola_rope_desc;
 
@@ -433,9 +433,9 @@ typedef struct {
  * [T][ldqo] and k_out [T][ldko].  An output may be its input (same pointer and
  * pitch); any other overlap is not allowed.  The angle is formed in 64 bits
  * from frequencies in 64 bits, whatever the dtype; the products are fp32,
- * rounded once. Rows and pitches of any alignment run at full speed; the
- * vector width falls with the largest power of two that divides head_dim and
- * rot_dim / 2. */
+ * rounded once.  Rows may have any alignment and pitch (of the elements' own);
+ * large results are fastest where they start on 64 bytes.  The vector width
+ * falls with the largest power of two that divides head_dim and rot_dim / 2. */
 int cola_rope_fwd(const cola_rope_desc* desc, const void* q, const void* k, const int32_t* positions,
                   void* q_out, void* k_out, cola_stream_t stream);
 /* The gradient: dq_out, dk_out (pitches ldq, ldk) turned back into dq, dk
@@ -492,8 +492,8 @@ int cola_page_map(const cola_page_map_desc* desc, const int32_t* kv_len, const i
 
 /* Attention of a batch whose requests share their first prefix_len tokens, over
  * the paged cache: the prefix's keys are read once for all rows of the batch.
- * Request r has its rows (new tokens) in start[r] .. start[r + 1] - 1 (start NULL:
- * one row each, row r) and kv_len[r] tokens of its own in the cache, in the pages
+ * Request r has its rows (new tokens) in start[r] .. start[r + 1] - 1 (n_req + 1
+ * entries that do not fall; start NULL: one row each, row r) and kv_len[r] tokens of its own in the cache, in the pages
  * table[r][..], its new ones the last of them.  Query head h reads key head
  * h / (heads_q / heads).  Row i of n rows sees the whole prefix and its own
  * tokens 0 .. kv_len - n + i:
@@ -508,9 +508,12 @@ int cola_page_map(const cola_page_map_desc* desc, const int32_t* kv_len, const i
  * the data alone (fixed order of every sum).
  * bf16; head_dim 64 or 128; q, out, K, V, ws 16-byte aligned, ldq and ldo
  * multiples of 8; out must not overlap q.  Products and sums are fp32, the
- * probabilities rounded to bf16 for the second product. */
+ * probabilities rounded to bf16 for the second product.  ws is scratch of the
+ * stated size (0: may be NULL) that holds nothing between calls; calls that share
+ * it, replays of captured graphs among them, must be ordered. */
 typedef struct {
-    int64_t n_req;            /* requests, 0 .. 65535 */
+    int64_t n_req;            /* requests, 0 .. 65535; n_req * heads_q <= 2^28, and n_req * heads_q *
+                                 min(max_new, T) <= 2^36 */
     int64_t T;                /* rows of q and out; T * heads_q < 2^31 */
     int64_t heads_q;          /* a multiple of the cache's heads */
     int64_t prefix_len;       /* tokens in the pages of prefix_table (0: NULL) */
@@ -518,7 +521,7 @@ typedef struct {
     int64_t max_new;          /* most rows of one request (>= 1) */
     int64_t max_pages;        /* entries per row of table, 0 = as many as max_kv needs */
     int64_t ldq, ldo;         /* row pitches, 0 = heads_q * head_dim */
-    double scale;             /* 0 = 1 / sqrt(head_dim); not negative */
+    double scale;             /* 0 = 1 / sqrt(head_dim); 1e-30 .. 6e29 */
 } cola_prefix_attn_desc;
 size_t cola_prefix_attn_workspace_bytes(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache);
 int cola_prefix_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, const void* q, const void* K,

@@ -10,11 +10,15 @@
 // request's own tokens another, both split along the keys where there are few
 // rows, and a second launch joins the parts in a fixed order.
 //
-// A work item is (row tile, key head, part of the keys).  Its rows are (query,
-// head of the group) pairs, the head running fastest; NT columns of 16 of them
-// are the matrix instructions' n side.  The four waves of a workgroup take the
-// part's blocks of 32 keys in turn, each with its own running maximum and sum, and
-// join through LDS at the end.  A wave keeps everything in registers:
+// A work item is (row tile, key head, part of the keys), one to a workgroup (a
+// loop over items on the GPU held too many registers: two waves a SIMD where four
+// to six fit).  Its rows are (query, head of the group) pairs, the head running
+// fastest, so that heads that share keys share their reads.  Three kernels' worth
+// of tiles, by the number of rows:
+//
+// 16 or 32 rows (single tokens, short chunks): bound by the keys' bytes, so the
+// least may stand between memory and the matrix unit.  A wave keeps everything in
+// registers, NT columns of 16 rows:
 //   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, K rows straight from the cache in the
 //                 operand's layout (lane l: key l % 16, 8 elements at 8 (l / 16)),
 //                 two tiles of 16 keys;
@@ -26,10 +30,24 @@
 //                 together with one v_perm a pair.  Row m of output tile t is
 //                 then element D m + t, so a lane ends with 4 D neighbouring
 //                 elements of its row.
-// The probabilities are rounded to bf16 for the second product only; the sum l is
-// of the fp32 ones (the log-sum-exp needs them), each lane's own until the end.
-// No LDS, no transposing pass, no barrier in the loop: key and value bytes go
-// from memory to the matrix unit.
+// No LDS, no transposing pass, no barrier in the loop.  The four waves of a
+// workgroup take the part's blocks of 32 keys in turn, each with its own running
+// maximum and sum, and join through LDS at the end; where single-token requests
+// are many, a wave has an item of its own.  200 requests of 32 heads of 128 and up to
+// 300 own tokens (490 MB): 96 us, 5.1 TB/s of the 6.2 that reading alone reaches.
+//
+// More rows: tiles of 128, bound by the softmax's arithmetic and the matrix
+// products, keys staged in LDS once for all of them (below).  16 chunks of up to
+// 256 tokens, 32 heads of 64, behind 4096 + 1000 tokens (84 GFLOP): 137 us, 620
+// TFLOP/s; the exponentials, maxima and sums of a head of 64 take the vector unit
+// as long as its products take the matrix unit.
+//
+// Short prefixes: a request's own items read them along (the bytes come from L2),
+// and neither partial rows nor a join are left.
+//
+// The probabilities are rounded to bf16 for the second product only (the matrix
+// unit's type; half a step of 2^-8 each, which averages out over the keys); the sum
+// l is of the fp32 ones (the log-sum-exp needs them), each lane's own until the end.
 #include <math.h>
 
 #include <type_traits>
@@ -343,8 +361,6 @@ __device__ __forceinline__ void block(Wave<HD, NT>& w, const Args& a, Keys<HD>& 
 }
 
 // LDS of one wave's state on its way to another: accumulators, sum, maximum.
-template <int HD, int NT>
-constexpr int WAVES = HD * NT <= 128 ? 3 : 2;
 template <int HD, int NT>
 constexpr int kStateFloats = 64 * NT * (HD / 16 * 4 + 2);
 
@@ -666,105 +682,105 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
     // first those up to `all`; this wave's rows up to w_any and w_all.
     auto walk = [&](auto causal, const int32_t* table, int k0, int any, int all, int w_any, int w_all)
                     __attribute__((always_inline)) {
-    constexpr bool C = decltype(causal)::value;
-    const int n = any > k0 ? (any - k0 + STG - 1) / STG : 0;
+        constexpr bool C = decltype(causal)::value;
+        const int n = any > k0 ? (any - k0 + STG - 1) / STG : 0;
 
-    // The pages of stage i's tiles of 16, looked up a turn before they are used.
-    int page[Tile::TILES] = {};
-    auto look = [&](int i) __attribute__((always_inline)) {
-        const int kb = k0 + STG * i;
-        if (1 << a.lg_page >= STG) {                   // the stage lies in one page
-            const int p = page_of(a, table, kb, any);
+        // The pages of stage i's tiles of 16, looked up a turn before they are used.
+        int page[Tile::TILES] = {};
+        auto look = [&](int i) __attribute__((always_inline)) {
+            const int kb = k0 + STG * i;
+            if (1 << a.lg_page >= STG) {                   // the stage lies in one page
+                const int p = page_of(a, table, kb, any);
 #pragma unroll
-            for (int x = 0; x < Tile::TILES; ++x) page[x] = p;
-        } else {
+                for (int x = 0; x < Tile::TILES; ++x) page[x] = p;
+            } else {
 #pragma unroll
-            for (int x = 0; x < Tile::TILES; ++x) page[x] = page_of(a, table, kb + 16 * x, any);
-        }
-    };
-    constexpr uint32_t ALL = (1u << Tile::TILES) - 1;
-    // Stage i into the buffer at `to`: keys from `any` on and missing pages arrive as
-    // zeros (they lie past the descriptor's range).  Returns the pages that are there.
-    auto load = [&](int i, char* to) __attribute__((always_inline)) -> uint32_t {
-        uint32_t there = 0;
-        int mine = page[0];
+                for (int x = 0; x < Tile::TILES; ++x) page[x] = page_of(a, table, kb + 16 * x, any);
+            }
+        };
+        constexpr uint32_t ALL = (1u << Tile::TILES) - 1;
+        // Stage i into the buffer at `to`: keys from `any` on and missing pages arrive as
+        // zeros (they lie past the descriptor's range).  Returns the pages that are there.
+        auto load = [&](int i, char* to) __attribute__((always_inline)) -> uint32_t {
+            uint32_t there = 0;
+            int mine = page[0];
 #pragma unroll
-        for (int x = 0; x < Tile::TILES; ++x) {
-            there |= (uint32_t)in_cache(a, page[x]) << x;
-            if (x == Tile::RW * wave / 16) mine = page[x];
-        }
-        const int kb = k0 + STG * i + (Tile::RW * wave & ~15), rows = rows_in(in_cache(a, mine), kb, any);
-        const int64_t at = row_of(a, mine, head, kb);
-        to += Tile::RW * wave * Tile::ROW;
-        const auto rk = rows_of<HD>(a.K, at, rows), rv = rows_of<HD>(a.V, at, rows);
-#pragma unroll
-        for (int j = 0; j < Tile::NL; ++j) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lptr_t)(to + 1024 * j), 16, from[j], 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lptr_t)(to + B + 1024 * j), 16, from[j], 0, 0, 0);
-        }
-        return there;
-    };
-    uint32_t there = 0, next = 0;
-    // Stage i from one buffer while the next is loaded into the other: the
-    // __restrict parameters say that they don't overlap (without them the compiler
-    // waits for the loads in flight before the first read).
-    auto step = [&](char* __restrict to, char* __restrict kt, int i) __attribute__((always_inline)) {
-        const int kb = k0 + STG * i;
-        next = i + 1 < n ? load(i + 1, to) : 0;
-        // A key that some row of the tile sees and another does not must not reach
-        // the second by 0 * inf: values that are not finite leave the product,
-        // and go to the rows that see them by themselves.
-        const bool mixed = C && kb + STG > all;
-        if (mixed) {
-            char* mine = kt + B + Tile::RW * wave * Tile::ROW + 16 * lane;
-            uint32_t any_odd = 0;
+            for (int x = 0; x < Tile::TILES; ++x) {
+                there |= (uint32_t)in_cache(a, page[x]) << x;
+                if (x == Tile::RW * wave / 16) mine = page[x];
+            }
+            const int kb = k0 + STG * i + (Tile::RW * wave & ~15), rows = rows_in(in_cache(a, mine), kb, any);
+            const int64_t at = row_of(a, mine, head, kb);
+            to += Tile::RW * wave * Tile::ROW;
+            const auto rk = rows_of<HD>(a.K, at, rows), rv = rows_of<HD>(a.V, at, rows);
 #pragma unroll
             for (int j = 0; j < Tile::NL; ++j) {
-                u32x4 x = *reinterpret_cast<const u32x4*>(mine + 1024 * j);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    any_odd |= not_finite2(x[e]);
-                    x[e] = finite2(x[e]);
-                }
-                *reinterpret_cast<u32x4*>(mine + 1024 * j) = x;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lptr_t)(to + 1024 * j), 16, from[j], 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lptr_t)(to + B + 1024 * j), 16, from[j], 0, 0, 0);
             }
-            if (any_odd) odd[i & 1] = i;
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        }
-        if (kb < w_any) wide_block<HD>(w, kt, kb, there, kb + STG > w_all || there != ALL, a.c, hh);
-        if (mixed && odd[i & 1] == i) {
-#pragma unroll 1
-            for (int k = 0; k < min(STG, any - kb); ++k) {
-                if (!(there >> (k / 16) & 1)) continue;
-                const uint16_t* x = a.V + row_of(a, page_of(a, table, kb + k, any), head, kb + k) * HD;
+            return there;
+        };
+        uint32_t there = 0, next = 0;
+        // Stage i from one buffer while the next is loaded into the other: the
+        // __restrict parameters say that they don't overlap (without them the compiler
+        // waits for the loads in flight before the first read).
+        auto step = [&](char* __restrict to, char* __restrict kt, int i) __attribute__((always_inline)) {
+            const int kb = k0 + STG * i;
+            next = i + 1 < n ? load(i + 1, to) : 0;
+            // A key that some row of the tile sees and another does not must not reach
+            // the second by 0 * inf: values that are not finite leave the product,
+            // and go to the rows that see them by themselves.
+            const bool mixed = C && kb + STG > all;
+            if (mixed) {
+                char* mine = kt + B + Tile::RW * wave * Tile::ROW + 16 * lane;
+                uint32_t any_odd = 0;
 #pragma unroll
-                for (int u = 0; u < HD / 32; ++u)
+                for (int j = 0; j < Tile::NL; ++j) {
+                    u32x4 x = *reinterpret_cast<const u32x4*>(mine + 1024 * j);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const uint32_t y = x[32 * u + acc_row(v, hh)];
-                        w.o[u][v] += not_finite(y) && kb + k < w.lim ? bf16_to_f32(y) : 0.0f;
+                    for (int e = 0; e < 4; ++e) {
+                        any_odd |= not_finite2(x[e]);
+                        x[e] = finite2(x[e]);
                     }
+                    *reinterpret_cast<u32x4*>(mine + 1024 * j) = x;
+                }
+                if (any_odd) odd[i & 1] = i;
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
-        }
-        there = next;
-        if (i + 2 < n) look(i + 2);
-    };
-    if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-    if (n > 0) {
-        look(0);
-        there = load(0, lds);
-        if (n > 1) look(1);
-    }
-    turn();
-    // The queries have arrived, too; said in a way that the compiler sees, or it
-    // waits for "them" (and so for the next stage) in every turn of the loop.
-#pragma unroll
-    for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(w.q[i]));
+            if (kb < w_any) wide_block<HD>(w, kt, kb, there, kb + STG > w_all || there != ALL, a.c, hh);
+            if (mixed && odd[i & 1] == i) {
 #pragma unroll 1
-    for (int i = 0; i < n; ++i) {
-        step(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
+                for (int k = 0; k < min(STG, any - kb); ++k) {
+                    if (!(there >> (k / 16) & 1)) continue;
+                    const uint16_t* x = a.V + row_of(a, page_of(a, table, kb + k, any), head, kb + k) * HD;
+#pragma unroll
+                    for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const uint32_t y = x[32 * u + acc_row(v, hh)];
+                            w.o[u][v] += not_finite(y) && kb + k < w.lim ? bf16_to_f32(y) : 0.0f;
+                        }
+                }
+            }
+            there = next;
+            if (i + 2 < n) look(i + 2);
+        };
+        if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+        if (n > 0) {
+            look(0);
+            there = load(0, lds);
+            if (n > 1) look(1);
+        }
         turn();
-    }
+        // The queries have arrived, too; said in a way that the compiler sees, or it
+        // waits for "them" (and so for the next stage) in every turn of the loop.
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) asm volatile("" : "+v"(w.q[i]));
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            step(lds + 2 * B * ((i + 1) & 1), lds + 2 * B * (i & 1), i);
+            turn();
+        }
     };
     if constexpr (ALONG) {
         const int end_p = uniform(a.n_pages > 0 ? a.prefix : 0), w_end = w0 < n_rows ? end_p : 0;

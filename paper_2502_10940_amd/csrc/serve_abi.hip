@@ -77,7 +77,7 @@ int check_rope(const cola_rope_desc* d, bool cache, RopeArgs* a) {
     if (!d || !dtype_ok(d->dtype) || d->reserved != 0) return COLA_ERR_INVALID_ARG;
     if (d->layout != COLA_ROPE_HALF && d->layout != COLA_ROPE_INTERLEAVED) return COLA_ERR_INVALID_ARG;
     if (d->scaling < COLA_ROPE_NONE || d->scaling > COLA_ROPE_WAVELENGTH) return COLA_ERR_INVALID_ARG;
-    if (!(d->base > 1.0) || !isfinite(d->base) || !(d->mscale >= 0.0) || !isfinite(d->mscale)) return COLA_ERR_INVALID_ARG;
+    if (!(d->base > 1.0) || !isfinite(d->base) || !(d->mscale >= 0.0) || !(d->mscale <= 1e30)) return COLA_ERR_INVALID_ARG;
     if (d->scaling != COLA_ROPE_NONE && (!(d->factor >= 1.0) || !isfinite(d->factor))) return COLA_ERR_INVALID_ARG;
     if (d->scaling == COLA_ROPE_YARN || d->scaling == COLA_ROPE_WAVELENGTH)
         if (!(d->low > 0.0) || !(d->high > d->low) || !isfinite(d->high) || d->orig_len < 1) return COLA_ERR_INVALID_ARG;
@@ -152,9 +152,14 @@ int check_attn(const cola_prefix_attn_desc* d, const cola_cache_desc* c, PrefixA
     if (d->n_req < 0 || d->n_req > 65535 || d->T < 0 || d->T > kMaxInt || d->heads_q < 1 || d->heads_q > kMaxPitch)
         return COLA_ERR_BAD_SHAPE;
     if (d->T * d->heads_q > kMaxInt || d->heads_q % c->heads != 0) return COLA_ERR_BAD_SHAPE;
+    // A launch has a tile for every row that a request may have, whether it has or not:
+    // bounds whose empty tiles alone would take seconds are refused.
+    const int64_t pairs = d->n_req * d->heads_q;
+    if (pairs > (int64_t(1) << 28)) return COLA_ERR_BAD_SHAPE;
     if (d->prefix_len < 0 || d->prefix_len > kMaxKeys || d->max_kv < 0 || d->max_kv > kMaxKeys || d->max_new < 1 ||
         d->max_new > kMaxKeys || d->max_pages < 0 || d->max_pages > kMaxInt)
         return COLA_ERR_BAD_SHAPE;
+    if (pairs * (d->max_new < d->T ? d->max_new : d->T) > (int64_t(1) << 36)) return COLA_ERR_BAD_SHAPE;
     PrefixAttnShape s{};
     const int64_t need = (d->max_kv + c->page_size - 1) / c->page_size, w = d->heads_q * c->head_dim;
     s.max_pages = d->max_pages ? d->max_pages : need;

@@ -39,7 +39,7 @@ def test_rope_refusals(fn):
     nan, inf = math.nan, math.inf
     bad = [D(4, 2, 2, 64, dtype=7), D(4, 2, 2, 64, layout=2), D(4, 2, 2, 64, layout=-1), D(4, 2, 2, 64, scaling=5),
            D(4, 2, 2, 64, base=1.0), D(4, 2, 2, 64, base=nan), D(4, 2, 2, 64, base=inf), D(4, 2, 2, 64, mscale=-1.0),
-           D(4, 2, 2, 64, mscale=nan), D(4, 2, 2, 64, scaling="linear", factor=0.5),
+           D(4, 2, 2, 64, mscale=nan), D(4, 2, 2, 64, mscale=1e300), D(4, 2, 2, 64, scaling="linear", factor=0.5),
            D(4, 2, 2, 64, scaling="linear", factor=nan), D(4, 2, 2, 64, scaling="yarn", factor=2.0, low=1.0, high=32.0),
            D(4, 2, 2, 64, scaling="yarn", factor=2.0, orig_len=8, low=2.0, high=2.0),
            D(4, 2, 2, 64, scaling="wavelength", factor=2.0, orig_len=8, low=0.0, high=2.0)]
@@ -117,7 +117,8 @@ def test_attention_refusals():
     for bad in (D(-1, 5, 4, 40, 30), D(65536, 5, 4, 40, 30), D(3, -1, 4, 40, 30), D(3, 5, 0, 40, 30), D(3, 5, 3, 40, 30),
                 D(3, 5, 4, -1, 30), D(3, 5, 4, 40, -1), D(3, 5, 4, 40, 30, 0), D(3, 5, 4, (1 << 30) + 1, 30),
                 D(3, 5, 4, 40, 30, max_pages=1), D(3, 5, 4, 40, 30, ldq=248), D(3, 5, 4, 40, 30, ldq=260),
-                D(3, 5, 4, 40, 30, ldo=255), D(3, 1 << 30, 4, 40, 30), D(3, 5, 4, 40, 30, max_pages=-1)):
+                D(3, 5, 4, 40, 30, ldo=255), D(3, 1 << 30, 4, 40, 30), D(3, 5, 4, 40, 30, max_pages=-1),
+                D(65535, 5, 4098, 40, 30), D(65535, 1 << 17, 16, 40, 30, 1 << 17)):
         refused(cola.ERR_BAD_SHAPE, call, bad, c)
         assert cola.prefix_attn_workspace_bytes(bad, c) == 0
     for s in (-1.0, math.nan, math.inf, 1e-40, 1e38):
@@ -129,10 +130,13 @@ def test_attention_refusals():
     for key in ("ptab", "tab", "kv", "start", "lse"):
         refused(cola.ERR_INVALID_ARG, lambda key=key: call(d, c, **{key: FAKE + 2}))
     refused(cola.ERR_INVALID_ARG, lambda: call(d, c, out=FAKE))      # out over q
-    need = cola.prefix_attn_workspace_bytes(d, c)
+    # a prefix short enough to be read along with the own keys needs no workspace
+    assert cola.prefix_attn_workspace_bytes(d, c) == 0
+    far = D(3, 5, 4, 4000, 30, 2)
+    need = cola.prefix_attn_workspace_bytes(far, c)
     assert need > 0
-    refused(cola.ERR_WORKSPACE, lambda: call(d, c, n=need - 1))
-    refused(cola.ERR_WORKSPACE, lambda: call(d, c, ws=None))
+    refused(cola.ERR_WORKSPACE, lambda: call(far, c, n=need - 1))
+    refused(cola.ERR_WORKSPACE, lambda: call(far, c, ws=None))
     # empty batches enqueue nothing
     for e in (D(0, 5, 4, 40, 30), D(3, 0, 4, 40, 30)):
         assert cola.prefix_attn_workspace_bytes(e, c) == 0
@@ -149,8 +153,8 @@ def test_workspace_sizes_cover_their_parts():
                 n = cola.prefix_attn_workspace_bytes(d, c)
                 row = T * hq * (hd + 2) * 4
                 assert n == 0 or (n >= row and n <= 128 * row + 1024), (hq, T, L, kv, n)
-                if L and kv:
-                    assert n >= 2 * row
+                if L and kv:                # nothing, or a part of each (a short prefix is read along)
+                    assert n >= 2 * row or (n == 0 and L + kv <= 1024)
 
 
 def test_python_checks():
