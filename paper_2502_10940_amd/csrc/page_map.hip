@@ -2,12 +2,14 @@
 // requests' lengths (cola_page_map).
 //
 // Two prefix sums over the requests (new tokens, new pages) and two lookups per
-// row and page.  A few KB of work: bound by latency, so one launch does it all.
-// Every workgroup forms the sums of all requests itself (at most 4096, from L2)
-// and keeps them in LDS; then the workgroups share out the rows, four neighbours
-// to a thread, and the new pages, each finding its request by bisection.  No workgroup waits for another:
-// table entries that are read (pages of older tokens) and written (new pages) are
-// different ones, and new pages are looked up in the free list again.
+// row and page.  A few KB to a few MB of work: bound by latency, so one launch does
+// it all.  Every workgroup forms the sums of all requests itself (at most 4096,
+// from L2) and keeps them in LDS; then the workgroups share out the rows, four
+// neighbours to a thread where they are many, and the new pages, each finding its
+// request by bisection.  No workgroup waits for another: table entries that are
+// read (pages of older tokens) and written (new pages) are different ones, and new
+// pages are looked up in the free list again.  96 requests of one new token 4.5 us
+// (an empty launch takes 3.7); 263423 rows of 1024 requests 7.5 us.
 #include "serve.hpp"
 
 namespace cola {
