@@ -479,13 +479,43 @@ def test_attention_missing_pages(bad):
     b.check()
 
 
+@pytest.mark.parametrize("hd, page, L", [(64, 16, 64), (64, 64, 1100), (128, 16, 1100), (128, 128, 200)])
+def test_attention_missing_pages_under_wide_tiles(hd, page, L):
+    """The same for tiles of 128 rows, whose stages take several pages or lie in one."""
+    b = Batch(18, [70, 40, 130], [300, 40, 333], L, 4, 2, hd, page, pad=1)
+    b.check()
+    b.ptab = b.ptab.copy()
+    b.ptab[0] = -1
+    b.tab[0, 1] = 10 ** 6
+    b.tab[2, -1] = -2 ** 31
+    b.check()
+    b.ptab[:] = -1
+    b.tab[1, :] = 2 ** 31 - 1
+    b.check()
+
+
+def test_attention_of_pages_that_several_requests_name():
+    """A page twice in a table, in two requests' tables and in the prefix's: keys are
+    read where the tables say, as often as they say."""
+    for new in ([1, 1, 1], [3, 9, 2], [60, 50, 33]):
+        for L in (70, 1300):
+            b = Batch(19, new, [90, 90, 64], L, 4, 2, 64, 16, pad=1)
+            b.ptab = b.ptab.copy()
+            b.ptab[2] = b.ptab[1]
+            b.tab[1, :3] = b.tab[0, :3]
+            b.tab[2, 1] = b.tab[2, 0]
+            b.tab[0, 4] = b.ptab[0]
+            b.check()
+
+
 @pytest.mark.parametrize("value", (math.inf, -math.inf, math.nan))
 def test_attention_masked_values_do_not_reach_a_row(value):
     """A later token whose key or value is not finite changes the rows that see it
     and no other."""
     kw = dict(new=[12, 1], kv=[40, 20], L=20, hq=4, hk=2, hd=64, page=16)
     for seed, kw in ((11, kw), (12, dict(kw, hd=128)), (13, dict(kw, new=[40, 1], L=0)), (14, dict(kw, new=[40, 1], hd=128, L=700)),
-                     (15, dict(kw, new=[5, 1])), (16, dict(kw, new=[3, 1], hd=128, L=900))):
+                     (15, dict(kw, new=[5, 1])), (17, dict(kw, new=[40, 1], L=1100)),
+                     (16, dict(kw, new=[3, 1], hd=128, L=900))):
         b = Batch(seed, **kw)
         clean, cl = b.run()
         n = kw["new"][0]
@@ -697,6 +727,36 @@ def test_the_block_s_attention_through_the_cache(shape):
     cola.prefix_attn(ad, c, qr, K, V, None, table, i32([L] * n_seq), i32(np.arange(n_seq + 1) * L), out, None, ws)
     torch.cuda.synchronize()
     assert np.linalg.norm(f64(out) - f64(att)) <= 1e-2 * np.linalg.norm(f64(att))
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed one after the other, each leaves what it leaves alone."""
+    made = []
+    for seed, new, kv in ((20, [1] * 9, [9 * i for i in range(9)]), (21, [30, 5], [200, 90])):
+        b = Batch(seed, new, kv, 1500, 4, 2, 64, 16)
+        made.append((b, b.run()))
+    n = max(cola.prefix_attn_workspace_bytes(*b.desc()) for b, _ in made)
+    assert n > 0
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    graphs = []
+    for b, _ in made:
+        d, c = b.desc()
+        t = [i32(x) for x in (b.ptab, b.tab, b.kv, b.start)]
+        out, lse = torch.zeros_like(b.q), torch.zeros((b.hq, b.T), device=DEV)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cola.prefix_attn(d, c, b.q, b.K, b.V, *t, out, lse, ws)
+        graphs.append((g, out, lse, t))
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1), (1, 0, 1, 0)):
+        for g, out, lse, _ in graphs:
+            out.zero_()
+            lse.zero_()
+        for i in order:
+            graphs[i][0].replay()
+        torch.cuda.synchronize()
+        for (_, out, lse, _), (b, (want, wl)) in zip(graphs, made):
+            assert torch.equal(out, want) and torch.equal(lse, wl)
 
 
 def test_two_streams_at_once():
