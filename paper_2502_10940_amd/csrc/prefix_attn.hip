@@ -1089,6 +1089,7 @@ constexpr int64_t kAlongKeys = 640, kAlongBytes = 40000000;
 // against 31.9.  1000 + 100 keys take 23.0 against 18.2, 512 + 1000 keys 32.1 against
 // 28.8.
 constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
+constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
 int kind_of(int64_t rows) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : WIDE); }
@@ -1135,7 +1136,7 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     // parts' worth of own keys is one: a call without a join (111 requests of up to 538
     // keys, 52 queries of 16 heads over 2: 25.7 us against 42.6; 7 requests of up to 353
     // keys, 29 queries: 7.0 against 9.7).
-    auto parts = [&](int64_t keys, bool one, int* n, int64_t* len) {
+    auto parts = [&](int64_t keys, int64_t chunk, bool one, int* n, int64_t* len) {
         if (keys == 0) {
             *n = 0;
             *len = KB;
@@ -1147,8 +1148,14 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
         *len = ceil_div(ceil_div(keys, k), kRound) * kRound;
         *n = (int)ceil_div(keys, *len);
     };
-    parts(sh.prefix, false, &p.splits_p, &p.chunk_p);
-    parts(sh.max_kv, sh.prefix == 0, &p.splits_s, &p.chunk_s);
+    // Requests differ in length, and the bounds say nothing of it: where several have
+    // tiles of 128 rows, no part of their keys is long enough to be what the others
+    // wait for (16 requests, 128 queries of 20 heads over 4, up to 4000 keys: 67 us
+    // against 94; 8 behind 4096 + 4000 keys, 256 queries: 172 against 209; two requests
+    // 85 against 82, one 299 against 250).
+    const int64_t own = wide && sh.n_req >= 4 && chunk > kWideOwn ? kWideOwn : chunk;
+    parts(sh.prefix, chunk, false, &p.splits_p, &p.chunk_p);
+    parts(sh.max_kv, own, sh.prefix == 0, &p.splits_s, &p.chunk_s);
     const int64_t n = (p.splits_p + p.splits_s) * p.rows;
     p.direct = p.splits_p == 0 && p.splits_s == 1;
     p.ws_bytes = p.direct || n == 0 ? 0 : (size_t)((2 * n + 63) / 64 * 64 + n * sh.hd) * 4;
