@@ -413,7 +413,8 @@ KERNELS = {
     "wide-solo": ([1] * 513, [(5 * i) % 40 for i in range(513)], 650, 8, 8),
     "wide-two": ([20] * 3, [20, 50, 131], 700, 2, 2), "wide-wide": ([50, 40], [50, 333], 700, 2, 2),
     # many parts of the keys, of the requests' own and of the prefix
-    "parts": ([1, 1], [5000, 3], 3000, 2, 1), "parts-own": ([40], [3000], 0, 2, 2), "parts-wide": ([70, 40, 1, 50, 200], [5000, 200, 4100, 3, 1700], 0, 4, 2),
+    "parts": ([1, 1], [5000, 3], 3000, 2, 1), "parts-own": ([40], [3000], 0, 2, 2), "prompt": ([300], [300], 0, 6, 3), "prompt-parts": ([1000], [1100], 0, 2, 1),
+    "prompt-behind": ([500], [530], 1200, 2, 2), "parts-wide": ([70, 40, 1, 50, 200], [5000, 200, 4100, 3, 1700], 0, 4, 2),
     "parts-chunk": ([9, 30], [2000, 30], 2500, 2, 1),
 }
 
