@@ -6,9 +6,10 @@
 // cost 10 us of a forward call and 17 us of a backward call, as much as the
 // kernels of a small layer take; here about 1 us.  Each function takes the
 // arguments of the cola.py function of the same name (with the stream as an
-// integer; the serving calls have the current device before it) and returns the library's status, or None when any argument is not
-// the plain case (a tensor of the expected kind, or None where that is allowed):
-// cola.py then runs its own checks, which raise the error or take the call.
+// integer; the serving calls have the current device before it) and returns the
+// library's status, or None when any argument is not the plain case (a tensor of
+// the expected kind, or None where that is allowed): cola.py then runs its own
+// checks, which raise the error or take the call.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 

@@ -227,6 +227,29 @@ def test_append_past_4_gib():
     assert (np.abs(f64(out) - ref) <= R.attention_bound(ref, w, page)).all()
 
 
+@pytest.mark.parametrize("rows", (1, 20, 64))
+def test_attention_past_4_gib(rows):
+    """Every kind of tile reads pages whose bytes lie past 2^32 of the cache."""
+    hk, hd, page = 2, 64, 64
+    pages = (5 << 29) // (hk * hd * page)            # 2.5 Gi elements of 2 bytes
+    K = torch.empty((pages, hk, page, hd), dtype=torch.bfloat16, device=DEV)
+    V = torch.empty_like(K)
+    last = [pages - 1, pages // 2, 0]                # in the small cache: 0, 1, 2
+    for x, seed in ((K, 1), (V, 2)):
+        for p in last:
+            x[p] = rand(seed + p % 7, (hk, page, hd), "bf16")
+    small = [f64(torch.stack([x[p] for p in last])) for x in (K, V)]
+    hq, kv, L = 4, 2 * page - 5, 60
+    q = rand(3, (rows, hq * hd), "bf16")
+    out, lse = torch.empty_like(q), torch.empty((hq, rows), device=DEV)
+    d, c = cola.prefix_attn_desc(1, rows, hq, L, kv, rows), cola.cache_desc(pages, page, hk, hd)
+    ws = torch.empty(max(1, cola.prefix_attn_workspace_bytes(d, c)), dtype=torch.uint8, device=DEV)
+    cola.prefix_attn(d, c, q, K, V, i32([last[0]]), i32([last[1:]]), i32([kv]), i32([0, rows]), out, lse, ws)
+    ref, rl, w = R.attention(f64(q), *small, hq, [0], L, [[1, 2]], [kv], [0, rows], page)
+    assert (np.abs(f64(out) - ref) <= R.attention_bound(ref, w, L + kv)).all()
+    assert (np.abs(f64(lse) - rl) <= R.lse_bound(rl, L + kv)).all()
+
+
 # ---------------------------------------------------------------------------
 # tables
 # ---------------------------------------------------------------------------
