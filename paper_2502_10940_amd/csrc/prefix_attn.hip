@@ -39,8 +39,8 @@
 // More rows: tiles of 128, bound by the softmax's arithmetic and the matrix
 // products, keys staged in LDS once for all of them (below).  16 chunks of up to
 // 256 tokens, 32 heads of 64, behind 4096 + 1000 tokens (84 GFLOP): 137 us, 620
-// TFLOP/s; the exponentials, maxima and sums of a head of 64 take the vector unit
-// as long as its products take the matrix unit.
+// TFLOP/s; at a head of 64 the exponentials, maxima, sums and conversions take the
+// vector unit 20 cycles a score and wave, the two products the matrix unit 16.
 //
 // Short prefixes: a request's own items read them along (the bytes come from L2),
 // and neither partial rows nor a join are left.
