@@ -495,8 +495,9 @@ int cola_page_map(const cola_page_map_desc* desc, const int32_t* kv_len, const i
  * Request r has its rows (new tokens) in start[r] .. start[r + 1] - 1 (n_req + 1
  * entries that do not fall; start NULL: one row each, row r) and kv_len[r] tokens
  * of its own in the cache, in the pages table[r][..], its new ones the last of
- * them.  Query head h reads key head h / (heads_q / heads).  Row i of n rows sees
- * the whole prefix and its own tokens 0 .. kv_len - n + i:
+ * them.  Query head h reads key head h / (heads_q / heads).  Row i of n = start[r +
+ * 1] - start[r] (those past T counted) sees the whole prefix and its own tokens 0 ..
+ * kv_len - n + i:
  *   out = softmax(scale q K^T over the seen keys) V,   lse = ln sum exp(scale q K^T)
  * (lse fp32 [heads_q][T], or NULL).  A row that sees nothing gets out = 0 and
  * lse = -inf.  Rows of no request (before start[0], from start[n_req] on, past T)

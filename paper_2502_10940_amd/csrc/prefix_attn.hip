@@ -134,21 +134,24 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
     return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
-// Request r, from whatever the arrays hold: its first row and how many (at most
-// max_new), and of its own tokens the index of the first new one and the end.
+// Request r, from whatever the arrays hold: its first row and how many there are (up
+// to T, at most max_new), and of its own tokens the index of the first new one and
+// the end.  Its new tokens are counted past T, too: those that have no row are the
+// last ones of kv_len, and the rows that are there do not see them.
 struct Span {
     int row, n, first, end;
 };
 __device__ __forceinline__ Span span_of(const Args& a, int r) {
     Span s;
-    int64_t all = r < a.T ? 1 : 0;
+    int64_t all = r < a.T ? 1 : 0, here = all;
     s.row = r;
     if (a.start) {
-        const int64_t lo = min(max((int64_t)entry(a.start, r), (int64_t)0), a.T), hi = min((int64_t)entry(a.start, r + 1), a.T);
-        s.row = (int)lo;
+        const int64_t lo = max((int64_t)entry(a.start, r), (int64_t)0), hi = entry(a.start, r + 1);
+        s.row = (int)min(lo, a.T);
         all = max(hi - lo, (int64_t)0);
+        here = max(min(hi, a.T) - lo, (int64_t)0);
     }
-    s.n = (int)min(all, (int64_t)a.max_new);
+    s.n = (int)min(here, (int64_t)a.max_new);
     const int kv = a.max_kv > 0 ? max(entry(a.kv_len, r), 0) : 0;
     s.first = (int)(kv - all);
     s.end = min(kv, a.max_kv);

@@ -818,3 +818,36 @@ def test_timing_classes_count_the_launches(L, launches):
         cola.timing_enable(False)
         cola.timing_reset()
     assert n["pointwise"] == 3 and n["attn_fwd"] == launches and sum(n.values()) == 3 + launches
+
+
+# ---------------------------------------------------------------------------
+# batches with fewer rows than their requests have tokens
+# ---------------------------------------------------------------------------
+
+# (new, kv, L, hq, hk, rows): tiles of 16, 32 and 128 rows, the prefix along and apart
+CUT = {"one": ([2, 3], [9, 40], 0, 2, 2, 3), "one-along": ([2, 5], [9, 40], 30, 2, 1, 4), "one-prefix": ([2, 5], [9, 40], 1300, 2, 1, 5),
+       "two": ([5, 20], [9, 40], 0, 2, 2, 12), "two-prefix": ([5, 20], [9, 40], 1300, 2, 2, 9),
+       "wide": ([30, 90], [60, 300], 0, 4, 2, 75), "wide-along": ([30, 90], [60, 300], 50, 4, 2, 31), "wide-prefix": ([30, 90], [60, 300], 1300, 4, 2, 75),
+       "a-request-past-the-end": ([4, 9, 2], [4, 20, 2], 20, 2, 2, 4)}
+
+
+@pytest.mark.parametrize("hd", (64, 128))
+@pytest.mark.parametrize("name", sorted(CUT))
+def test_attention_of_a_batch_cut_at_its_rows(name, hd):
+    """A request whose last tokens have no row (page_map: "tokens past T have no row"):
+    the rows that are there see what they see in the whole batch, and not the later
+    tokens, which nothing has written to the cache."""
+    new, kv, L, hq, hk, rows = CUT[name]
+    b = Batch(30 + hd, new, kv, L, hq, hk, hd, 16)
+    for r, n in enumerate(new):
+        for i in range(n):
+            if b.start[r] + i >= rows:
+                j = kv[r] - n + i
+                for c in (b.K, b.V):
+                    c[int(b.tab[r, j // 16]), :, j % 16] = math.nan
+    ref, rl, w = b.reference()
+    b.T, b.q = rows, b.q[:rows].contiguous()
+    out, lse = b.run()
+    keys = L + max(kv)
+    assert (np.abs(f64(out) - ref[:rows]) <= R.attention_bound(ref, w, keys)[:rows]).all()
+    assert (np.abs(f64(lse) - rl[:, :rows]) <= R.lse_bound(rl[:, :rows], keys)).all()
