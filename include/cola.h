@@ -401,8 +401,11 @@ typedef enum { COLA_ROPE_HALF = 0, COLA_ROPE_INTERLEAVED = 1 } cola_rope_layout;
  *               between the pairs that make `high` and `low` turns in orig_len
  *               positions: p(t) = rot_dim ln(orig_len / (2 pi t)) / (2 ln base),
  *               w_i = (i - floor p(high)) / (ceil p(low) - floor p(high)), the
- *               ends kept within 0 .. rot_dim/2 - 1 (equal ends: 0.001 apart)
- *               (arXiv 2309.00071); cosine and sine times 1 + 0.1 ln factor
+ *               ends kept within 0 .. rot_dim - 1 (equal ends: 0.001 apart), w_i
+ *               within 0 .. 1; cosine and sine times 1 + 0.1 ln factor.  The method
+ *               is that of arXiv 2309.00071; its text has a ramp linear in the turns
+ *               that a pair makes, models that use it have this one, linear in the
+ *               pair's index
  *   WAVELENGTH  s_i f_i + (1 - s_i) f_i / factor, s_i = (orig_len f_i / (2 pi) -
  *               low) / (high - low) kept within 0 .. 1 */
 typedef enum {

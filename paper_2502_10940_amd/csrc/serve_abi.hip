@@ -46,9 +46,11 @@ void frequencies(const cola_rope_desc& d, RopeArgs* a) {
         auto pair = [&](double turns) {
             return (double)d.rot_dim * log((double)d.orig_len / (two_pi * turns)) / (2.0 * log(base));
         };
-        first = fmin(fmax(floor(pair(d.high)), 0.0), half - 1.0);
-        const double last = fmax(fmin(ceil(pair(d.low)), half - 1.0), 0.0);
-        width = fmax(last - first, 0.001);
+        // The ends may lie past the slowest pair, half - 1, up to rot_dim - 1: the bound
+        // is part of the rule that checkpoints with this scaling are trained under.
+        auto end = [&](double x) { return fmin(fmax(x, 0.0), (double)d.rot_dim - 1.0); };
+        first = end(floor(pair(d.high)));
+        width = fmax(end(ceil(pair(d.low))) - first, 0.001);
     }
     // f_i = base^(-2i/rot): products of one root, in the long double's 64 bits
     const long double root = half > 0 ? powl((long double)base, -1.0L / half) : 1.0L;

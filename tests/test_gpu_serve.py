@@ -851,3 +851,36 @@ def test_attention_of_a_batch_cut_at_its_rows(name, hd):
     keys = L + max(kv)
     assert (np.abs(f64(out) - ref[:rows]) <= R.attention_bound(ref, w, keys)[:rows]).all()
     assert (np.abs(f64(lse) - rl[:, :rows]) <= R.lse_bound(rl[:, :rows], keys)).all()
+
+
+# ---------------------------------------------------------------------------
+# yarn's ramp where its end lies past the slowest pair
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rot, orig_len, base", [(128, 65536, 10000.0), (64, 131072, 10000.0), (64, 1 << 40, 10000.0), (32, 4, 500000.0)])
+def test_yarn_ramp_past_the_slowest_pair(rot, orig_len, base):
+    """The ramp ends at the index, rounded up, at which a pair makes `low` turns.  It may
+    lie past the last pair, up to rot_dim - 1, and the ramp keeps its slope.  An
+    original length in which every pair makes `high` turns leaves them all as they
+    are; one in which none makes a turn divides all but the first."""
+    hd, T, low, high, factor = rot, 9, 1.0, 32.0, 8.0
+    pos = np.array([0, 1, 2, 3, 77, 1000, 4095, 65535, 500000])
+    turns_at = lambda t: rot * math.log(orig_len / (2 * math.pi * t)) / (2 * math.log(base))
+    lo, hi = (min(max(x, 0), rot - 1) for x in (math.floor(turns_at(high)), math.ceil(turns_at(low))))
+    if orig_len == 65536:
+        assert (lo, hi) == (40, 65)
+    f = []
+    for i in range(rot // 2):
+        x = min(max((i - lo) / max(hi - lo, 0.001), 0.0), 1.0)
+        f.append((1 - x) * base ** (-2 * i / rot) + x * base ** (-2 * i / rot) / factor)
+    m = 1 + 0.1 * math.log(factor)
+    q = rand(5, (T, hd), "f32")
+    out = torch.empty_like(q)
+    d = cola.rope_desc(T, 1, 0, hd, rot, "f32", "half", "yarn", base=base, factor=factor, orig_len=orig_len, low=low, high=high)
+    cola.rope_fwd(d, q, None, i32(pos), out, None)
+    x = f64(q)
+    a = pos[:, None] * np.array(f)
+    c, s = m * np.cos(a), m * np.sin(a)
+    u, v = x[:, :rot // 2], x[:, rot // 2:]
+    want = np.concatenate([u * c - v * s, v * c + u * s], 1)
+    assert (np.abs(f64(out) - want) <= R.rope_bound(x, 1, hd, rot, want, "f32", "half", m)).all()
