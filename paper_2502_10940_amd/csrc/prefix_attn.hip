@@ -1101,6 +1101,7 @@ constexpr int64_t kAlongKeys = 640, kAlongBytes = 40000000;
 // 28.8.
 constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
+constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
 int kind_of(int64_t rows) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : WIDE); }
@@ -1140,9 +1141,20 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     // with 512 items, 106 with 768, 116 with 1024; chunks of heads of 64 take 154, 151
     // and 141.
     const int64_t base_p = (int64_t)p.tiles_p * sh.hk, base_s = sh.n_req * p.tiles_s * sh.hk;
-    const int64_t blocks = base_p * ceil_div(sh.prefix, KB) + base_s * ceil_div(sh.max_kv, KB);
-    int64_t chunk = ceil_div(blocks, sh.hd == 128 ? 512 : 1024);
+    const int64_t blocks_p = base_p * ceil_div(sh.prefix, KB), blocks_s = base_s * ceil_div(sh.max_kv, KB);
+    const int64_t items = sh.hd == 128 ? 512 : 1024;
+    int64_t chunk = ceil_div(blocks_p + blocks_s, items);
     if (chunk < 8) chunk = 8;
+    // The prefix's length is known, max_kv only bounds the requests': their keys count
+    // for at most twice the prefix's where its parts are cut, or a bound far above the
+    // lengths would leave it too few to fill the chip (64 requests of up to 2000 keys
+    // behind 32768, 32 heads over 8 of 128, max_kv 32768: 97 us against 640; 200 of up
+    // to 300 behind 4001: 42 against 92).  No shorter than 1024 keys on that account
+    // (200 behind 3000, 16 heads of 64: 28.6 us against 30.2 with 512; 64 behind 8192:
+    // 34.0 against 30.2, and 51 with 2048).
+    int64_t chunk_p = ceil_div(3 * blocks_p, items);
+    if (chunk_p < kPrefixOwn) chunk_p = kPrefixOwn;
+    if (chunk_p > chunk) chunk_p = chunk;
     // As many parts as that gives, of equal length.  Without a prefix, less than two
     // parts' worth of own keys is one: a call without a join (111 requests of up to 538
     // keys, 52 queries of 16 heads over 2: 25.7 us against 42.6; 7 requests of up to 353
@@ -1165,7 +1177,7 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     // against 94; 8 behind 4096 + 4000 keys, 256 queries: 172 against 209; two requests
     // 85 against 82, one 299 against 250).
     const int64_t own = wide && sh.n_req >= 4 && chunk > kWideOwn ? kWideOwn : chunk;
-    parts(sh.prefix, chunk, false, &p.splits_p, &p.chunk_p);
+    parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
     parts(sh.max_kv, own, sh.prefix == 0, &p.splits_s, &p.chunk_s);
     const int64_t n = (p.splits_p + p.splits_s) * p.rows;
     p.direct = p.splits_p == 0 && p.splits_s == 1;

@@ -157,6 +157,21 @@ def test_workspace_sizes_cover_their_parts():
                     assert n >= 2 * row or (n == 0 and L + kv <= 1024)
 
 
+@pytest.mark.parametrize("n_req, prefix, hq, hk, hd", [(64, 32768, 32, 8, 128), (16, 32768, 32, 8, 128), (64, 8192, 32, 8, 128), (32, 16384, 32, 32, 64),
+                                                        (200, 4001, 32, 8, 128), (200, 3000, 16, 16, 64), (3, 100000, 8, 2, 64)])
+def test_the_prefix_keeps_its_parts_whatever_max_kv_bounds(n_req, prefix, hq, hk, hd):
+    """max_kv above the lengths: the prefix still goes out in parts of at most 1024 keys
+    (and what rounding to stages of 64 adds) or in a work item for half of the CUs."""
+    c = cola.cache_desc(10 ** 6, 64, hk, hd)
+    row = n_req * hq * (hd + 2) * 4
+    rows = n_req * hq // hk                             # of a key head, all in one batch
+    tiles = -(-rows // (16 if rows <= 16 else 32 if rows <= 32 else 128))
+    for max_kv in (1 << 15, 1 << 17, 1 << 20):
+        parts = cola.prefix_attn_workspace_bytes(cola.prefix_attn_desc(n_req, n_req, hq, prefix, max_kv), c) // row
+        parts -= 1                                      # at the least one of them is of own keys
+        assert parts * tiles * hk >= 128 or -(-prefix // max(parts, 1)) <= 1024 + 64, (max_kv, parts)
+
+
 def test_python_checks():
     z = lambda *s, dt=BF: torch.zeros(s, dtype=dt)
     d = cola.rope_desc(4, 2, 1, 64)
