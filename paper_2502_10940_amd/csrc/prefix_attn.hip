@@ -1101,6 +1101,7 @@ constexpr int64_t kAlongKeys = 640, kAlongBytes = 40000000;
 // 28.8.
 constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
+constexpr int64_t kWideOwnBytes = 64000000;  // of partial rows, where these parts are more than the chip needs
 constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
@@ -1175,9 +1176,22 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     // tiles of 128 rows, no part of their keys is long enough to be what the others
     // wait for (16 requests, 128 queries of 20 heads over 4, up to 4000 keys: 67 us
     // against 94; 8 behind 4096 + 4000 keys, 256 queries: 172 against 209; two requests
-    // 85 against 82, one 299 against 250).
-    const int64_t own = wide && sh.n_req >= 4 && chunk > kWideOwn ? kWideOwn : chunk;
+    // 85 against 82, one 299 against 250).  Not at any price: max_kv may be a server's
+    // context length, and each part is a row of fp32 for every row of the batch.  So
+    // the partial rows stay within kWideOwnBytes, or there are no more parts than the
+    // chip needs (4 requests of 8192 rows in all, 32 heads over 8 of 128, max_kv
+    // 131072: one part, where 64 would ask for 8.7 GB).  At 32, 64 and 128 MB: 4
+    // requests of up to 16000 keys, 128 queries, max_kv 32768: 165, 105, 112 us; 8
+    // behind 4096 + 4000, max_kv 32768: 134, 134, 183; 16 of up to 4000, max_kv 32768:
+    // 89, 126, 92; 5 of up to 30000, 512 queries: 790, 764, 734.
     parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
+    int64_t own = chunk;
+    if (wide && sh.n_req >= 4 && chunk > kWideOwn) {
+        const int64_t fit = kWideOwnBytes / (p.rows * (sh.hd + 2) * 4) - p.splits_p;
+        own = ceil_div(ceil_div(sh.max_kv, KB), fit < 1 ? 1 : fit);
+        if (own < kWideOwn) own = kWideOwn;
+        if (own > chunk) own = chunk;
+    }
     parts(sh.max_kv, own, sh.prefix == 0, &p.splits_s, &p.chunk_s);
     const int64_t n = (p.splits_p + p.splits_s) * p.rows;
     p.direct = p.splits_p == 0 && p.splits_s == 1;
