@@ -1089,6 +1089,13 @@ constexpr int64_t kSoloItems = 4096;
 // Parts up to which a thread reads all of a row's four elements (2 to 8 parts: the
 // same time as a wave to a row, or less; 3 parts of 70112 rows 13 us against 83).
 constexpr int64_t kJoinFew = 8;
+// Threads of that kind from which on parts don't matter: those that a loose max_kv
+// allows and no request has cost a wave to a row its 64 lanes (16 chunks of up to 256,
+// 32 heads of 64, behind 4096 + 1000 keys, 12 parts allowed and 2 there: 142 us against
+// 213 in all; 16 requests of up to 4000 keys, 21 allowed, 3 there: 67 against 92), and
+// 16 that are there take as long either way (128 requests behind 60000 keys, 32 heads
+// of 128: 156 and 159).
+constexpr int64_t kJoinThreads = 1 << 17;
 // Keys that a request's item takes along at most, and bytes of prefix that all
 // requests read again.  One request of 8 heads of 64 with 200 keys of its own: 5.1
 // us against 8.0 behind 64 keys, 7.4 against 8.1 behind 512, 10.0 against 8.5 behind
@@ -1101,7 +1108,7 @@ constexpr int64_t kAlongKeys = 640, kAlongBytes = 40000000;
 // 28.8.
 constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
-constexpr int64_t kWideOwnBytes = 64000000;  // of partial rows, where these parts are more than the chip needs
+constexpr int64_t kWideOwnBytes = 128000000;  // of partial rows, where these parts are more than the chip needs
 constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
@@ -1180,10 +1187,10 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     // context length, and each part is a row of fp32 for every row of the batch.  So
     // the partial rows stay within kWideOwnBytes, or there are no more parts than the
     // chip needs (4 requests of 8192 rows in all, 32 heads over 8 of 128, max_kv
-    // 131072: one part, where 64 would ask for 8.7 GB).  At 32, 64 and 128 MB: 4
-    // requests of up to 16000 keys, 128 queries, max_kv 32768: 165, 105, 112 us; 8
-    // behind 4096 + 4000, max_kv 32768: 134, 134, 183; 16 of up to 4000, max_kv 32768:
-    // 89, 126, 92; 5 of up to 30000, 512 queries: 790, 764, 734.
+    // 131072: one part, where 64 would ask for 8.7 GB).  At 64, 128 MB and without
+    // bound, max_kv 32768: 16 requests of up to 4000 keys 101, 67, 67 us; 32 of up to
+    // 3000, 16 heads over 4, 138, 105, 133; 5 of up to 30000, 512 queries, 764, 734, 803;
+    // 8 behind 4096 + 4000 135, 146, 164; 5 of up to 3000, 512 queries, 86, 107, 139.
     parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
     int64_t own = chunk;
     if (wide && sh.n_req >= 4 && chunk > kWideOwn) {
@@ -1216,9 +1223,9 @@ hipError_t launch_prefix_join(const PrefixAttnShape& sh, const PrefixAttnPlan& p
     if (p.direct) return hipSuccess;
     const Args a = args_of(sh, p, t);
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
-    // A thread for four elements while its loads of all parts fit a few rounds; a
-    // wave to a row beyond.
-    const bool few = p.splits_p + p.splits_s <= kJoinFew;
+    // A thread for four elements while its loads of all parts fit a few rounds, or where
+    // the rows fill the chip with such threads; a wave to a row beyond.
+    const bool few = p.splits_p + p.splits_s <= kJoinFew || p.rows * (sh.hd / 4) >= kJoinThreads;
     int64_t gx = ceil_div(new_rows * sh.hq, few ? NTHR / (sh.hd / 4) : NW);
     if (gx > 4096) gx = 4096;
     const dim3 grid((unsigned)gx, (unsigned)sh.n_req);

@@ -884,3 +884,24 @@ def test_yarn_ramp_past_the_slowest_pair(rot, orig_len, base):
     u, v = x[:, :rot // 2], x[:, rot // 2:]
     want = np.concatenate([u * c - v * s, v * c + u * s], 1)
     assert (np.abs(f64(out) - want) <= R.rope_bound(x, 1, hd, rot, want, "f32", "half", m)).all()
+
+
+# ---------------------------------------------------------------------------
+# joins of many parts
+# ---------------------------------------------------------------------------
+
+# Rows that fill the chip with a thread for four elements, and fewer: (new, kv, L, hq, hk, max_kv)
+JOINS = {"many-rows": ([1] * 130, [(11 * i) % 70 for i in range(130)], 2600, 32, 1, None),
+         "many-rows-loose-bound": ([33] * 4, [33, 50, 300, 1600], 0, 32, 1, 40000),
+         "few-rows-loose-bound": ([33] * 4, [33, 50, 300, 1600], 0, 4, 1, 40000)}
+
+
+@pytest.mark.parametrize("hd", (64, 128))
+@pytest.mark.parametrize("name", sorted(JOINS))
+def test_attention_joins_of_more_than_eight_parts(name, hd):
+    new, kv, L, hq, hk, max_kv = JOINS[name]
+    b = Batch(40 + hd, new, kv, L, hq * 128 // hd if name.startswith("many") else hq, hk, hd, 64, pad=2, max_kv=max_kv)
+    d, c = b.desc()
+    assert cola.prefix_attn_workspace_bytes(d, c) > 8 * b.T * b.hq * (hd + 2) * 4
+    assert name.startswith("few") == (b.T * b.hq * hd // 4 < 1 << 17)
+    b.check()

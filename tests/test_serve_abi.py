@@ -175,7 +175,7 @@ def test_the_prefix_keeps_its_parts_whatever_max_kv_bounds(n_req, prefix, hq, hk
 @pytest.mark.parametrize("max_kv, max_new", [(131072, 8192), (32768, 2048), (131072, 131072), (1 << 20, 512)])
 def test_workspace_of_a_prompt_call_under_a_server_s_bounds(max_kv, max_new):
     """max_kv and max_new as large as a context: the parts that only even out unequal
-    requests ask for at most 64 MB, and a large batch, which fills the chip, for none."""
+    requests ask for at most 128 MB, and a large batch, which fills the chip, for none."""
     for hq, hk, hd in ((32, 8, 128), (32, 32, 64), (8, 1, 128)):
         c = cola.cache_desc(10 ** 6, 64, hk, hd)
         size = lambda n, T, L: cola.prefix_attn_workspace_bytes(cola.prefix_attn_desc(n, T, hq, L, max_kv, max_new), c)
@@ -185,9 +185,9 @@ def test_workspace_of_a_prompt_call_under_a_server_s_bounds(max_kv, max_new):
                 tiles = n * hk * -(-min(T, max_new) * hq // hk // 128)
                 parts = -(-items // tiles)              # of the own keys, as far as the chip needs them
                 row = T * hq * (hd + 2) * 4
-                assert size(n, T, 0) <= (0 if parts == 1 and row > 32e6 else max(64e6, parts * row) + 256), (n, T)
+                assert size(n, T, 0) <= (0 if parts == 1 and row > 64e6 else max(128e6, parts * row) + 256), (n, T)
                 # behind a prefix: its parts by the same count, none of less than 1024 of its 4000 keys
-                assert size(n, T, 4000) <= max(64e6, (parts + min(4, -(-items // (hk * -(-T * hq // hk // 128))))) * row) + 256, (n, T)
+                assert size(n, T, 4000) <= max(128e6, (parts + min(4, -(-items // (hk * -(-T * hq // hk // 128))))) * row) + 256, (n, T)
 
 
 def test_python_checks():
