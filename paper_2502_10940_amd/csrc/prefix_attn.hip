@@ -1109,6 +1109,7 @@ constexpr int64_t kAlongKeys = 640, kAlongBytes = 40000000;
 constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
 constexpr int64_t kWideOwnBytes = 128000000;  // of partial rows, where these parts are more than the chip needs
+constexpr int64_t kWideOwnTurns = 1 << 16;   // workgroups up to which there are such parts: 1.3 ns for each that has no rows
 constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
@@ -1185,8 +1186,9 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     // against 94; 8 behind 4096 + 4000 keys, 256 queries: 172 against 209; two requests
     // 85 against 82, one 299 against 250).  Not at any price: max_kv may be a server's
     // context length, and each part is a row of fp32 for every row of the batch.  So
-    // the partial rows stay within kWideOwnBytes, or there are no more parts than the
-    // chip needs (4 requests of 8192 rows in all, 32 heads over 8 of 128, max_kv
+    // the partial rows stay within kWideOwnBytes and the workgroups, which a request
+    // has whether it has rows or not, within kWideOwnTurns, or there are no more parts
+    // than the chip needs (4 requests of 8192 rows in all, 32 heads over 8 of 128, max_kv
     // 131072: one part, where 64 would ask for 8.7 GB).  At 64, 128 MB and without
     // bound, max_kv 32768: 16 requests of up to 4000 keys 101, 67, 67 us; 32 of up to
     // 3000, 16 heads over 4, 138, 105, 133; 5 of up to 30000, 512 queries, 764, 734, 803;
@@ -1194,7 +1196,8 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
     int64_t own = chunk;
     if (wide && sh.n_req >= 4 && chunk > kWideOwn) {
-        const int64_t fit = kWideOwnBytes / (p.rows * (sh.hd + 2) * 4) - p.splits_p;
+        int64_t fit = kWideOwnBytes / (p.rows * (sh.hd + 2) * 4) - p.splits_p;
+        if (fit > kWideOwnTurns / base_s) fit = kWideOwnTurns / base_s;
         own = ceil_div(ceil_div(sh.max_kv, KB), fit < 1 ? 1 : fit);
         if (own < kWideOwn) own = kWideOwn;
         if (own > chunk) own = chunk;

@@ -905,3 +905,15 @@ def test_attention_joins_of_more_than_eight_parts(name, hd):
     assert cola.prefix_attn_workspace_bytes(d, c) > 8 * b.T * b.hq * (hd + 2) * 4
     assert name.startswith("few") == (b.T * b.hq * hd // 4 < 1 << 17)
     b.check()
+
+
+@pytest.mark.parametrize("L", (0, 700))
+def test_attention_of_more_turns_than_a_grid(L):
+    """More than 2^23 workgroups go out in several launches: rows of the first request, of
+    one in the middle and of the last, whose turns are past the first launch."""
+    n, heads = 65535, 129
+    new, kv = [0] * n, [0] * n
+    for r, (x, y) in {0: (2, 20), 40000: (1, 5), n - 1: (2, 33)}.items():
+        new[r], kv[r] = x, y
+    assert (n - 1) * heads > 1 << 23
+    Batch(50, new, kv, L, heads, heads, 64, 16).check()

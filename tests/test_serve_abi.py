@@ -190,6 +190,51 @@ def test_workspace_of_a_prompt_call_under_a_server_s_bounds(max_kv, max_new):
                 assert size(n, T, 4000) <= max(128e6, (parts + min(4, -(-items // (hk * -(-T * hq // hk // 128))))) * row) + 256, (n, T)
 
 
+class Shape(ctypes.Structure):           # PrefixAttnShape and PrefixAttnPlan of csrc/serve.hpp
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_req", "T", "max_new", "prefix", "max_kv", "max_pages", "n_pages", "page_size")] + \
+               [(n, ctypes.c_int) for n in ("hq", "hk", "hd")] + [(n, ctypes.c_int64) for n in ("ldq", "ldo")] + [("scale", ctypes.c_double)]
+
+
+class Plan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("kind_p", "kind_s", "tiles_p", "tiles_s", "splits_p", "splits_s")] + \
+               [(n, ctypes.c_int64) for n in ("chunk_p", "chunk_s", "rows")] + [("direct", ctypes.c_bool), ("ws_bytes", ctypes.c_size_t)]
+
+
+def plan(n_req, T, hq, hk, hd, prefix, max_kv, max_new, page=16):
+    """The launch plan of a call, from the library's own function."""
+    f = cola.lib()._ZN4cola16plan_prefix_attnERKNS_15PrefixAttnShapeE
+    f.restype, f.argtypes = Plan, [ctypes.POINTER(Shape)]
+    d, c = cola.prefix_attn_desc(n_req, T, hq, prefix, max_kv, max_new), cola.cache_desc(1 << 20, page, hk, hd)
+    p = f(ctypes.byref(Shape(n_req, T, max_new, prefix, max_kv, -(-max_kv // page), 1 << 20, page, hq, hk, hd, hq * hd, hq * hd, hd ** -0.5)))
+    assert p.rows == T * hq and p.ws_bytes == cola.prefix_attn_workspace_bytes(d, c)
+    return p
+
+
+def turns(p, n_req, hk):
+    """Workgroups of the launch on the requests' own keys (whole rounds of eight)."""
+    units = n_req * hk * p.splits_s
+    return units if p.tiles_s == 1 else -(-units // 8) * 8 * p.tiles_s
+
+
+@pytest.mark.parametrize("hd", (64, 128))
+def test_workgroups_of_every_accepted_bound(hd):
+    """Below 2^30 at the largest bounds that are not refused; and parts that even out
+    requests come to 2^16 workgroups at most."""
+    for n in (1, 3, 4, 100, 4096, 65535):
+        for g, hk in ((1, 1), (8, 1), (3, 3), (4, 64), (1, 512)):
+            for max_new in (1, 2, 5, 17, 33, 129, 4097, 1 << 20):
+                for T in (1, 33, max_new, 1 << 20):
+                    for max_kv in (0, 16, 30000, 1 << 20):
+                        if T * g * hk > 2 ** 31 - 1 or n * g * hk > 2 ** 28 or n * g * hk * min(max_new, T) > 2 ** 36:
+                            continue
+                        p = plan(n, T, g * hk, hk, hd, 0, max_kv, max_new)
+                        base = n * hk * p.tiles_s
+                        assert turns(p, n, hk) < 2 ** 30
+                        # more parts than fill the chip: within the bound
+                        if p.splits_s > 1 and base * (p.splits_s - 1) > 1024:
+                            assert base * p.splits_s <= 2 ** 16, (n, g, hk, max_new, T, max_kv, p.splits_s)
+
+
 def test_python_checks():
     z = lambda *s, dt=BF: torch.zeros(s, dtype=dt)
     d = cola.rope_desc(4, 2, 1, 64)
