@@ -514,7 +514,9 @@ int cola_page_map(const cola_page_map_desc* desc, const int32_t* kv_len, const i
  * multiples of 8; out must not overlap q.  Products and sums are fp32, the
  * probabilities rounded to bf16 for the second product.  ws is scratch of the
  * stated size (0: may be NULL) that holds nothing between calls; calls that share
- * it, replays of captured graphs among them, must be ordered. */
+ * it, replays of captured graphs among them, must be ordered.  The size is each
+ * descriptor's own: smaller bounds may be cut into more parts and need more, so a
+ * workspace for several descriptors has the largest of their sizes. */
 typedef struct {
     int64_t n_req;            /* requests, 0 .. 65535; n_req * heads_q <= 2^28, and n_req * heads_q *
                                  min(max_new, T) <= 2^36 */

@@ -235,6 +235,16 @@ def test_workgroups_of_every_accepted_bound(hd):
                             assert base * p.splits_s <= 2 ** 16, (n, g, hk, max_new, T, max_kv, p.splits_s)
 
 
+def test_workspace_is_each_descriptor_s_own():
+    """A smaller max_kv may need more than a larger one, as the header says; a call with
+    less than its own size is refused."""
+    c = cola.cache_desc(10 ** 4, 16, 4, 64)
+    small, large = (cola.prefix_attn_desc(300, 300, 4, 100000, kv) for kv in (300, 100000))
+    n = [cola.prefix_attn_workspace_bytes(d, c) for d in (small, large)]
+    assert n[0] > n[1] > 0
+    refused(cola.ERR_WORKSPACE, lambda: cola.prefix_attn(small, c, *attn_args(n=n[1]), 0))
+
+
 def test_python_checks():
     z = lambda *s, dt=BF: torch.zeros(s, dtype=dt)
     d = cola.rope_desc(4, 2, 1, 64)
