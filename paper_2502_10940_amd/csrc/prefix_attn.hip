@@ -1052,7 +1052,7 @@ Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAtt
     a.units_p = (int64_t)p.splits_p * sh.hk;
     a.units_s = sh.n_req * p.splits_s * sh.hk;
     a.items_p = turns(a.units_p, p.tiles_p);
-    a.blocks = a.items_p + (p.nt_s == SOLO ? (a.units_s + NW - 1) / NW : turns(a.units_s, p.tiles_s));
+    a.blocks = a.items_p + (p.kind_s == SOLO ? (a.units_s + NW - 1) / NW : turns(a.units_s, p.tiles_s));
     a.direct = p.direct;
     a.c = (float)(sh.scale * (double)kLog2e);
     return a;
@@ -1061,7 +1061,7 @@ Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAtt
 template <int HD>
 hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t s) {
 #define COLA_GO(P, S) \
-    if (p.nt_p == P && p.nt_s == S) prefix_attn_kernel<HD, P, S><<<grid, NTHR, 0, s>>>(a)
+    if (p.kind_p == P && p.kind_s == S) prefix_attn_kernel<HD, P, S><<<grid, NTHR, 0, s>>>(a)
     COLA_GO(ALONG, ONE);
     else COLA_GO(ALONG, TWO);
     else COLA_GO(ALONG, FLAT);
@@ -1123,20 +1123,20 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     const int64_t g = sh.hq / sh.hk;
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
     p.rows = sh.T * sh.hq;
-    p.nt_s = kind_of(new_rows * g);
-    p.nt_p = kind_of(sh.T * g);                              // never below nt_s
-    p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.nt_p));
-    p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.nt_s));
-    if (p.nt_s == ONE && sh.max_new == 1)
-        p.nt_s = sh.n_req * sh.hk >= kSoloItems && (sh.prefix == 0 || p.nt_p == WIDE) ? SOLO : FLAT;
+    p.kind_s = kind_of(new_rows * g);
+    p.kind_p = kind_of(sh.T * g);                              // never below kind_s
+    p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.kind_p));
+    p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.kind_s));
+    if (p.kind_s == ONE && sh.max_new == 1)
+        p.kind_s = sh.n_req * sh.hk >= kSoloItems && (sh.prefix == 0 || p.kind_p == WIDE) ? SOLO : FLAT;
     // without a prefix, the kernel whose prefix part asks for least
-    if (sh.prefix == 0) p.nt_p = p.nt_s == TWO || p.nt_s == WIDE ? p.nt_s : ONE;
+    if (sh.prefix == 0) p.kind_p = p.kind_s == TWO || p.kind_s == WIDE ? p.kind_s : ONE;
     // Short prefixes and few requests: the prefix's bytes come from L2 for each of them,
     // which costs less than a launch that joins.
-    const bool wide = p.nt_s == WIDE;
-    if (sh.prefix > 0 && sh.prefix + sh.max_kv <= (wide ? kWideAlongKeys : kAlongKeys) && p.nt_s != SOLO &&
+    const bool wide = p.kind_s == WIDE;
+    if (sh.prefix > 0 && sh.prefix + sh.max_kv <= (wide ? kWideAlongKeys : kAlongKeys) && p.kind_s != SOLO &&
         sh.n_req * p.tiles_s * sh.prefix * sh.hk * sh.hd * 4 <= (wide ? kWideAlongBytes : kAlongBytes)) {
-        p.nt_p = ALONG;
+        p.kind_p = ALONG;
         p.tiles_p = 1;
         p.chunk_p = kRound;
         p.splits_s = 1;

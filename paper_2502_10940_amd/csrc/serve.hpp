@@ -52,9 +52,9 @@ struct PrefixAttnPtrs {
     float* lse;
     void* ws;
 };
-// Launches of one call, and the floats of its workspace.
+// Launches of one call, and the bytes of its workspace.
 struct PrefixAttnPlan {
-    int nt_p, nt_s;                   // 16-row columns per wave on the prefix and on the requests' own tokens
+    int kind_p, kind_s;               // kinds of tiles on the prefix and on the requests' own tokens (Kind in prefix_attn.hip)
     int tiles_p, tiles_s;             // row tiles: of the batch, of one request
     int splits_p, splits_s;           // parts of the keys
     int64_t chunk_p, chunk_s;         // keys per part

@@ -245,6 +245,28 @@ def test_workspace_is_each_descriptor_s_own():
     refused(cola.ERR_WORKSPACE, lambda: cola.prefix_attn(small, c, *attn_args(n=n[1]), 0))
 
 
+# Kind in csrc/prefix_attn.hip, as the names of the GPU tests' cases have it
+KINDS = {"one": 1, "two": 2, "solo": 3, "flat": 4, "along": 5, "wide": 8}
+
+
+@pytest.mark.parametrize("hd", (64, 128))
+def test_cases_named_after_kernels_run_them(hd):
+    """The GPU tests of each kernel have the batches that the plan gives it."""
+    from test_gpu_serve import KERNELS
+    seen = set()
+    for name, (new, kv, L, hq, hk) in KERNELS.items():
+        p = plan(len(new), sum(new) + 2, hq, hk, hd, L, max(kv), max(new), 16 if hd == 64 else 64)
+        seen.add((p.kind_p, p.kind_s))
+        a, _, b = name.partition("-")
+        if a in KINDS and b.split("-")[0] in KINDS:
+            b = b.split("-")[0]
+            # without a prefix a kernel's first half is not run
+            assert (p.kind_p == KINDS[a] or L == 0) and p.kind_s == KINDS[b], (name, p.kind_p, p.kind_s)
+    every = {("along", x) for x in ("one", "two", "flat", "wide")} | {("one", x) for x in ("one", "flat", "solo")} | \
+            {("two", x) for x in ("one", "flat", "two")} | {("wide", x) for x in ("one", "flat", "solo", "two", "wide")}
+    assert seen == {(KINDS[x], KINDS[y]) for x, y in every}
+
+
 def test_python_checks():
     z = lambda *s, dt=BF: torch.zeros(s, dtype=dt)
     d = cola.rope_desc(4, 2, 1, 64)
