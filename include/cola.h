@@ -436,7 +436,8 @@ typedef struct {
  * [T][ldqo] and k_out [T][ldko].  An output may be its input (same pointer and
  * pitch); any other overlap is not allowed.  The angle is formed in 64 bits
  * from frequencies in 64 bits, whatever the dtype; the products are fp32,
- * rounded once.  Rows may have any alignment and pitch (of the elements' own);
+ * rounded once (cosine and sine to 2^-17 for bf16, by the hardware instructions, and
+ * as the library functions give them for fp32).  Rows may have any alignment and pitch (of the elements' own);
  * large results are fastest where they start on 64 bytes.  The vector width
  * falls with the largest power of two that divides head_dim and rot_dim / 2. */
 int cola_rope_fwd(const cola_rope_desc* desc, const void* q, const void* k, const int32_t* positions,
@@ -477,16 +478,16 @@ int cola_cache_append(const cola_rope_desc* rot, const cola_cache_desc* cache, c
  *   free_next[0]  free_at[0] + the number of pages taken from free_pages
  * free_at[0] (NULL: 0) is the list's first unused entry.  Where the list ends
  * too early (free_next > n_free) the missing entries are -1, and so are slots in
- * such pages and slots of tokens past max_pages * page_size; tokens past T have
- * no row.  free_next must not be free_at: a step that runs twice on the same
- * inputs writes the same values. */
+ * such pages, slots of tokens past max_pages * page_size and slots past 2^31 - 1;
+ * positions past 2^31 - 1 are that; tokens past T have no row.  free_next must not
+ * be free_at: a step that runs twice on the same inputs writes the same values. */
 typedef struct {
     int64_t n_req;            /* 0 .. COLA_PAGE_MAP_MAX_REQ */
-    int64_t T;                /* rows of slots and positions */
+    int64_t T;                /* rows of slots and positions, below 2^31 */
     int64_t page_size;        /* a power of two, 1 .. 4096 */
-    int64_t max_pages;        /* entries per row of the table */
-    int64_t n_free;           /* entries of free_pages */
-    int64_t pos0;             /* position of every request's token 0 (the shared prefix's length) */
+    int64_t max_pages;        /* entries per row of the table; n_req * max_pages < 2^31 */
+    int64_t n_free;           /* entries of free_pages, below 2^31 */
+    int64_t pos0;             /* position of every request's token 0 (the shared prefix's length), below 2^31 */
 } cola_page_map_desc;
 #define COLA_PAGE_MAP_MAX_REQ 4096
 int cola_page_map(const cola_page_map_desc* desc, const int32_t* kv_len, const int32_t* n_new,
