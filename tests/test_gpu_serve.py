@@ -917,3 +917,128 @@ def test_attention_of_more_turns_than_a_grid(L):
         new[r], kv[r] = x, y
     assert (n - 1) * heads > 1 << 23
     Batch(50, new, kv, L, heads, heads, 64, 16).check()
+
+
+# ---------------------------------------------------------------------------
+# paths that only large calls take
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n_req, mean, page, idle, listed", [(1024, 90, 16, 3, None), (300, 310, 128, 1, None), (2, 40000, 64, 0, None),
+                                                             (4096, 23, 1, 2, 50000), (1, 65550, 4096, 0, 7)])
+def test_page_map_of_many_rows(n_req, mean, page, idle, listed):
+    """More than 65536 rows, four to a thread: requests without tokens among the others,
+    rows that no four divide, a free list that ends too early."""
+    rng = np.random.default_rng(n_req)
+    n = rng.integers(0, 2 * mean, n_req) if n_req > 2 else np.full(n_req, mean)
+    n[::7] = 0 if n_req > 2 else mean
+    kv = n + rng.integers(0, 300, n_req)
+    width = int(-(-kv.max() // page)) + 1
+    table = rng.integers(0, 10 ** 5, (n_req, width))
+    free = rng.permutation(4 * 10 ** 5)[:listed]
+    T = int(n.sum()) + idle
+    assert T > 1 << 16
+    for rows in (T, T - 5):
+        check_map(kv, n, free, 2, table, page, rows, 1000)
+
+
+def test_page_map_of_many_rows_at_any_alignment():
+    """Slots and positions that begin at any element."""
+    n_req, each, page = 70, 1000, 32
+    T, width = n_req * each + 2, -(-each // page)
+    kv, free = i32([each] * n_req), torch.randperm(n_req * width, device=DEV).int()
+    d = cola.page_map_desc(n_req, T, page, width, free.numel(), 9)
+    want = None
+    for off in (0, 1, 2, 3):
+        table = torch.full((n_req, width), -1, dtype=torch.int32, device=DEV)
+        start, nxt = torch.zeros(n_req + 1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        slots, pos = (torch.full((T + 8,), -77, dtype=torch.int32, device=DEV) for _ in range(2))
+        cola.page_map(d, kv, kv, free, None, table, start, slots[off:off + T], pos[off:off + T], nxt)
+        for b in (slots, pos):
+            assert (b[:off] == -77).all() and (b[off + T:] == -77).all()
+        got = [table, start, slots[off:off + T].clone(), pos[off:off + T].clone(), nxt]
+        want = want or got
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ref = R.page_map([each] * n_req, [each] * n_req, free.tolist(), 0, np.full((n_req, width), -1), page, T, 9)
+    assert (want[0].cpu().numpy() == ref[0]).all() and want[2].tolist() == ref[2] and want[3].tolist() == ref[3]
+
+
+def test_page_map_past_32_bits():
+    """Slots and positions that an int32 does not hold."""
+    big = 2 ** 31 - 1
+    free = np.array([2 ** 19 - 1, 2 ** 19, 2 ** 30])
+    got = run_map([1, 1, 1], [1, 1, 1], free, 0, np.zeros((3, 1), np.int64), 4096, 3, big)
+    assert got[2] == [(2 ** 19 - 1) * 4096, -1, -1] and got[3] == [big] * 3
+    got = run_map([20], [20], free, 0, np.zeros((1, 1), np.int64), 4096, 20, big - 5)
+    assert got[3] == [min(big - 5 + i, big) for i in range(20)]
+
+
+@pytest.mark.parametrize("layout", ("half", "interleaved"))
+def test_large_fp32_results_are_the_small_ones(layout):
+    """fp32 results of more than 48 MB leave by other stores: the bits of the same rows in
+    parts; and so do rows of the cache."""
+    T, hq, hk, hd, page = 3200, 32, 8, 128, 16
+    q, k, v = (rand(s, (T, h * hd), "f32") for s, h in ((1, hq), (2, hk), (3, hk)))
+    pos = torch.arange(T, dtype=torch.int32, device=DEV) * 7
+    slots = torch.randperm(T, device=DEV).int()
+    c = cola.cache_desc(T // page, page, hk, hd, "f32")
+    assert 4 * T * (hq + hk) * hd > 48e6 > 4 * T // 4 * (hq + 2 * hk) * hd
+    res = []
+    for step in (T, T // 4):
+        r = [torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(q)] + [torch.zeros((T // page, hk, page, hd), device=DEV) for _ in range(2)]
+        for at in range(0, T, step):
+            n = slice(at, at + step)
+            d = cola.rope_desc(step, hq, hk, hd, 96, "f32", layout)
+            cola.rope_fwd(d, q[n], k[n], pos[n], r[0][n], r[1][n])
+            cola.cache_append(d, c, q[n], k[n], v[n], pos[n], slots[n], r[2][n], r[3], r[4])
+        res.append(r)
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+    ref = R.rope(f64(q[-3:]), hq, hd, 96, f64(pos[-3:]), layout)
+    assert (np.abs(f64(res[0][0][-3:]) - ref) <= R.rope_bound(f64(q[-3:]), hq, hd, 96, ref, "f32", layout)).all()
+    assert torch.equal(res[0][0], res[0][2])
+
+
+@pytest.mark.parametrize("hd, hq, new", [(64, 2, 1), (128, 4, 1), (64, 2, 3)])
+def test_attention_joins_of_more_than_64_parts(hd, hq, new):
+    """The wave that joins a row has the statistics of two parts to a lane."""
+    b = Batch(60 + hd, [new], [2300], 20000, hq, 1, hd, 64)
+    d, c = b.desc()
+    assert cola.prefix_attn_workspace_bytes(d, c) > 64 * b.T * b.hq * (hd + 2) * 4
+    b.check()
+
+
+@pytest.mark.parametrize("name", ["one-one", "one-flat", "one-solo", "two-one", "two-flat", "two-two", "wide-one", "wide-flat", "wide-solo", "wide-two",
+                                  "wide-wide", "along-one", "along-two", "along-wide"])
+def test_attention_kernels_past_4_gib(name):
+    """Each kernel on pages whose bytes lie past 2^32 of the cache: the bits that it
+    gives where they lie at its beginning."""
+    new, kv, L, hq, hk = KERNELS[name]
+    hd, page = 64, 16
+    b = Batch(70, new, kv, L, hq, hk, hd, page, pad=1, junk=0.0)
+    want = b.run()
+    n, pages = b.K.shape[0], (5 << 29) // (hk * hd * page)      # 2.5 Gi elements of 2 bytes
+    rng = np.random.default_rng(1)
+    at = pages - 1 - rng.permutation(pages // 8)[:n - 1]         # the last eighth: past 0.8 of the cache
+    at = np.concatenate([[0], at])
+    assert 2 * int(at[1:].min()) * hk * hd * page > 1 << 32
+    K, V = (torch.empty((pages, hk, page, hd), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    for x, y in ((K, b.K), (V, b.V)):
+        x[torch.from_numpy(at).to(DEV)] = y
+    b.K, b.V = K, V
+    b.ptab, b.tab = at[b.ptab], np.where(b.tab >= 0, at[np.maximum(b.tab, 0)], -1)
+    got = b.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("new, L", [([1, 1], 40), ([1, 1], 2000), ([3, 2], 40), ([20, 5], 2000), ([90, 2], 40), ([90, 2], 2000)])
+def test_attention_of_a_cache_without_pages(new, L):
+    """No page is in the cache: every row sees nothing."""
+    T, hq = sum(new) + 1, 2
+    d, c = cola.prefix_attn_desc(len(new), T, hq, L, 64, max(new)), cola.cache_desc(0, 16, 2, 64)
+    q = rand(1, (T, hq * 64), "bf16")
+    out, lse = torch.full_like(q, 7.0), torch.full((hq, T), 7.0, device=DEV)
+    K = torch.empty((0, 2, 16, 64), dtype=torch.bfloat16, device=DEV)
+    n = cola.prefix_attn_workspace_bytes(d, c)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) if n else None
+    cola.prefix_attn(d, c, q, K, K, torch.zeros(-(-L // 16), dtype=torch.int32, device=DEV), torch.zeros((len(new), 4), dtype=torch.int32, device=DEV),
+                     i32([64] * len(new)), i32(np.cumsum([0] + new)), out, lse, ws)
+    assert (out[:-1] == 0).all() and torch.isneginf(lse[:, :-1]).all() and (out[-1] == 7).all() and (lse[:, -1] == 7).all()
