@@ -437,9 +437,10 @@ typedef struct {
  * pitch); any other overlap is not allowed.  The angle is formed in 64 bits
  * from frequencies in 64 bits, whatever the dtype; the products are fp32,
  * rounded once (cosine and sine to 2^-17 for bf16, by the hardware instructions, and
- * as the library functions give them for fp32).  Rows may have any alignment and pitch (of the elements' own);
- * large results are fastest where they start on 64 bytes.  The vector width
- * falls with the largest power of two that divides head_dim and rot_dim / 2. */
+ * as the library functions give them for fp32).  Rows may have any alignment and
+ * pitch (of the elements' own); large results are fastest where they start on 64
+ * bytes.  The vector width falls with the largest power of two that divides
+ * head_dim and rot_dim / 2. */
 int cola_rope_fwd(const cola_rope_desc* desc, const void* q, const void* k, const int32_t* positions,
                   void* q_out, void* k_out, cola_stream_t stream);
 /* The gradient: dq_out, dk_out (pitches ldq, ldk) turned back into dq, dk
@@ -508,9 +509,12 @@ int cola_page_map(const cola_page_map_desc* desc, const int32_t* kv_len, const i
  * are left as they were.  What lies in the cache past a row's seen tokens does
  * not reach it, infinities and NaN included.
  * max_kv and max_new bound kv_len and a request's rows: tokens past max_kv are not
- * seen, rows past max_new are left as they were.  They size the launch and the
- * workspace; lengths below them cost less.  Results depend on the descriptor and
- * the data alone (fixed order of every sum).
+ * seen, rows past max_new are left as they were.  They size the launch, the
+ * workspace and the parts into which keys are split; lengths below them cost less
+ * than the bounds would, but the closer the bounds, the better the split: where few
+ * requests have one token each, a max_kv of 16 times the lengths takes up to 6 times
+ * as long as the lengths themselves.  Results depend on the descriptor and the data
+ * alone (fixed order of every sum).
  * bf16; head_dim 64 or 128; q, out, K, V, ws 16-byte aligned, ldq and ldo
  * multiples of 8; out must not overlap q.  Products and sums are fp32, the
  * probabilities rounded to bf16 for the second product.  ws is scratch of the

@@ -37,10 +37,12 @@
 // 300 own tokens (490 MB): 96 us, 5.1 TB/s of the 6.2 that reading alone reaches.
 //
 // More rows: tiles of 128, bound by the softmax's arithmetic and the matrix
-// products, keys staged in LDS once for all of them (below).  16 chunks of up to
-// 256 tokens, 32 heads of 64, behind 4096 + 1000 tokens (84 GFLOP): 137 us, 620
-// TFLOP/s; at a head of 64 the exponentials, maxima, sums and conversions take the
-// vector unit 20 cycles a score and wave, the two products the matrix unit 16.
+// products one after the other, keys staged in LDS once for all of them (below).  16
+// chunks of up to 256 tokens, 32 heads of 64, behind 4096 + 1000 tokens (84 GFLOP):
+// 138 us, 610 TFLOP/s; at a head of 64 the exponentials, maxima, sums and conversions
+// take the vector unit 20 cycles a score and wave, the two products the matrix unit
+// 16, and with two waves a SIMD neither is busy all the time (56 and 31 % of the
+// launch).
 //
 // Short prefixes: a request's own items read them along (the bytes come from L2),
 // and neither partial rows nor a join are left.
