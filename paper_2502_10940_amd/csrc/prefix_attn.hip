@@ -1094,7 +1094,7 @@ constexpr int64_t kJoinFew = 8;
 // Threads of that kind from which on parts don't matter: those that a loose max_kv
 // allows and no request has cost a wave to a row its 64 lanes (16 chunks of up to 256,
 // 32 heads of 64, behind 4096 + 1000 keys, 12 parts allowed and 2 there: 142 us against
-// 213 in all; 16 requests of up to 4000 keys, 21 allowed, 3 there: 67 against 92), and
+// 218 in all; 16 requests of up to 4000 keys, 21 allowed, 3 there: 68 against 91), and
 // 16 that are there take as long either way (128 requests behind 60000 keys, 32 heads
 // of 128: 156 and 159).
 constexpr int64_t kJoinThreads = 1 << 17;
@@ -1192,9 +1192,9 @@ PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh) {
     // has whether it has rows or not, within kWideOwnTurns, or there are no more parts
     // than the chip needs (4 requests of 8192 rows in all, 32 heads over 8 of 128, max_kv
     // 131072: one part, where 64 would ask for 8.7 GB).  At 64, 128 MB and without
-    // bound, max_kv 32768: 16 requests of up to 4000 keys 101, 67, 67 us; 32 of up to
-    // 3000, 16 heads over 4, 138, 105, 133; 5 of up to 30000, 512 queries, 764, 734, 803;
-    // 8 behind 4096 + 4000 135, 146, 164; 5 of up to 3000, 512 queries, 86, 107, 139.
+    // bound, max_kv 32768: 16 requests of up to 4000 keys 101, 68, 68 us; 32 of up to
+    // 3000, 16 heads over 4, 139, 105, 124; 5 of up to 30000, 512 queries, 803, 756, 832;
+    // 8 behind 4096 + 4000 134, 146, 127; 5 of up to 3000, 512 queries, 88, 111, 125.
     parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
     int64_t own = chunk;
     if (wide && sh.n_req >= 4 && chunk > kWideOwn) {
