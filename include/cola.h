@@ -539,6 +539,134 @@ int cola_prefix_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* c
                      const void* V, const int32_t* prefix_table, const int32_t* table, const int32_t* kv_len,
                      const int32_t* start, void* out, float* lse, void* ws, size_t ws_bytes, cola_stream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Norms of q and k: each head x of D elements becomes, before the rotation,
+ *   n (.) g,   n = x / sqrt(mean(x^2) + eps)
+ * with a gain g of D elements for q's heads and one for k's (dtype of the rows,
+ * element-aligned; NULL: ones).  desc is cola_rope_fwd's: rot_dim, layouts, scalings,
+ * pitches, positions, alignment and overlap as there.  The sum of squares, the norm
+ * and the products are fp32 whatever the dtype, and each result is rounded once.  eps
+ * is positive and finite.  mscale multiplies the rotated elements only.
+ * ------------------------------------------------------------------------ */
+int cola_norm_rope_fwd(const cola_rope_desc* desc, double eps, const void* q, const void* k, const void* g_q,
+                       const void* g_k, const int32_t* positions, void* q_out, void* k_out, cola_stream_t stream);
+
+/* Its gradients, from the forward's inputs (nothing else is kept for them): with dz
+ * the rows of dq_out turned back and w = dz (.) g,
+ *   dg = sum over rows and heads of dz (.) n,   dx = (w - n mean(w (.) n)) / sqrt(mean(x^2) + eps).
+ * desc as in the forward: dq_out and dk_out have the pitches ldqo and ldko; q, dq, k and
+ * dk have ldq and ldk.  dq may be q or dq_out, dk may be k or dk_out (same pointer and
+ * pitch).  dg_q and dg_k (fp32 [head_dim]) are overwritten, zeros for T = 0; NULL: not
+ * wanted.  They are summed in a fixed order.  ws: scratch that holds nothing between
+ * calls, 4-byte aligned. */
+size_t cola_norm_rope_workspace_bytes(const cola_rope_desc* desc);
+int cola_norm_rope_bwd(const cola_rope_desc* desc, double eps, const void* dq_out, const void* dk_out, const void* q,
+                       const void* k, const void* g_q, const void* g_k, const int32_t* positions, void* dq, void* dk,
+                       float* dg_q, float* dg_k, void* ws, size_t ws_bytes, cola_stream_t stream);
+
+/* cola_cache_append with these norms: q normalised and turned into q_out, k normalised
+ * and turned into the cache, v copied into it. */
+int cola_norm_append(const cola_rope_desc* rot, const cola_cache_desc* cache, double eps, const void* q, const void* k,
+                     const void* v, const void* g_q, const void* g_k, const int32_t* positions, const int32_t* slots,
+                     void* q_out, void* K, void* V, cola_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Drafted tokens: a step that verifies a tree of guesses for each request.
+ * A request's new tokens are the nodes of its tree, in rows start[r] .. start[r + 1] -
+ * 1 (as cola_page_map numbers them); node i descends from node parent[i] < i, or from
+ * the request's older tokens alone.  Nodes lie in the cache in the order of their
+ * rows, behind the older tokens; each sees those and its ancestors:
+ *   cola_page_map    start, slots and pages (its positions count rows, not depths)
+ *   cola_tree_map    which nodes a row sees, and positions by depth
+ *   cola_norm_append or cola_cache_append, cola_tree_attn for each layer
+ *   cola_logits_adjust
+ * When the program has chosen a path through the tree, its j-th token belongs into the
+ * slot of node j: a second append of the rows' k and v, with slots[start[r] + j] for
+ * the row of the path's j-th node, -1 for all others and heads_q = 0, puts it there; the
+ * request's length is then its older tokens and the path.
+ * ------------------------------------------------------------------------ */
+#define COLA_TREE_MAX 256             /* nodes of a request's tree */
+
+typedef struct {
+    int64_t n_req;            /* 0 .. 65535 */
+    int64_t T;                /* rows of parent, mask and positions, below 2^31 */
+    int64_t max_new;          /* most nodes of one request, 1 .. COLA_TREE_MAX */
+    int64_t pos0;             /* position of every request's token 0, 0 .. 2^31 - 1 */
+} cola_tree_map_desc;
+
+/* Node i of request r, in row t = start[r] + i (n = start[r + 1] - start[r] nodes, those
+ * that have no row counted), with W = ceil(max_new / 64):
+ *   mask[t][0 .. W-1]  bit j % 64 of word j / 64: node j is i or an ancestor of i
+ *   positions[t]       pos0 + kv_len[r] - n + the number of i's ancestors (kept within
+ *                      0 .. 2^31 - 1)
+ * parent (int32 [T]) counts in the request; a value outside 0 .. i - 1 means none.  Rows
+ * of no request, and nodes from max_new on, get an empty mask and position 0.  start
+ * has n_req + 1 entries that do not fall; NULL: one row each.  mask (8-byte aligned) and
+ * positions must not overlap the inputs. */
+int cola_tree_map(const cola_tree_map_desc* desc, const int32_t* parent, const int32_t* kv_len, const int32_t* start,
+                  uint64_t* mask, int32_t* positions, cola_stream_t stream);
+
+/* cola_prefix_attn for such trees: all as there, but of its request's n new tokens, the
+ * keys kv_len[r] - n + j, a row t sees those whose bit j is set in mask[t][..] (W =
+ * ceil(max_new / 64) words a row, 8-byte aligned; bits from n on count for nothing).  Any
+ * masks are taken: a row may not see itself, or nothing at all (out = 0, lse = -inf).
+ * max_new is at most COLA_TREE_MAX. */
+size_t cola_tree_attn_workspace_bytes(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache);
+int cola_tree_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, const void* q, const void* K,
+                   const void* V, const int32_t* prefix_table, const int32_t* table, const int32_t* kv_len,
+                   const int32_t* start, const uint64_t* mask, void* out, float* lse, void* ws, size_t ws_bytes,
+                   cola_stream_t stream);
+
+/* Rules on the logits of a step, before a token is chosen from each row.  Row t of
+ * request r (rows by start as above; NULL: one row each) has as its history the
+ * request's prompt, history[r][0 .. prompt_len[r] - 1], its answer, history[r][prompt_len[r]
+ * .. hist_len[r] - 1], and the drafted tokens draft[start[r] + j] of the nodes j in its
+ * mask.  With c(v) the number of times that token v is in the answer or among those
+ * drafted tokens:
+ *   x = l(v)
+ *   v in the prompt, or c(v) > 0:   x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *   x -= frequency[r] c(v) + presence[r] [c(v) > 0]
+ *   x += bias of v                  (request r's list: entries bias_start[r] .. bias_start[r + 1] - 1
+ *                                    of bias_token and bias; of one token's entries the last counts)
+ *   v not allowed:                  x = -inf  (bit v % 32 of word v / 32 of allowed[allowed_row[t]];
+ *                                    an allowed_row outside 0 .. n_allowed - 1 allows all; NULL: row t)
+ * in fp32, rounded once.  Each rule is left out where its pointers are NULL, and
+ * penalties where hist_len and draft are.  Tokens outside 0 .. V - 1 count for nothing;
+ * lengths and list bounds are kept within their arrays.  Rows of no request are left as
+ * they were.  NaN stays NaN where it is allowed.  out may be logits (same pointer and
+ * pitch); any other overlap is not allowed. */
+typedef struct {
+    int64_t T;                /* rows, below 2^31 */
+    int64_t V;                /* tokens of the vocabulary, 1 .. 2^22 */
+    int64_t n_req;            /* 0 .. 65535 */
+    int64_t max_hist;         /* entries per row of history, below 2^31 */
+    int64_t max_new;          /* most rows of one request that have drafted tokens, 0 .. COLA_TREE_MAX (0: none) */
+    int64_t n_bias;           /* entries of bias_token and bias, below 2^31 */
+    int64_t n_allowed;        /* rows of allowed, below 2^31 */
+    int64_t ldl, ldo;         /* row pitches of logits and out, 0 = V; at most COLA_MAX_PITCH */
+    int64_t lda;              /* words per row of allowed, 0 = ceil(V / 32) */
+    int32_t dtype;            /* cola_dtype of logits and out */
+    int32_t reserved;         /* 0 */
+} cola_logits_desc;
+
+typedef struct {
+    const int32_t *history;               /* [n_req][max_hist] */
+    const int32_t *prompt_len;            /* [n_req], NULL: 0 */
+    const int32_t *hist_len;              /* [n_req], NULL: no history */
+    const int32_t *draft;                 /* [T], NULL: none */
+    const uint64_t *mask;                 /* [T][ceil(max_new / 64)], with draft */
+    const float *repetition;              /* [n_req], positive; NULL: 1 */
+    const float *presence, *frequency;    /* [n_req]; NULL: 0 */
+    const int32_t *bias_start;            /* [n_req + 1], NULL: no biases */
+    const int32_t *bias_token;            /* [n_bias] */
+    const float *bias;                    /* [n_bias] */
+    const uint32_t *allowed;              /* [n_allowed][lda], NULL: all */
+    const int32_t *allowed_row;           /* [T], NULL: row t */
+} cola_logits_rules;
+
+int cola_logits_adjust(const cola_logits_desc* desc, const cola_logits_rules* rules, const void* logits,
+                       const int32_t* start, void* out, cola_stream_t stream);
+
 /* Tuning options, process-wide (every GPU and thread of the process), read
  * at each call; for tuning, comparisons and tests, not needed for correct
  * results.  Every setting gives results within the stated tolerances;
@@ -589,12 +717,15 @@ typedef enum {
                               layers with dX, which is then not in
                               COLA_KC_BWD_DX                              */
     COLA_KC_ATTN_FWD = 14, /* block: causal attention forward; serving:
-                              cola_prefix_attn, both of its launches      */
+                              cola_prefix_attn and cola_tree_attn, both
+                              launches                                    */
     COLA_KC_ATTN_BWD = 15, /* block: attention backward (dq, then dk dv)  */
-    COLA_KC_NORM = 16,     /* block: RMSNorm forward (+ residual sum)     */
-    COLA_KC_NORM_BWD = 17, /* block: RMSNorm backward (+ residual grad)   */
+    COLA_KC_NORM = 16,     /* block: RMSNorm forward (+ residual sum);
+                              cola_norm_rope_fwd, cola_norm_append        */
+    COLA_KC_NORM_BWD = 17, /* block: RMSNorm backward (+ residual grad);
+                              cola_norm_rope_bwd, both of its launches    */
     COLA_KC_POINTWISE = 18,/* block: gated product, residual add, sigma;
-                              serving: rotation, cache, tables            */
+                              serving: rotation, cache, tables, logits    */
     COLA_KC_COUNT = 19
 } cola_kernel_class;
 

@@ -28,7 +28,7 @@ CXX = "g++"
 
 SOURCES = ["gemm_dispatch.hip", "gemm_stream.hip", "gemm_pp.hip", "gemm_mid.hip", "gemm_skinny.hip", "gemm_f32.hip",
            "cola_abi.hip", "attention.hip", "block_ops.hip", "block_abi.hip", "rope.hip", "page_map.hip",
-           "prefix_attn.hip", "serve_abi.hip"]
+           "prefix_attn.hip", "tree_attn.hip", "norm_rope.hip", "tree_map.hip", "logits.hip", "serve_abi.hip"]
 # Per-source extra flags.  The 256 x 256 kernel's epilogues run over 256
 # accumulators per lane: past the default limit the unroller stops and the
 # accumulators go to scratch memory.
@@ -36,7 +36,8 @@ EXTRA = {"gemm_pp.hip": ["-mllvm", "-pragma-unroll-threshold=500000"],
          # MFMA accumulators in ordinary VGPRs: the attention kernels scale and read
          # theirs with VALU code between MFMAs (no copies to and from AGPRs)
          "attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "prefix_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "prefix_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "tree_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 FLAGS = ["-std=c++17", "-O3", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]

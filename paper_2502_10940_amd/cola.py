@@ -108,6 +108,28 @@ class PrefixAttnDesc(ctypes.Structure):
                                               "ldq", "ldo")] + [("scale", ctypes.c_double)]
 
 
+TREE_MAX = 256                # COLA_TREE_MAX
+
+
+class TreeMapDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_req", "T", "max_new", "pos0")]
+
+
+class LogitsDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "V", "n_req", "max_hist", "max_new", "n_bias", "n_allowed", "ldl", "ldo",
+                                              "lda")] + \
+               [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+# cola_logits_rules
+LOGITS_RULES = ("history", "prompt_len", "hist_len", "draft", "mask", "repetition", "presence", "frequency", "bias_start",
+                "bias_token", "bias", "allowed", "allowed_row")
+
+
+class LogitsRules(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in LOGITS_RULES]
+
+
 _lib = None
 
 _P = ctypes.c_void_p
@@ -154,6 +176,14 @@ EXPORTS = {
     "cola_prefix_attn_workspace_bytes": ([ctypes.POINTER(PrefixAttnDesc), ctypes.POINTER(CacheDesc)], _SZ),
     "cola_prefix_attn": ([ctypes.POINTER(PrefixAttnDesc), ctypes.POINTER(CacheDesc)] + [_P] * 10 + [_SZ, _P],
                          ctypes.c_int),
+    "cola_norm_rope_fwd": ([ctypes.POINTER(RopeDesc), ctypes.c_double] + [_P] * 8, ctypes.c_int),
+    "cola_norm_rope_workspace_bytes": ([ctypes.POINTER(RopeDesc)], _SZ),
+    "cola_norm_rope_bwd": ([ctypes.POINTER(RopeDesc), ctypes.c_double] + [_P] * 12 + [_SZ, _P], ctypes.c_int),
+    "cola_norm_append": ([ctypes.POINTER(RopeDesc), ctypes.POINTER(CacheDesc), ctypes.c_double] + [_P] * 11, ctypes.c_int),
+    "cola_tree_map": ([ctypes.POINTER(TreeMapDesc)] + [_P] * 6, ctypes.c_int),
+    "cola_tree_attn_workspace_bytes": ([ctypes.POINTER(PrefixAttnDesc), ctypes.POINTER(CacheDesc)], _SZ),
+    "cola_tree_attn": ([ctypes.POINTER(PrefixAttnDesc), ctypes.POINTER(CacheDesc)] + [_P] * 11 + [_SZ, _P], ctypes.c_int),
+    "cola_logits_adjust": ([ctypes.POINTER(LogitsDesc), ctypes.POINTER(LogitsRules), _P, _P, _P, _P], ctypes.c_int),
     "cola_set_option": ([ctypes.c_int, ctypes.c_int], ctypes.c_int),
     "cola_get_option": ([ctypes.c_int], ctypes.c_int),
 }
@@ -778,10 +808,7 @@ def _check_pages(c: CacheDesc, K, V):
         _need_flat(name, t, (c.n_pages, c.heads, c.page_size, c.head_dim), _torch_dtype(c.dtype))
 
 
-def cache_append(d: RopeDesc, c: CacheDesc, q, k, v, positions, slots, q_out, K, V, stream=None):
-    """q turned into q_out, k turned and v as it is into the cache at each row's slot."""
-    if _try_here("cache_append", stream, (d, c, q, k, v, positions, slots, q_out, K, V)):
-        return
+def _check_append(d: RopeDesc, c: CacheDesc, q, k, v, positions, slots, q_out, K, V):
     import torch
     if d.dtype in (F32, BF16) and min(d.T, d.heads_q, d.heads_k, d.head_dim, d.ldq, d.ldk, d.ldv, d.ldqo) >= 0:
         dt = _torch_dtype(d.dtype)
@@ -795,6 +822,13 @@ def cache_append(d: RopeDesc, c: CacheDesc, q, k, v, positions, slots, q_out, K,
         if d.T > 0:
             _one_device([("q", q), ("k", k), ("v", v), ("positions", positions), ("slots", slots), ("q_out", q_out),
                          ("K", K), ("V", V)])
+
+
+def cache_append(d: RopeDesc, c: CacheDesc, q, k, v, positions, slots, q_out, K, V, stream=None):
+    """q turned into q_out, k turned and v as it is into the cache at each row's slot."""
+    if _try_here("cache_append", stream, (d, c, q, k, v, positions, slots, q_out, K, V)):
+        return
+    _check_append(d, c, q, k, v, positions, slots, q_out, K, V)
     _check(lib().cola_cache_append(ctypes.byref(d), ctypes.byref(c), _ptr(q), _ptr(k), _ptr(v), _ptr(positions),
                                    _ptr(slots), _ptr(q_out), _ptr(K), _ptr(V), _stream(stream)))
 
@@ -831,13 +865,8 @@ def prefix_attn_workspace_bytes(d: PrefixAttnDesc, c: CacheDesc) -> int:
     return int(lib().cola_prefix_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(c)))
 
 
-def prefix_attn(d: PrefixAttnDesc, c: CacheDesc, q, K, V, prefix_table, table, kv_len, start, out, lse, ws=None,
-                ws_bytes=None, stream=None):
-    """out and lse of a batch whose requests see prefix_len shared tokens and their own (start None: a row each)."""
-    if _try_here("prefix_attn", stream, (d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, ws_bytes)):
-        return
+def _check_attn(d: PrefixAttnDesc, c: CacheDesc, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, mask=None):
     import torch
-    ws_bytes = _ws_bytes(ws, ws_bytes)
     ps = c.page_size
     if min(d.n_req, d.T, d.heads_q, d.prefix_len, d.max_kv, d.max_pages, d.ldq, d.ldo, c.head_dim) >= 0 and ps > 0:
         w = d.heads_q * c.head_dim
@@ -851,9 +880,159 @@ def prefix_attn(d: PrefixAttnDesc, c: CacheDesc, q, K, V, prefix_table, table, k
             _need_flat("kv_len", kv_len, (d.n_req,), torch.int32)
         _need_flat("start", start, (d.n_req + 1,), torch.int32)
         _need_flat("lse", lse, (d.heads_q, d.T), torch.float32)
+        _need_flat("mask", mask, (d.T, -(-d.max_new // 64)), torch.int64)
         if d.T > 0 and d.n_req > 0:
             _one_device([("q", q), ("K", K), ("V", V), ("prefix_table", prefix_table), ("table", table),
-                         ("kv_len", kv_len), ("start", start), ("out", out), ("lse", lse), ("ws", ws)])
+                         ("kv_len", kv_len), ("start", start), ("out", out), ("lse", lse), ("ws", ws), ("mask", mask)])
+
+
+def prefix_attn(d: PrefixAttnDesc, c: CacheDesc, q, K, V, prefix_table, table, kv_len, start, out, lse, ws=None,
+                ws_bytes=None, stream=None):
+    """out and lse of a batch whose requests see prefix_len shared tokens and their own (start None: a row each)."""
+    if _try_here("prefix_attn", stream, (d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, ws_bytes)):
+        return
+    ws_bytes = _ws_bytes(ws, ws_bytes)
+    _check_attn(d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws)
     _check(lib().cola_prefix_attn(ctypes.byref(d), ctypes.byref(c), _ptr(q), _ptr(K), _ptr(V), _ptr(prefix_table),
                                   _ptr(table), _ptr(kv_len), _ptr(start), _ptr(out), _ptr(lse), _ptr(ws), ws_bytes,
                                   _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# norms of q and k (cola_norm_rope_*, cola_norm_append)
+# ---------------------------------------------------------------------------
+
+def _check_gains(d: RopeDesc, g_q, g_k):
+    if d.dtype in (F32, BF16) and d.head_dim >= 0:
+        _need_flat("g_q", g_q, (d.head_dim,), _torch_dtype(d.dtype))
+        _need_flat("g_k", g_k, (d.head_dim,), _torch_dtype(d.dtype))
+        if d.T > 0:
+            _one_device([("g_q", g_q), ("g_k", g_k)])
+
+
+def norm_rope_fwd(d: RopeDesc, q, k, g_q, g_k, positions, q_out, k_out, eps=1e-6, stream=None):
+    """Each head of q and k normalised, scaled by its gain (None: ones) and turned by its row's position."""
+    if _try_here("norm_rope_fwd", stream, (d, q, k, g_q, g_k, positions, q_out, k_out, eps)):
+        return
+    _check_rope(d, q, k, positions, q_out, k_out)
+    _check_gains(d, g_q, g_k)
+    _check(lib().cola_norm_rope_fwd(ctypes.byref(d), eps, _ptr(q), _ptr(k), _ptr(g_q), _ptr(g_k), _ptr(positions),
+                                    _ptr(q_out), _ptr(k_out), _stream(stream)))
+
+
+def norm_rope_workspace_bytes(d: RopeDesc) -> int:
+    return int(lib().cola_norm_rope_workspace_bytes(ctypes.byref(d)))
+
+
+def norm_rope_bwd(d: RopeDesc, dq_out, dk_out, q, k, g_q, g_k, positions, dq, dk, dg_q, dg_k, ws=None, ws_bytes=None,
+                  eps=1e-6, stream=None):
+    """Gradients of norm_rope_fwd (the same descriptor): dq, dk, and the gains' in fp32 (None: not wanted)."""
+    if _try_here("norm_rope_bwd", stream, (d, dq_out, dk_out, q, k, g_q, g_k, positions, dq, dk, dg_q, dg_k, ws, ws_bytes,
+                                           eps)):
+        return
+    import torch
+    ws_bytes = _ws_bytes(ws, ws_bytes)
+    _check_rope(d, q, k, positions, dq_out, dk_out)
+    _check_gains(d, g_q, g_k)
+    if d.dtype in (F32, BF16) and min(d.T, d.heads_q, d.heads_k, d.head_dim, d.ldq, d.ldk) >= 0:
+        for name, t, w, ld in (("dq", dq, d.heads_q * d.head_dim, d.ldq), ("dk", dk, d.heads_k * d.head_dim, d.ldk)):
+            if w > 0:
+                _need_rows(name, t, d.T, w, ld or w, _torch_dtype(d.dtype))
+        _need_flat("dg_q", dg_q, (d.head_dim,), torch.float32)
+        _need_flat("dg_k", dg_k, (d.head_dim,), torch.float32)
+        _one_device([("dg_q", dg_q), ("dg_k", dg_k)])
+        if d.T > 0:
+            _one_device([("dq", dq), ("dk", dk), ("ws", ws)])
+    _check(lib().cola_norm_rope_bwd(ctypes.byref(d), eps, _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(g_q), _ptr(g_k),
+                                    _ptr(positions), _ptr(dq), _ptr(dk), _ptr(dg_q), _ptr(dg_k), _ptr(ws), ws_bytes,
+                                    _stream(stream)))
+
+
+def norm_append(d: RopeDesc, c: CacheDesc, q, k, v, g_q, g_k, positions, slots, q_out, K, V, eps=1e-6, stream=None):
+    """cache_append with the norms: q into q_out, k normalised and turned and v as it is into the cache."""
+    if _try_here("norm_append", stream, (d, c, q, k, v, g_q, g_k, positions, slots, q_out, K, V, eps)):
+        return
+    _check_append(d, c, q, k, v, positions, slots, q_out, K, V)
+    _check_gains(d, g_q, g_k)
+    _check(lib().cola_norm_append(ctypes.byref(d), ctypes.byref(c), eps, _ptr(q), _ptr(k), _ptr(v), _ptr(g_q), _ptr(g_k),
+                                  _ptr(positions), _ptr(slots), _ptr(q_out), _ptr(K), _ptr(V), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# drafted tokens (cola_tree_map, cola_tree_attn) and rules on logits (cola_logits_adjust)
+# ---------------------------------------------------------------------------
+
+def tree_map_desc(n_req, T, max_new, pos0=0):
+    """Descriptor of a step's trees: n_req requests, T rows, at most max_new drafted tokens each."""
+    return TreeMapDesc(n_req, T, max_new, pos0)
+
+
+def tree_map(d: TreeMapDesc, parent, kv_len, start, mask, positions, stream=None):
+    """mask (int64 [T][ceil(max_new / 64)]) and positions of drafted tokens from their parents."""
+    if _try_here("tree_map", stream, (d, parent, kv_len, start, mask, positions)):
+        return
+    import torch
+    if min(d.n_req, d.T, d.max_new) >= 0:
+        for name, t, shape in (("parent", parent, (d.T,)), ("kv_len", kv_len, (d.n_req,)), ("start", start, (d.n_req + 1,)),
+                               ("positions", positions, (d.T,))):
+            _need_flat(name, t, shape, torch.int32)
+        _need_flat("mask", mask, (d.T, -(-d.max_new // 64)), torch.int64)
+        if d.T > 0:
+            _one_device([("parent", parent), ("kv_len", kv_len), ("start", start), ("mask", mask), ("positions", positions)])
+    _check(lib().cola_tree_map(ctypes.byref(d), _ptr(parent), _ptr(kv_len), _ptr(start), _ptr(mask), _ptr(positions),
+                               _stream(stream)))
+
+
+def tree_attn_workspace_bytes(d: PrefixAttnDesc, c: CacheDesc) -> int:
+    return int(lib().cola_tree_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(c)))
+
+
+def tree_attn(d: PrefixAttnDesc, c: CacheDesc, q, K, V, prefix_table, table, kv_len, start, mask, out, lse, ws=None,
+              ws_bytes=None, stream=None):
+    """prefix_attn whose requests' new tokens see each other by mask (tree_map's), not in their order."""
+    if _try_here("tree_attn", stream, (d, c, q, K, V, prefix_table, table, kv_len, start, mask, out, lse, ws, ws_bytes)):
+        return
+    ws_bytes = _ws_bytes(ws, ws_bytes)
+    _check_attn(d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, mask)
+    _check(lib().cola_tree_attn(ctypes.byref(d), ctypes.byref(c), _ptr(q), _ptr(K), _ptr(V), _ptr(prefix_table),
+                                _ptr(table), _ptr(kv_len), _ptr(start), _ptr(mask), _ptr(out), _ptr(lse), _ptr(ws), ws_bytes,
+                                _stream(stream)))
+
+
+def logits_desc(T, V, n_req, max_hist=0, max_new=0, dtype="f32", n_bias=0, n_allowed=0, ldl=0, ldo=0, lda=0):
+    """Descriptor of the rules on T rows of V logits of n_req requests."""
+    return LogitsDesc(T, V, n_req, max_hist, max_new, n_bias, n_allowed, ldl, ldo, lda,
+                      DTYPES[dtype] if isinstance(dtype, str) else int(dtype), 0)
+
+
+def logits_rules(**tensors):
+    """The tensors of cola_logits_rules by their names (those left out: no such rule), in its order."""
+    unknown = set(tensors) - set(LOGITS_RULES)
+    if unknown:
+        raise ValueError(f"no such rule: {', '.join(sorted(unknown))}")
+    return tuple(tensors.get(n) for n in LOGITS_RULES)
+
+
+def logits_adjust(d: LogitsDesc, rules, logits, start, out, stream=None):
+    """out: the rows of logits after penalties, biases and masks (rules: logits_rules); start None: a row a request."""
+    if _try_here("logits_adjust", stream, (d, rules, logits, start, out)):
+        return
+    import torch
+    if len(rules) != len(LOGITS_RULES):
+        raise ValueError(f"rules: {len(rules)} tensors, logits_rules gives {len(LOGITS_RULES)}")
+    u = dict(zip(LOGITS_RULES, rules))
+    if d.dtype in (F32, BF16) and min(d.T, d.V, d.n_req, d.max_hist, d.max_new, d.n_bias, d.n_allowed, d.ldl, d.ldo, d.lda) >= 0:
+        _need_rows("logits", logits, d.T, d.V, d.ldl or d.V, _torch_dtype(d.dtype))
+        _need_rows("out", out, d.T, d.V, d.ldo or d.V, _torch_dtype(d.dtype))
+        n, i32, f32 = d.n_req, torch.int32, torch.float32
+        for name, shape, dt in (("history", (n, d.max_hist), i32), ("prompt_len", (n,), i32), ("hist_len", (n,), i32),
+                                ("draft", (d.T,), i32), ("mask", (d.T, -(-d.max_new // 64)), torch.int64),
+                                ("repetition", (n,), f32), ("presence", (n,), f32), ("frequency", (n,), f32),
+                                ("bias_start", (n + 1,), i32), ("bias_token", (d.n_bias,), i32), ("bias", (d.n_bias,), f32),
+                                ("allowed", (d.n_allowed, d.lda or -(-d.V // 32)), i32), ("allowed_row", (d.T,), i32)):
+            _need_flat(name, u[name], shape, dt)
+        _need_flat("start", start, (n + 1,), i32)
+        if d.T > 0 and n > 0:
+            _one_device([("logits", logits), ("out", out), ("start", start), *u.items()])
+    R = LogitsRules(**{k: _ptr(t) for k, t in u.items()})
+    _check(lib().cola_logits_adjust(ctypes.byref(d), ctypes.byref(R), _ptr(logits), _ptr(start), _ptr(out), _stream(stream)))

@@ -1,5 +1,6 @@
-// serve.hpp -- declarations of the serving path shared by rope.hip, page_map.hip,
-// prefix_attn.hip and serve_abi.hip.  Not part of the public ABI (that is
+// serve.hpp -- declarations of the serving path shared by rope.hip, norm_rope.hip,
+// page_map.hip, tree_map.hip, prefix_attn.hpp, prefix_attn.hip, tree_attn.hip,
+// logits.hip and serve_abi.hip.  Not part of the public ABI (that is
 // include/cola.h).
 #pragma once
 
@@ -30,6 +31,50 @@ struct RopeArgs {
 };
 hipError_t launch_rope(bool bf16, bool cache, RopeArgs& a, hipStream_t s);
 
+// The rotation with each head normalised and scaled before it.  Backward: q and k are
+// the forward's, dqo and dko the gradients' rows, qo and ko what they become (at the
+// pitches ldq, ldk).
+struct NormRopeArgs : RopeArgs {
+    const void *gq, *gk;              // gains [hd], or NULL
+    const void *dqo, *dko;
+    float *dgq, *dgk, *part;          // part: [workgroups][2][hd]
+    float eps, inv_hd;
+    // filled by the launcher: lanes of a head, elements of a vector
+    int group, pv;
+    bool past;
+};
+enum NormKind : int { NORM_FWD = 0, NORM_APPEND = 1, NORM_BWD = 2 };
+// Most workgroups of the backward's first launch, but where one row needs more: four a
+// CU, as many as are there at once.
+constexpr int64_t kParts = 1024;
+size_t norm_rope_parts(bool bf16, NormRopeArgs a);
+hipError_t launch_norm_rope(bool bf16, NormKind kind, NormRopeArgs& a, hipStream_t s);
+hipError_t launch_norm_gain(const NormRopeArgs& a, size_t parts, hipStream_t s);
+
+struct TreeMapArgs {
+    const int32_t *parent, *kv_len, *start;
+    uint64_t* mask;
+    int32_t* positions;
+    int64_t T, pos0;
+    int n_req, max_new, words;
+};
+hipError_t launch_tree_map(const TreeMapArgs& a, hipStream_t s);
+
+struct LogitsArgs {
+    const void* logits;
+    void* out;
+    const int32_t *start, *history, *prompt_len, *hist_len, *draft;
+    const uint64_t* mask;
+    const float *repetition, *presence, *frequency;
+    const int32_t *bias_start, *bias_token;
+    const float* bias;
+    const uint32_t* allowed;
+    const int32_t* allowed_row;
+    int64_t T, V, ldl, ldo, lda, max_hist, n_bias, n_allowed;
+    int n_req, max_new, words;
+};
+hipError_t launch_logits(bool bf16, const LogitsArgs& a, hipStream_t s);
+
 struct PageMapArgs {
     const int32_t *kv_len, *n_new, *free_pages, *free_at;
     int32_t *table, *start, *slots, *positions, *free_next;
@@ -51,10 +96,11 @@ struct PrefixAttnPtrs {
     uint16_t* out;
     float* lse;
     void* ws;
+    const uint64_t* mask;             // trees: [T][words of max_new bits]; NULL: new tokens see each other in order
 };
 // Launches of one call, and the bytes of its workspace.
 struct PrefixAttnPlan {
-    int kind_p, kind_s;               // kinds of tiles on the prefix and on the requests' own tokens (Kind in prefix_attn.hip)
+    int kind_p, kind_s;               // kinds of tiles on the prefix and on the requests' own tokens (Kind in prefix_attn.hpp)
     int tiles_p, tiles_s;             // row tiles: of the batch, of one request
     int splits_p, splits_s;           // parts of the keys
     int64_t chunk_p, chunk_s;         // keys per part
@@ -63,6 +109,9 @@ struct PrefixAttnPlan {
     size_t ws_bytes;
 };
 PrefixAttnPlan plan_prefix_attn(const PrefixAttnShape& sh);
+PrefixAttnPlan plan_tree_attn(const PrefixAttnShape& sh);
+// One launch of the kernels for trees; args: their arguments (Args in prefix_attn.hpp).
+hipError_t start_tree_attn(int hd, const PrefixAttnPlan& p, const void* args, unsigned grid, hipStream_t s);
 hipError_t launch_prefix_attn(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAttnPtrs& t, hipStream_t s);
 hipError_t launch_prefix_join(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAttnPtrs& t, hipStream_t s);
 

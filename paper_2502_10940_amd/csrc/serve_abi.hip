@@ -1,7 +1,9 @@
 // serve_abi.hip -- the serving entry points of libcola.so (include/cola.h):
-// cola_rope_fwd, cola_rope_bwd, cola_cache_append, cola_page_map and
-// cola_prefix_attn.  Argument checks, frequencies and launches; the kernels are in
-// rope.hip, page_map.hip and prefix_attn.hip.
+// cola_rope_fwd, cola_rope_bwd, cola_cache_append, cola_page_map, cola_prefix_attn,
+// cola_norm_rope_fwd, cola_norm_rope_bwd, cola_norm_append, cola_tree_map,
+// cola_tree_attn and cola_logits_adjust.  Argument checks, frequencies and launches; the
+// kernels are in rope.hip, page_map.hip, prefix_attn.hip, norm_rope.hip, tree_map.hip,
+// tree_attn.hip and logits.hip.
 #include <math.h>
 
 #include "block.hpp"
@@ -26,6 +28,7 @@ int guarded(F&& f) {
 int chk(hipError_t e, const char* where) { return e == hipSuccess ? COLA_OK : set_hip_error(e, where); }
 
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool al8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 bool al4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool dtype_ok(int32_t t) { return t == COLA_F32 || t == COLA_BF16; }
 bool aligned(const void* p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == COLA_F32 ? 3u : 1u)) == 0; }
@@ -144,8 +147,54 @@ int rope(const cola_rope_desc* d, const void* q, const void* k, const int32_t* p
     });
 }
 
+// ---- rows into the cache ----
+int check_append(const cola_rope_desc* rot, const cola_cache_desc* cache) {
+    const int st = check_cache(cache);
+    if (st != COLA_OK) return st;
+    if (rot->heads_k != cache->heads || rot->head_dim != cache->head_dim) return COLA_ERR_BAD_SHAPE;
+    return rot->dtype != cache->dtype ? COLA_ERR_INVALID_ARG : COLA_OK;
+}
+
+// The pointers of an append, checked, and its frequencies (T > 0).
+int take_append(const cola_rope_desc* rot, const cola_cache_desc* cache, const void* q, const void* k, const void* v,
+                const int32_t* positions, const int32_t* slots, void* q_out, void* K, void* V, RopeArgs* a) {
+    if ((a->hq > 0 && (!q || !q_out)) || !k || !v || !slots) return COLA_ERR_INVALID_ARG;
+    if (cache->n_pages > 0 && (!K || !V || K == V)) return COLA_ERR_INVALID_ARG;
+    for (const void* p : {q, k, v, (const void*)q_out})
+        if (!aligned(p, rot->dtype)) return COLA_ERR_INVALID_ARG;
+    if (!al4(positions) || !al4(slots) || !al16(K) || !al16(V)) return COLA_ERR_INVALID_ARG;
+    if (a->hq > 0 && !in_place_ok(q, a->ldq, q_out, a->ldqo)) return COLA_ERR_INVALID_ARG;
+    a->q = q; a->k = k; a->v = v; a->qo = q_out; a->K = K; a->V = V; a->pos = positions; a->slots = slots;
+    a->lg_page = log2_of(cache->page_size);
+    a->n_slots = cache->n_pages * cache->page_size;
+    a->sign = 1.0f;
+    frequencies(*rot, a);
+    return COLA_OK;
+}
+
+// ---- norms ----
+int check_norm(const cola_rope_desc* d, bool cache, double eps, const void* g_q, const void* g_k, NormRopeArgs* a) {
+    const int st = check_rope(d, cache, a);
+    if (st != COLA_OK) return st;
+    const float e = (float)eps;
+    if (!(e > 0.0f) || !isfinite(e)) return COLA_ERR_INVALID_ARG;
+    if (!aligned(g_q, d->dtype) || !aligned(g_k, d->dtype)) return COLA_ERR_INVALID_ARG;
+    a->gq = g_q; a->gk = g_k;
+    a->eps = e;
+    a->inv_hd = 1.0f / (float)a->hd;
+    return COLA_OK;
+}
+
+// Rows that are there where there are heads, aligned to their elements.
+bool rows_ok(const cola_rope_desc* d, const RopeArgs& a, const void* q, const void* k, const void* qo, const void* ko) {
+    if ((a.hq > 0 && (!q || !qo)) || (a.hk > 0 && (!k || !ko))) return false;
+    for (const void* p : {q, k, qo, ko})
+        if (!aligned(p, d->dtype)) return false;
+    return true;
+}
+
 // ---- attention ----
-int check_attn(const cola_prefix_attn_desc* d, const cola_cache_desc* c, PrefixAttnShape* out) {
+int check_attn(const cola_prefix_attn_desc* d, const cola_cache_desc* c, bool tree, PrefixAttnShape* out) {
     const int st = check_cache(c);
     if (st != COLA_OK) return st;
     if (!d) return COLA_ERR_INVALID_ARG;
@@ -161,7 +210,7 @@ int check_attn(const cola_prefix_attn_desc* d, const cola_cache_desc* c, PrefixA
     const int64_t pairs = d->n_req * d->heads_q;
     if (pairs > (int64_t(1) << 28)) return COLA_ERR_BAD_SHAPE;
     if (d->prefix_len < 0 || d->prefix_len > kMaxKeys || d->max_kv < 0 || d->max_kv > kMaxKeys || d->max_new < 1 ||
-        d->max_new > kMaxKeys || d->max_pages < 0 || d->max_pages > kMaxInt)
+        d->max_new > (tree ? COLA_TREE_MAX : kMaxKeys) || d->max_pages < 0 || d->max_pages > kMaxInt)
         return COLA_ERR_BAD_SHAPE;
     if (pairs * (d->max_new < d->T ? d->max_new : d->T) > (int64_t(1) << 36)) return COLA_ERR_BAD_SHAPE;
     PrefixAttnShape s{};
@@ -180,6 +229,54 @@ int check_attn(const cola_prefix_attn_desc* d, const cola_cache_desc* c, PrefixA
     s.hq = (int)d->heads_q; s.hk = (int)c->heads; s.hd = (int)c->head_dim;
     *out = s;
     return COLA_OK;
+}
+
+size_t attn_workspace(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, bool tree) {
+    PrefixAttnShape sh;
+    if (check_attn(desc, cache, tree, &sh) != COLA_OK || sh.n_req == 0 || sh.T == 0) return 0;
+    return (tree ? plan_tree_attn(sh) : plan_prefix_attn(sh)).ws_bytes;
+}
+
+// cola_prefix_attn, or cola_tree_attn.
+int attend(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, const void* q, const void* K, const void* V,
+           const int32_t* prefix_table, const int32_t* table, const int32_t* kv_len, const int32_t* start, bool tree,
+           const uint64_t* mask, void* out, float* lse, void* ws, size_t ws_bytes, cola_stream_t stream) {
+    return guarded([&]() -> int {
+        PrefixAttnShape sh;
+        const int st = check_attn(desc, cache, tree, &sh);
+        if (st != COLA_OK) return st;
+        if (sh.n_req == 0 || sh.T == 0) return COLA_OK;
+        if (!q || !out || q == out) return COLA_ERR_INVALID_ARG;
+        if (sh.n_pages > 0 && (!K || !V)) return COLA_ERR_INVALID_ARG;
+        if ((sh.prefix > 0 && !prefix_table) || (sh.max_kv > 0 && (!table || !kv_len))) return COLA_ERR_INVALID_ARG;
+        for (const void* p : {q, K, V, (const void*)out, (const void*)ws})
+            if (!al16(p)) return COLA_ERR_INVALID_ARG;
+        for (const void* p : {(const void*)prefix_table, (const void*)table, (const void*)kv_len, (const void*)start,
+                              (const void*)lse})
+            if (!al4(p)) return COLA_ERR_INVALID_ARG;
+        if (tree && (!mask || !al8(mask))) return COLA_ERR_INVALID_ARG;
+        const PrefixAttnPlan p = tree ? plan_tree_attn(sh) : plan_prefix_attn(sh);
+        if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return COLA_ERR_WORKSPACE;
+        PrefixAttnPtrs t{};
+        t.q = static_cast<const uint16_t*>(q);
+        t.K = static_cast<const uint16_t*>(K);
+        t.V = static_cast<const uint16_t*>(V);
+        t.prefix_table = prefix_table; t.table = table; t.kv_len = kv_len; t.start = start;
+        t.out = static_cast<uint16_t*>(out);
+        t.lse = lse;
+        t.ws = ws;
+        t.mask = mask;
+        hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+        // work for the bounds: the lengths themselves are in GPU memory
+        const double rows = (double)p.rows, keys = (double)sh.prefix + (double)sh.max_kv;
+        const double bytes = 4.0 * rows * sh.hd + 4.0 * ((double)sh.prefix + (double)sh.n_req * sh.max_kv) * sh.hk * sh.hd;
+        const int e = chk(timed_fn(COLA_KC_ATTN_FWD, 4.0 * rows * keys * sh.hd, bytes, s,
+                                   [&] { return launch_prefix_attn(sh, p, t, s); }), tree ? "tree_attn" : "prefix_attn");
+        if (e != COLA_OK || p.direct) return e;
+        const double parts = (double)p.splits_p + p.splits_s;
+        return chk(timed_fn(COLA_KC_ATTN_FWD, 2.0 * rows * sh.hd * parts, rows * sh.hd * (4.0 * parts + 2.0), s,
+                            [&] { return launch_prefix_join(sh, p, t, s); }), "prefix_join");
+    });
 }
 
 }  // namespace
@@ -202,22 +299,11 @@ int cola_cache_append(const cola_rope_desc* rot, const cola_cache_desc* cache, c
     return guarded([&]() -> int {
         RopeArgs a{};
         int st = check_rope(rot, true, &a);
-        if (st == COLA_OK) st = check_cache(cache);
+        if (st == COLA_OK) st = check_append(rot, cache);
         if (st != COLA_OK) return st;
-        if (rot->heads_k != cache->heads || rot->head_dim != cache->head_dim) return COLA_ERR_BAD_SHAPE;
-        if (rot->dtype != cache->dtype) return COLA_ERR_INVALID_ARG;
         if (a.T == 0) return COLA_OK;
-        if ((a.hq > 0 && (!q || !q_out)) || !k || !v || !slots) return COLA_ERR_INVALID_ARG;
-        if (cache->n_pages > 0 && (!K || !V || K == V)) return COLA_ERR_INVALID_ARG;
-        for (const void* p : {q, k, v, (const void*)q_out})
-            if (!aligned(p, rot->dtype)) return COLA_ERR_INVALID_ARG;
-        if (!al4(positions) || !al4(slots) || !al16(K) || !al16(V)) return COLA_ERR_INVALID_ARG;
-        if (a.hq > 0 && !in_place_ok(q, a.ldq, q_out, a.ldqo)) return COLA_ERR_INVALID_ARG;
-        a.q = q; a.k = k; a.v = v; a.qo = q_out; a.K = K; a.V = V; a.pos = positions; a.slots = slots;
-        a.lg_page = log2_of(cache->page_size);
-        a.n_slots = cache->n_pages * cache->page_size;
-        a.sign = 1.0f;
-        frequencies(*rot, &a);
+        st = take_append(rot, cache, q, k, v, positions, slots, q_out, K, V, &a);
+        if (st != COLA_OK) return st;
         const double es = rot->dtype == COLA_BF16 ? 2.0 : 4.0, n = (double)a.T * a.hd;
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
         return chk(timed_fn(COLA_KC_POINTWISE, 3.0 * (double)a.T * (a.hq + a.hk) * a.rot, 2.0 * es * n * (a.hq + 2 * a.hk), s,
@@ -253,47 +339,170 @@ int cola_page_map(const cola_page_map_desc* d, const int32_t* kv_len, const int3
 }
 
 size_t cola_prefix_attn_workspace_bytes(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache) {
-    PrefixAttnShape sh;
-    if (check_attn(desc, cache, &sh) != COLA_OK || sh.n_req == 0 || sh.T == 0) return 0;
-    return plan_prefix_attn(sh).ws_bytes;
+    return attn_workspace(desc, cache, false);
 }
 
 int cola_prefix_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, const void* q, const void* K,
                      const void* V, const int32_t* prefix_table, const int32_t* table, const int32_t* kv_len,
                      const int32_t* start, void* out, float* lse, void* ws, size_t ws_bytes, cola_stream_t stream) {
+    return attend(desc, cache, q, K, V, prefix_table, table, kv_len, start, false, nullptr, out, lse, ws, ws_bytes, stream);
+}
+
+size_t cola_tree_attn_workspace_bytes(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache) {
+    return attn_workspace(desc, cache, true);
+}
+
+int cola_tree_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, const void* q, const void* K,
+                   const void* V, const int32_t* prefix_table, const int32_t* table, const int32_t* kv_len,
+                   const int32_t* start, const uint64_t* mask, void* out, float* lse, void* ws, size_t ws_bytes,
+                   cola_stream_t stream) {
+    return attend(desc, cache, q, K, V, prefix_table, table, kv_len, start, true, mask, out, lse, ws, ws_bytes, stream);
+}
+
+int cola_norm_rope_fwd(const cola_rope_desc* desc, double eps, const void* q, const void* k, const void* g_q,
+                       const void* g_k, const int32_t* positions, void* q_out, void* k_out, cola_stream_t stream) {
     return guarded([&]() -> int {
-        PrefixAttnShape sh;
-        const int st = check_attn(desc, cache, &sh);
+        NormRopeArgs a{};
+        const int st = check_norm(desc, false, eps, g_q, g_k, &a);
         if (st != COLA_OK) return st;
-        if (sh.n_req == 0 || sh.T == 0) return COLA_OK;
-        if (!q || !out || q == out) return COLA_ERR_INVALID_ARG;
-        if (sh.n_pages > 0 && (!K || !V)) return COLA_ERR_INVALID_ARG;
-        if ((sh.prefix > 0 && !prefix_table) || (sh.max_kv > 0 && (!table || !kv_len))) return COLA_ERR_INVALID_ARG;
-        for (const void* p : {q, K, V, (const void*)out, (const void*)ws})
-            if (!al16(p)) return COLA_ERR_INVALID_ARG;
-        for (const void* p : {(const void*)prefix_table, (const void*)table, (const void*)kv_len, (const void*)start,
-                              (const void*)lse})
-            if (!al4(p)) return COLA_ERR_INVALID_ARG;
-        const PrefixAttnPlan p = plan_prefix_attn(sh);
-        if (p.ws_bytes > 0 && (!ws || ws_bytes < p.ws_bytes)) return COLA_ERR_WORKSPACE;
-        PrefixAttnPtrs t{};
-        t.q = static_cast<const uint16_t*>(q);
-        t.K = static_cast<const uint16_t*>(K);
-        t.V = static_cast<const uint16_t*>(V);
-        t.prefix_table = prefix_table; t.table = table; t.kv_len = kv_len; t.start = start;
-        t.out = static_cast<uint16_t*>(out);
-        t.lse = lse;
-        t.ws = ws;
+        if (a.T == 0) return COLA_OK;
+        if (!rows_ok(desc, a, q, k, q_out, k_out) || !al4(positions)) return COLA_ERR_INVALID_ARG;
+        if ((a.hq > 0 && !in_place_ok(q, a.ldq, q_out, a.ldqo)) || (a.hk > 0 && !in_place_ok(k, a.ldk, k_out, a.ldko)))
+            return COLA_ERR_INVALID_ARG;
+        a.q = q; a.k = k; a.qo = q_out; a.ko = k_out; a.pos = positions;
+        a.sign = 1.0f;
+        frequencies(*desc, &a);
+        const double es = desc->dtype == COLA_BF16 ? 2.0 : 4.0, n = (double)a.T * (a.hq + a.hk) * a.hd;
         hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-        // work for the bounds: the lengths themselves are in GPU memory
-        const double rows = (double)p.rows, keys = (double)sh.prefix + (double)sh.max_kv;
-        const double bytes = 4.0 * rows * sh.hd + 4.0 * ((double)sh.prefix + (double)sh.n_req * sh.max_kv) * sh.hk * sh.hd;
-        const int e = chk(timed_fn(COLA_KC_ATTN_FWD, 4.0 * rows * keys * sh.hd, bytes, s,
-                                   [&] { return launch_prefix_attn(sh, p, t, s); }), "prefix_attn");
-        if (e != COLA_OK || p.direct) return e;
-        const double parts = (double)p.splits_p + p.splits_s;
-        return chk(timed_fn(COLA_KC_ATTN_FWD, 2.0 * rows * sh.hd * parts, rows * sh.hd * (4.0 * parts + 2.0), s,
-                            [&] { return launch_prefix_join(sh, p, t, s); }), "prefix_join");
+        return chk(timed_fn(COLA_KC_NORM, 7.0 * n, 2.0 * es * n, s,
+                            [&] { return launch_norm_rope(desc->dtype == COLA_BF16, NORM_FWD, a, s); }), "norm_rope");
+    });
+}
+
+size_t cola_norm_rope_workspace_bytes(const cola_rope_desc* desc) {
+    NormRopeArgs a{};
+    if (check_norm(desc, false, 1.0, nullptr, nullptr, &a) != COLA_OK || a.T == 0) return 0;
+    return norm_rope_parts(desc->dtype == COLA_BF16, a) * 8 * (size_t)a.hd;
+}
+
+int cola_norm_rope_bwd(const cola_rope_desc* desc, double eps, const void* dq_out, const void* dk_out, const void* q,
+                       const void* k, const void* g_q, const void* g_k, const int32_t* positions, void* dq, void* dk,
+                       float* dg_q, float* dg_k, void* ws, size_t ws_bytes, cola_stream_t stream) {
+    return guarded([&]() -> int {
+        NormRopeArgs a{};
+        const int st = check_norm(desc, false, eps, g_q, g_k, &a);
+        if (st != COLA_OK) return st;
+        if (!al4(dg_q) || !al4(dg_k) || !al4(positions) || !al4(ws) || (dg_q && dg_q == dg_k)) return COLA_ERR_INVALID_ARG;
+        if ((a.hq == 0 && dg_q) || (a.hk == 0 && dg_k)) return COLA_ERR_INVALID_ARG;
+        const bool bf16 = desc->dtype == COLA_BF16;
+        hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+        if (a.T == 0) {
+            for (float* g : {dg_q, dg_k}) {
+                if (!g) continue;
+                const int e = chk(timed_fn(COLA_KC_FILL, 0.0, 4.0 * a.hd, s, [&] { return launch_fill_zero(g, a.hd, s); }), "norm_fill");
+                if (e != COLA_OK) return e;
+            }
+            return COLA_OK;
+        }
+        if (!rows_ok(desc, a, q, k, dq, dk) || !rows_ok(desc, a, dq_out, dk_out, dq, dk)) return COLA_ERR_INVALID_ARG;
+        // dq and dk have the pitches of q and k
+        if ((a.hq > 0 && !in_place_ok(dq_out, a.ldqo, dq, a.ldq)) || (a.hk > 0 && !in_place_ok(dk_out, a.ldko, dk, a.ldk)))
+            return COLA_ERR_INVALID_ARG;
+        const size_t parts = norm_rope_parts(bf16, a);
+        if (!ws || ws_bytes < parts * 8 * (size_t)a.hd) return COLA_ERR_WORKSPACE;
+        a.q = q; a.k = k; a.dqo = dq_out; a.dko = dk_out; a.qo = dq; a.ko = dk; a.pos = positions;
+        a.dgq = dg_q; a.dgk = dg_k; a.part = static_cast<float*>(ws);
+        a.sign = -1.0f;
+        frequencies(*desc, &a);
+        const double es = bf16 ? 2.0 : 4.0, n = (double)a.T * (a.hq + a.hk) * a.hd;
+        const int e = chk(timed_fn(COLA_KC_NORM_BWD, 20.0 * n, 3.0 * es * n, s,
+                                   [&] { return launch_norm_rope(bf16, NORM_BWD, a, s); }), "norm_rope_bwd");
+        if (e != COLA_OK || (!dg_q && !dg_k)) return e;
+        return chk(timed_fn(COLA_KC_NORM_BWD, 2.0 * (double)parts * a.hd, 8.0 * (double)parts * a.hd, s,
+                            [&] { return launch_norm_gain(a, parts, s); }), "norm_gain");
+    });
+}
+
+int cola_norm_append(const cola_rope_desc* rot, const cola_cache_desc* cache, double eps, const void* q, const void* k,
+                     const void* v, const void* g_q, const void* g_k, const int32_t* positions, const int32_t* slots,
+                     void* q_out, void* K, void* V, cola_stream_t stream) {
+    return guarded([&]() -> int {
+        NormRopeArgs a{};
+        int st = check_norm(rot, true, eps, g_q, g_k, &a);
+        if (st == COLA_OK) st = check_append(rot, cache);
+        if (st != COLA_OK) return st;
+        if (a.T == 0) return COLA_OK;
+        st = take_append(rot, cache, q, k, v, positions, slots, q_out, K, V, &a);
+        if (st != COLA_OK) return st;
+        const double es = rot->dtype == COLA_BF16 ? 2.0 : 4.0, n = (double)a.T * a.hd;
+        hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+        return chk(timed_fn(COLA_KC_NORM, 7.0 * n * (a.hq + a.hk), 2.0 * es * n * (a.hq + 2 * a.hk), s,
+                            [&] { return launch_norm_rope(rot->dtype == COLA_BF16, NORM_APPEND, a, s); }), "norm_append");
+    });
+}
+
+int cola_tree_map(const cola_tree_map_desc* d, const int32_t* parent, const int32_t* kv_len, const int32_t* start,
+                  uint64_t* mask, int32_t* positions, cola_stream_t stream) {
+    return guarded([&]() -> int {
+        if (!d) return COLA_ERR_INVALID_ARG;
+        if (d->n_req < 0 || d->n_req > 65535 || d->T < 0 || d->T > kMaxInt || d->max_new < 1 || d->max_new > COLA_TREE_MAX ||
+            d->pos0 < 0 || d->pos0 > kMaxInt)
+            return COLA_ERR_BAD_SHAPE;
+        if (d->T == 0) return COLA_OK;
+        if (!mask || !positions || (d->n_req > 0 && (!parent || !kv_len))) return COLA_ERR_INVALID_ARG;
+        if ((const void*)positions == parent || (const void*)mask == parent || (const void*)mask == positions) return COLA_ERR_INVALID_ARG;
+        for (const void* p : {(const void*)parent, (const void*)kv_len, (const void*)start, (const void*)positions})
+            if (!al4(p)) return COLA_ERR_INVALID_ARG;
+        if (!al8(mask)) return COLA_ERR_INVALID_ARG;
+        TreeMapArgs a{};
+        a.parent = parent; a.kv_len = kv_len; a.start = start; a.mask = mask; a.positions = positions;
+        a.T = d->T; a.pos0 = d->pos0;
+        a.n_req = (int)d->n_req; a.max_new = (int)d->max_new; a.words = (int)((d->max_new + 63) / 64);
+        hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+        return chk(timed_fn(COLA_KC_POINTWISE, 0.0, (double)d->T * (8.0 + 8.0 * a.words), s,
+                            [&] { return launch_tree_map(a, s); }), "tree_map");
+    });
+}
+
+int cola_logits_adjust(const cola_logits_desc* d, const cola_logits_rules* rules, const void* logits,
+                       const int32_t* start, void* out, cola_stream_t stream) {
+    return guarded([&]() -> int {
+        if (!d || !rules || !dtype_ok(d->dtype) || d->reserved != 0) return COLA_ERR_INVALID_ARG;
+        if (d->T < 0 || d->T > kMaxInt || d->V < 1 || d->V > kMaxPitch || d->n_req < 0 || d->n_req > 65535 || d->max_hist < 0 ||
+            d->max_hist > kMaxKeys || d->max_new < 0 || d->max_new > COLA_TREE_MAX || d->n_bias < 0 || d->n_bias > kMaxInt ||
+            d->n_allowed < 0 || d->n_allowed > kMaxInt)
+            return COLA_ERR_BAD_SHAPE;
+        LogitsArgs a{};
+        a.ldl = d->ldl ? d->ldl : d->V;
+        a.ldo = d->ldo ? d->ldo : d->V;
+        a.lda = d->lda ? d->lda : (d->V + 31) / 32;
+        if (a.ldl < d->V || a.ldl > kMaxPitch || a.ldo < d->V || a.ldo > kMaxPitch || a.lda < (d->V + 31) / 32 || a.lda > kMaxPitch)
+            return COLA_ERR_BAD_SHAPE;
+        if (d->T == 0 || d->n_req == 0) return COLA_OK;
+        const cola_logits_rules& u = *rules;
+        if (!logits || !out || !in_place_ok(logits, a.ldl, out, a.ldo)) return COLA_ERR_INVALID_ARG;
+        if (!aligned(logits, d->dtype) || !aligned(out, d->dtype) || !al8(u.mask)) return COLA_ERR_INVALID_ARG;
+        for (const void* p : {(const void*)start, (const void*)u.history, (const void*)u.prompt_len, (const void*)u.hist_len,
+                              (const void*)u.draft, (const void*)u.repetition, (const void*)u.presence, (const void*)u.frequency,
+                              (const void*)u.bias_start, (const void*)u.bias_token, (const void*)u.bias, (const void*)u.allowed,
+                              (const void*)u.allowed_row})
+            if (!al4(p)) return COLA_ERR_INVALID_ARG;
+        if (u.hist_len && d->max_hist > 0 && !u.history) return COLA_ERR_INVALID_ARG;
+        if (u.draft && (!u.mask || d->max_new < 1)) return COLA_ERR_INVALID_ARG;
+        if (u.bias_start && d->n_bias > 0 && (!u.bias_token || !u.bias)) return COLA_ERR_INVALID_ARG;
+        a.logits = logits; a.out = out; a.start = start;
+        a.history = u.history; a.prompt_len = u.prompt_len; a.hist_len = u.hist_len; a.draft = u.draft; a.mask = u.mask;
+        if (u.hist_len || u.draft) {
+            a.repetition = u.repetition; a.presence = u.presence; a.frequency = u.frequency;
+        }
+        a.bias_start = u.bias_start; a.bias_token = u.bias_token; a.bias = u.bias;
+        a.allowed = d->n_allowed > 0 ? u.allowed : nullptr; a.allowed_row = u.allowed_row;
+        a.T = d->T; a.V = d->V; a.max_hist = d->max_hist; a.n_bias = d->n_bias; a.n_allowed = d->n_allowed;
+        a.n_req = (int)d->n_req; a.max_new = (int)d->max_new; a.words = (int)((d->max_new + 63) / 64);
+        const double es = d->dtype == COLA_BF16 ? 2.0 : 4.0, n = (double)d->T * (double)d->V;
+        hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+        return chk(timed_fn(COLA_KC_POINTWISE, 4.0 * n, 2.0 * es * n, s,
+                            [&] { return launch_logits(d->dtype == COLA_BF16, a, s); }), "logits_adjust");
     });
 }
 

@@ -417,17 +417,17 @@ PyObject* page_map(PyObject*, Args v, Py_ssize_t n) {    // d, kv_len, n_new, fr
     });
 }
 
-PyObject* prefix_attn(PyObject*, Args v, Py_ssize_t n) { // d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, ws_bytes, device, stream
-    return call([&](int* st) {
-        cola_prefix_attn_desc d;
-        Cache c;
-        Here h;
-        void *q, *K, *V, *table = nullptr, *out, *lse, *ws;
-        const int32_t *prefix, *kv = nullptr, *start;
-        size_t ws_bytes;
-        if (n != 15 || !h.init(v + 13) || !take_desc(v[0], &d) || !c.init(v[1]) || c.c.dtype != COLA_BF16 || d.n_req < 1 ||
-            d.T < 1)
-            return false;
+// The arguments that prefix_attn and tree_attn share: d, c, q, K, V, prefix_table, table, kv_len, start; then
+// out, lse, ws, ws_bytes.
+struct Attend {
+    cola_prefix_attn_desc d;
+    Cache c;
+    void *q, *K, *V, *table = nullptr, *out, *lse, *ws;
+    const int32_t *prefix, *kv = nullptr, *start;
+    size_t ws_bytes;
+
+    bool init(const Here& h, Args v, Args o) {
+        if (!take_desc(v[0], &d) || !c.init(v[1]) || c.c.dtype != COLA_BF16 || d.n_req < 1 || d.T < 1) return false;
         for (int64_t x : {d.n_req, d.T, d.heads_q, d.prefix_len, d.max_kv, d.max_pages, d.ldq, d.ldo})
             if (!count_ok(x)) return false;
         const int64_t w = d.heads_q * c.c.head_dim, ps = c.c.page_size;
@@ -438,12 +438,152 @@ PyObject* prefix_attn(PyObject*, Args v, Py_ssize_t n) { // d, c, q, K, V, prefi
             const int64_t width = d.max_pages ? d.max_pages : (d.max_kv + ps - 1) / ps;
             if (!h.flat(v[6], {d.n_req, width}, at::kInt, false, &table) || !h.ints(v[7], d.n_req, false, &kv)) return false;
         }
-        if (!h.ints(v[8], d.n_req + 1, true, &start) || !h.rows(v[9], d.T, w, d.ldo, at::kBFloat16, &out) ||
-            !h.flat(v[10], {d.heads_q, d.T}, at::kFloat, true, &lse) || !take_ws(v[11], v[12], &ws, &ws_bytes))
+        if (!h.ints(v[8], d.n_req + 1, true, &start) || !h.rows(o[0], d.T, w, d.ldo, at::kBFloat16, &out) ||
+            !h.flat(o[1], {d.heads_q, d.T}, at::kFloat, true, &lse) || !take_ws(o[2], o[3], &ws, &ws_bytes))
             return false;
-        if (ws && THPVariable_Unpack(v[11]).get_device() != h.device) return false;
-        COLA_CALL(cola_prefix_attn(&d, &c.c, q, K, V, prefix, static_cast<const int32_t*>(table), kv, start, out,
-                                   static_cast<float*>(lse), ws, ws_bytes, h.s()));
+        return !ws || THPVariable_Unpack(o[2]).get_device() == h.device;
+    }
+};
+
+PyObject* prefix_attn(PyObject*, Args v, Py_ssize_t n) { // d, c, q, K, V, prefix_table, table, kv_len, start, out, lse, ws, ws_bytes, device, stream
+    return call([&](int* st) {
+        Attend a;
+        Here h;
+        if (n != 15 || !h.init(v + 13) || !a.init(h, v, v + 9)) return false;
+        COLA_CALL(cola_prefix_attn(&a.d, &a.c.c, a.q, a.K, a.V, a.prefix, static_cast<const int32_t*>(a.table), a.kv, a.start,
+                                   a.out, static_cast<float*>(a.lse), a.ws, a.ws_bytes, h.s()));
+    });
+}
+
+PyObject* tree_attn(PyObject*, Args v, Py_ssize_t n) {   // prefix_attn's with mask before out
+    return call([&](int* st) {
+        Attend a;
+        Here h;
+        void* mask;
+        if (n != 16 || !h.init(v + 14) || !a.init(h, v, v + 10) || !dim_ok(a.d.max_new) ||
+            !h.flat(v[9], {a.d.T, (a.d.max_new + 63) / 64}, at::kLong, false, &mask))
+            return false;
+        COLA_CALL(cola_tree_attn(&a.d, &a.c.c, a.q, a.K, a.V, a.prefix, static_cast<const int32_t*>(a.table), a.kv, a.start,
+                                 static_cast<const uint64_t*>(mask), a.out, static_cast<float*>(a.lse), a.ws, a.ws_bytes, h.s()));
+    });
+}
+
+bool take_real(PyObject* o, double* out) {
+    if (!PyFloat_CheckExact(o)) return false;
+    *out = PyFloat_AS_DOUBLE(o);
+    return true;
+}
+
+struct Gains {
+    void *q, *k;
+    double eps;
+    bool init(const Here& h, const Rope& r, PyObject* g_q, PyObject* g_k, PyObject* e) {
+        return take_real(e, &eps) && h.flat(g_q, {r.d.head_dim}, r.t, true, &q) && h.flat(g_k, {r.d.head_dim}, r.t, true, &k);
+    }
+};
+
+PyObject* norm_rope_fwd(PyObject*, Args v, Py_ssize_t n) { // d, q, k, g_q, g_k, positions, q_out, k_out, eps, device, stream
+    return call([&](int* st) {
+        Rope r;
+        Here h;
+        Gains g;
+        void *q, *k, *qo, *ko;
+        const int32_t* pos;
+        if (n != 11 || !h.init(v + 9) || !r.init(v[0]) || !g.init(h, r, v[3], v[4], v[8]) ||
+            !h.rows(v[1], r.d.T, r.wq, r.d.ldq, r.t, &q) || !h.rows(v[2], r.d.T, r.wk, r.d.ldk, r.t, &k) ||
+            !h.ints(v[5], r.d.T, true, &pos) || !h.rows(v[6], r.d.T, r.wq, r.d.ldqo, r.t, &qo) ||
+            !h.rows(v[7], r.d.T, r.wk, r.d.ldko, r.t, &ko))
+            return false;
+        COLA_CALL(cola_norm_rope_fwd(&r.d, g.eps, q, k, g.q, g.k, pos, qo, ko, h.s()));
+    });
+}
+
+PyObject* norm_rope_bwd(PyObject*, Args v, Py_ssize_t n) { // d, dq_out, dk_out, q, k, g_q, g_k, positions, dq, dk, dg_q, dg_k, ws, ws_bytes, eps, device, stream
+    return call([&](int* st) {
+        Rope r;
+        Here h;
+        Gains g;
+        void *q, *k, *dqo, *dko, *dq, *dk, *dgq, *dgk, *ws;
+        const int32_t* pos;
+        size_t ws_bytes;
+        if (n != 17 || !h.init(v + 15) || !r.init(v[0]) || !g.init(h, r, v[5], v[6], v[14]) ||
+            !h.rows(v[1], r.d.T, r.wq, r.d.ldqo, r.t, &dqo) || !h.rows(v[2], r.d.T, r.wk, r.d.ldko, r.t, &dko) ||
+            !h.rows(v[3], r.d.T, r.wq, r.d.ldq, r.t, &q) || !h.rows(v[4], r.d.T, r.wk, r.d.ldk, r.t, &k) ||
+            !h.ints(v[7], r.d.T, true, &pos) || !h.rows(v[8], r.d.T, r.wq, r.d.ldq, r.t, &dq) ||
+            !h.rows(v[9], r.d.T, r.wk, r.d.ldk, r.t, &dk) || !h.flat(v[10], {r.d.head_dim}, at::kFloat, true, &dgq) ||
+            !h.flat(v[11], {r.d.head_dim}, at::kFloat, true, &dgk) || !take_ws(v[12], v[13], &ws, &ws_bytes))
+            return false;
+        if (ws && THPVariable_Unpack(v[12]).get_device() != h.device) return false;
+        COLA_CALL(cola_norm_rope_bwd(&r.d, g.eps, dqo, dko, q, k, g.q, g.k, pos, dq, dk, static_cast<float*>(dgq),
+                                     static_cast<float*>(dgk), ws, ws_bytes, h.s()));
+    });
+}
+
+PyObject* norm_append(PyObject*, Args v, Py_ssize_t n) { // d, c, q, k, v, g_q, g_k, positions, slots, q_out, K, V, eps, device, stream
+    return call([&](int* st) {
+        Rope r;
+        Cache c;
+        Here h;
+        Gains g;
+        void *q, *k, *val, *qo, *K, *V;
+        const int32_t *pos, *slots;
+        if (n != 15 || !h.init(v + 13) || !r.init(v[0]) || !c.init(v[1]) || !g.init(h, r, v[5], v[6], v[12]) ||
+            !h.rows(v[2], r.d.T, r.wq, r.d.ldq, r.t, &q) || !h.rows(v[3], r.d.T, r.wk, r.d.ldk, r.t, &k) ||
+            !h.rows(v[4], r.d.T, r.wk, r.d.ldv, r.t, &val) || !h.ints(v[7], r.d.T, true, &pos) ||
+            !h.ints(v[8], r.d.T, false, &slots) || !h.rows(v[9], r.d.T, r.wq, r.d.ldqo, r.t, &qo) ||
+            !c.pages(h, v[10], &K) || !c.pages(h, v[11], &V))
+            return false;
+        COLA_CALL(cola_norm_append(&r.d, &c.c, g.eps, q, k, val, g.q, g.k, pos, slots, qo, K, V, h.s()));
+    });
+}
+
+PyObject* tree_map(PyObject*, Args v, Py_ssize_t n) {    // d, parent, kv_len, start, mask, positions, device, stream
+    return call([&](int* st) {
+        cola_tree_map_desc d;
+        Here h;
+        void* mask;
+        const int32_t *parent, *kv, *start, *pos;
+        if (n != 8 || !h.init(v + 6) || !take_desc(v[0], &d) || !dim_ok(d.n_req) || !dim_ok(d.T) || !dim_ok(d.max_new) ||
+            !h.ints(v[1], d.T, false, &parent) || !h.ints(v[2], d.n_req, false, &kv) || !h.ints(v[3], d.n_req + 1, true, &start) ||
+            !h.flat(v[4], {d.T, (d.max_new + 63) / 64}, at::kLong, false, &mask) || !h.ints(v[5], d.T, false, &pos))
+            return false;
+        COLA_CALL(cola_tree_map(&d, parent, kv, start, static_cast<uint64_t*>(mask), const_cast<int32_t*>(pos), h.s()));
+    });
+}
+
+PyObject* logits_adjust(PyObject*, Args v, Py_ssize_t n) { // d, rules, logits, start, out, device, stream
+    return call([&](int* st) {
+        cola_logits_desc d;
+        cola_logits_rules u;
+        Here h;
+        void *logits, *out, *mask, *rep, *pres, *freq, *bias, *allowed;
+        const int32_t* start;
+        if (n != 7 || !h.init(v + 5) || !take_desc(v[0], &d) || !PyTuple_CheckExact(v[1]) || PyTuple_GET_SIZE(v[1]) != 13 ||
+            (d.dtype != COLA_F32 && d.dtype != COLA_BF16) || !dim_ok(d.T) || !dim_ok(d.V) || !dim_ok(d.n_req))
+            return false;
+        for (int64_t x : {d.max_hist, d.max_new, d.n_bias, d.n_allowed, d.ldl, d.ldo, d.lda})
+            if (!count_ok(x)) return false;
+        const at::ScalarType t = d.dtype == COLA_BF16 ? at::kBFloat16 : at::kFloat;
+        auto rule = [&](int i) { return PyTuple_GET_ITEM(v[1], i); };
+        void* history;
+        if (!h.flat(rule(0), {d.n_req, d.max_hist}, at::kInt, true, &history) || !h.ints(rule(1), d.n_req, true, &u.prompt_len) ||
+            !h.ints(rule(2), d.n_req, true, &u.hist_len) || !h.ints(rule(3), d.T, true, &u.draft) ||
+            !h.flat(rule(4), {d.T, (d.max_new + 63) / 64}, at::kLong, true, &mask) ||
+            !h.flat(rule(5), {d.n_req}, at::kFloat, true, &rep) || !h.flat(rule(6), {d.n_req}, at::kFloat, true, &pres) ||
+            !h.flat(rule(7), {d.n_req}, at::kFloat, true, &freq) || !h.ints(rule(8), d.n_req + 1, true, &u.bias_start) ||
+            !h.ints(rule(9), d.n_bias, true, &u.bias_token) || !h.flat(rule(10), {d.n_bias}, at::kFloat, true, &bias) ||
+            !h.flat(rule(11), {d.n_allowed, d.lda ? d.lda : (d.V + 31) / 32}, at::kInt, true, &allowed) ||
+            !h.ints(rule(12), d.T, true, &u.allowed_row) || !h.rows(v[2], d.T, d.V, d.ldl, t, &logits) ||
+            !h.ints(v[3], d.n_req + 1, true, &start) || !h.rows(v[4], d.T, d.V, d.ldo, t, &out))
+            return false;
+        u.history = static_cast<const int32_t*>(history);
+        u.mask = static_cast<const uint64_t*>(mask);
+        u.repetition = static_cast<const float*>(rep);
+        u.presence = static_cast<const float*>(pres);
+        u.frequency = static_cast<const float*>(freq);
+        u.bias = static_cast<const float*>(bias);
+        u.allowed = static_cast<const uint32_t*>(allowed);
+        COLA_CALL(cola_logits_adjust(&d, &u, logits, start, out, h.s()));
     });
 }
 
@@ -451,7 +591,8 @@ PyObject* prefix_attn(PyObject*, Args v, Py_ssize_t n) { // d, c, q, K, V, prefi
 PyMethodDef methods[] = {COLA_METHOD(fwd),       COLA_METHOD(fwd_outer), COLA_METHOD(infer),       COLA_METHOD(bwd),
                          COLA_METHOD(bwd_outer), COLA_METHOD(group_fwd), COLA_METHOD(group_infer), COLA_METHOD(group_bwd),
                          COLA_METHOD(rope_fwd),  COLA_METHOD(rope_bwd),  COLA_METHOD(cache_append), COLA_METHOD(page_map),
-                         COLA_METHOD(prefix_attn),
+                         COLA_METHOD(prefix_attn), COLA_METHOD(norm_rope_fwd), COLA_METHOD(norm_rope_bwd), COLA_METHOD(norm_append),
+                         COLA_METHOD(tree_map),  COLA_METHOD(tree_attn), COLA_METHOD(logits_adjust),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,658 @@
+"""Head norms, drafted trees and rules on logits on the GPU against their definitions in 64
+bits (tests/verify_ref.py), element by element within the bounds derived there: odd
+and smallest sizes, layouts, far positions, strides and alignments, masks that leave
+nothing, infinities and NaN in masked places, batches cut at their rows, bounds above
+and below the lengths; gradients against the formula's and against differences;
+streams, graphs, workspace contents; and a run of them together as a program uses
+them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import serve_ref as R
+import verify_ref as W
+from paper_2502_10940_amd import cola
+from test_gpu_serve import ATTN, DEV, DT, KERNELS, ROPE, SCALINGS, Batch, f64, i32, pitched, rand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    cola.lib()
+    yield
+
+
+def gain(seed, hd, dtype):
+    return (1.0 + 0.3 * rand(seed, (hd,), "f32")).to(DT[dtype])
+
+
+def workspace(d, fill=0xFF):
+    return torch.full((cola.norm_rope_workspace_bytes(d),), fill, dtype=torch.uint8, device=DEV)
+
+
+# ---------------------------------------------------------------------------
+# norms
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("layout", ("half", "interleaved"))
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("case", range(len(ROPE)), ids=["%dx%d+%dx%d-%d" % c for c in ROPE])
+def test_norm_rope(case, dtype, layout):
+    """Both directions, gains given and not."""
+    T, hq, hk, hd, rot = ROPE[case]
+    name = sorted(SCALINGS)[case % len(SCALINGS)]
+    if name == "base" and rot <= 2:
+        name = "linear"
+    sc = dict(SCALINGS[name], base=500000.0 if case % 2 else 10000.0)
+    rng = np.random.default_rng(200 + case)
+    pos = rng.integers(0, 1 << 20, T)
+    pos[0] = (2 ** 31 - 1) if case % 2 else -5
+    m = 1.25 if case % 3 == 0 else 0.0
+    eps = 1e-6 if case % 2 else 0.37
+    d = cola.rope_desc(T, hq, hk, hd, rot, dtype, layout, name, mscale=m, **sc)
+    kw = dict(layout=layout, eps=eps, mscale=m, scaling=name, **sc)
+    x = {n: rand(case + i, (T, max(h, 1) * hd), dtype) for i, (n, h) in enumerate((("q", hq), ("k", hk)))}
+    dy = {n: rand(case + 70 + i, (T, max(h, 1) * hd), dtype) for i, (n, h) in enumerate((("q", hq), ("k", hk)))}
+    g = {"q": gain(case, hd, dtype), "k": gain(case + 9, hd, dtype)}
+    if case % 4 == 3:
+        g["k" if case % 8 == 3 else "q"] = None
+    there = {"q": hq > 0, "k": hk > 0}
+    pick = lambda t, n: t if there[n] else None
+    out = {n: torch.full_like(x[n], math.nan) for n in "qk"}
+    cola.norm_rope_fwd(d, pick(x["q"], "q"), pick(x["k"], "k"), g["q"], g["k"], i32(pos), pick(out["q"], "q"), pick(out["k"], "k"), eps=eps)
+    dx = {n: torch.full_like(x[n], math.nan) for n in "qk"}
+    dg = {n: torch.full((hd,), math.nan, device=DEV) for n in "qk"}
+    cola.norm_rope_bwd(d, pick(dy["q"], "q"), pick(dy["k"], "k"), pick(x["q"], "q"), pick(x["k"], "k"), g["q"], g["k"], i32(pos),
+                       pick(dx["q"], "q"), pick(dx["k"], "k"), pick(dg["q"], "q"), pick(dg["k"], "k"), workspace(d), eps=eps)
+    torch.cuda.synchronize()
+    for n in "qk":
+        if not there[n]:
+            assert torch.isnan(out[n]).all() and torch.isnan(dx[n]).all() and torch.isnan(dg[n]).all()
+            continue
+        gn = None if g[n] is None else f64(g[n])
+        ref, bound = W.norm_rope(f64(x[n]), gn, hd, rot, pos, dtype, **kw)
+        err = np.abs(f64(out[n]) - ref)
+        assert (err <= bound).all(), (n, (err / bound).max())
+        (rx, bx), (rg, bg) = W.norm_rope_bwd(f64(dy[n]), f64(x[n]), gn, hd, rot, pos, dtype, **kw)
+        err = np.abs(f64(dx[n]) - rx)
+        assert (err <= bx).all(), (n, (err / bx).max())
+        err = np.abs(f64(dg[n]) - rg)
+        assert (err <= bg).all(), (n, (err / bg).max())
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("layout", ("half", "interleaved"))
+def test_norm_rope_pitches_alignment_and_in_place(dtype, layout):
+    """Slices of one buffer at an odd pitch and start: the bits of tight rows, nothing else
+    touched; in place too, in both directions."""
+    T, hq, hk, hd, seq = 37, 4, 2, 64, 10
+    q, k, dq, dk = (rand(i, (T, h * hd), dtype) for i, h in enumerate((hq, hk, hq, hk)))
+    gq, gk = gain(5, hd + 3, dtype)[3:].clone(), gain(6, hd + 3, dtype)[3:]      # the second 3 elements off
+    want = [torch.empty_like(q), torch.empty_like(k)]
+    d = cola.rope_desc(T, hq, hk, hd, dtype=dtype, layout=layout, seq_len=seq)
+    cola.norm_rope_fwd(d, q, k, gq, gk, None, *want)
+    back = [torch.empty_like(q), torch.empty_like(k)]
+    dg = [torch.empty(hd, device=DEV) for _ in range(2)]
+    cola.norm_rope_bwd(d, dq, dk, q, k, gq, gk, None, *back, *dg, workspace(d))
+    for ldi, ldk, off in ((hq * hd + hk * hd, hq * hd + hk * hd, 8), (hq * hd + 3, hk * hd + 1, 1), (hq * hd + 37, hk * hd, 5)):
+        (pq, bq), (pk, bk) = pitched(q, ldi, off), pitched(k, ldk, off)
+        oq, ob = pitched(torch.zeros_like(q), hq * hd + 5, 3)
+        ok, okb = pitched(torch.zeros_like(k), hk * hd + 7, 1)
+        d = cola.rope_desc(T, hq, hk, hd, dtype=dtype, layout=layout, seq_len=seq, ldq=ldi, ldk=ldk, ldqo=hq * hd + 5, ldko=hk * hd + 7)
+        cola.norm_rope_fwd(d, pq, pk, gq, gk, None, oq, ok)
+        assert torch.equal(oq, want[0]) and torch.equal(ok, want[1])
+        for b, n in ((ob, q), (okb, k)):
+            assert torch.isnan(b).sum() == b.numel() - n.numel()         # the padding stayed
+        # the gradients' rows at the outputs' pitches, results over the inputs
+        oq.copy_(dq), ok.copy_(dk)
+        got = [torch.empty(hd, device=DEV) for _ in range(2)]
+        cola.norm_rope_bwd(d, oq, ok, pq, pk, gq, gk, None, pq, pk, *got, workspace(d))
+        assert torch.equal(pq, back[0]) and torch.equal(pk, back[1])
+        assert all(torch.equal(a, b) for a, b in zip(got, dg))
+        for b, n in ((bq, q), (bk, k)):
+            assert torch.isnan(b).sum() == b.numel() - n.numel()
+        pq.copy_(q), pk.copy_(k)
+        d = cola.rope_desc(T, hq, hk, hd, dtype=dtype, layout=layout, seq_len=seq, ldq=ldi, ldk=ldk, ldqo=ldi, ldko=ldk)
+        cola.norm_rope_fwd(d, pq, pk, gq, gk, None, pq, pk)
+        assert torch.equal(pq, want[0]) and torch.equal(pk, want[1])
+    # over the gradients' rows
+    d = cola.rope_desc(T, hq, hk, hd, dtype=dtype, layout=layout, seq_len=seq)
+    a, b = dq.clone(), dk.clone()
+    cola.norm_rope_bwd(d, a, b, q, k, gq, gk, None, a, b, None, None, workspace(d))
+    assert torch.equal(a, back[0]) and torch.equal(b, back[1])
+
+
+@pytest.mark.parametrize("layout", ("half", "interleaved"))
+def test_norm_gradient_against_differences(layout):
+    """<dx, e> + <dg, f> against a central difference of <y, c> along (e, f) on the GPU, in
+    fp32: what the same difference of the 64-bit forward is off, and the roundings of
+    the two forwards (2^-20 of a pair's magnitudes in each element) over the step."""
+    T, h, hd, rot = 6, 2, 32, 24
+    x, e, c = (rand(s, (T, h * hd), "f32") for s in (1, 2, 3))
+    g, f = gain(4, hd, "f32"), rand(5, (hd,), "f32")
+    pos = [0, 1, 5, 100, 70000, 3]
+    d = cola.rope_desc(T, h, 0, hd, rot, "f32", layout)
+    s = 2.0 ** -5
+    y = []
+    for k in (s, -s):
+        out = torch.empty_like(x)
+        cola.norm_rope_fwd(d, x + k * e, None, g + k * f, None, i32(pos), out, None)
+        y.append((f64(out) * f64(c)).sum())
+    dx, dg = torch.empty_like(x), torch.empty(hd, device=DEV)
+    cola.norm_rope_bwd(d, c, None, x, None, g, None, i32(pos), dx, None, dg, None, workspace(d))
+    grad = (f64(dx) * f64(e)).sum() + (f64(dg) * f64(f)).sum()
+    ref = lambda k: (W.norm_rope(f64(x + k * e), f64(g + k * f), hd, rot, pos, "f32", layout)[0] * f64(c)).sum()
+    (rx, bx), (rg, bg) = W.norm_rope_bwd(f64(c), f64(x), f64(g), hd, rot, pos, "f32", layout)
+    exact = (rx * f64(e)).sum() + (rg * f64(f)).sum()
+    cut = abs((ref(s) - ref(-s)) / (2 * s) - exact)
+    _, yb = W.norm_rope(f64(x), f64(g), hd, rot, pos, "f32", layout)
+    rounding = 2 * 1.2 * (yb * np.abs(f64(c))).sum() / (2 * s)
+    own = (bx * np.abs(f64(e))).sum() + (bg * np.abs(f64(f))).sum()
+    assert abs((y[0] - y[1]) / (2 * s) - grad) <= cut + rounding + own
+
+
+def test_norm_rope_of_no_rows_and_no_gains():
+    d = cola.rope_desc(0, 2, 2, 64)
+    dg = [torch.full((64,), 7.0, device=DEV) for _ in range(2)]
+    x = torch.zeros((0, 128), dtype=torch.bfloat16, device=DEV)
+    cola.norm_rope_bwd(d, x, x, x, x, None, None, None, x, x, *dg, None)
+    assert all((t == 0).all() for t in dg)
+    cola.norm_rope_fwd(d, x, x, None, None, None, x, x)
+
+
+@pytest.mark.parametrize("value", (0.0, math.inf, math.nan, 3.0e38))
+def test_norm_rope_rows_do_not_reach_each_other(value):
+    """A head of zeros gives zeros and finite gradients; one of anything else leaves the rows
+    and heads beside it as they are."""
+    T, h, hd = 21, 4, 64
+    q, dy, g = rand(1, (T, h * hd), "bf16"), rand(2, (T, h * hd), "bf16"), gain(3, hd, "bf16")
+    d = cola.rope_desc(T, h, 0, hd)
+
+    def both(q):
+        out, dx = torch.empty_like(q), torch.empty_like(q)
+        dg = torch.empty(hd, device=DEV)
+        cola.norm_rope_fwd(d, q, None, g, None, None, out, None)
+        cola.norm_rope_bwd(d, dy, None, q, None, g, None, None, dx, None, dg, None, workspace(d))
+        return out, dx, dg
+
+    a = both(q)
+    z = q.clone()
+    z[5, hd:2 * hd] = value
+    b = both(z)
+    keep = torch.ones_like(q, dtype=torch.bool)
+    keep[5, hd:2 * hd] = False
+    for u, v in zip(a[:2], b[:2]):
+        assert torch.equal(u[keep], v[keep])
+    if value == 0.0:
+        assert (b[0][5, hd:2 * hd] == 0).all() and all(torch.isfinite(t.float()).all() for t in b)
+
+
+@pytest.mark.parametrize("dtype, layout", [("bf16", "half"), ("bf16", "interleaved"), ("f32", "half")])
+def test_large_norm_results_are_the_small_ones(dtype, layout):
+    """Sizes whose results go past the caches: every row has the bits that a small call
+    gives it, and dg is within its bound."""
+    T, hq, hk, hd = 9001, 24, 8, 128
+    q, k, dq, dk = (rand(i, (T, h * hd), dtype) for i, h in enumerate((hq, hk, hq, hk)))
+    gq, gk = gain(5, hd, dtype), gain(6, hd, dtype)
+    pos = torch.randint(0, 1 << 20, (T,), device=DEV, dtype=torch.int32)
+    o = [torch.empty_like(q), torch.empty_like(k)]
+    dx = [torch.empty_like(q), torch.empty_like(k)]
+    dg = [torch.empty(hd, device=DEV) for _ in range(2)]
+    d = cola.rope_desc(T, hq, hk, hd, dtype=dtype, layout=layout)
+    cola.norm_rope_fwd(d, q, k, gq, gk, pos, *o)
+    cola.norm_rope_bwd(d, dq, dk, q, k, gq, gk, pos, *dx, *dg, workspace(d))
+    for lo, n in ((0, 3), (4000, 17), (T - 5, 5)):
+        part = [t[lo:lo + n].clone() for t in (q, k, dq, dk, pos)]
+        s = [torch.empty_like(part[0]), torch.empty_like(part[1])]
+        sd = cola.rope_desc(n, hq, hk, hd, dtype=dtype, layout=layout)
+        cola.norm_rope_fwd(sd, part[0], part[1], gq, gk, part[4], *s)
+        assert all(torch.equal(a[lo:lo + n], b) for a, b in zip(o, s))
+        cola.norm_rope_bwd(sd, part[2], part[3], part[0], part[1], gq, gk, part[4], *s, None, None, workspace(sd))
+        assert all(torch.equal(a[lo:lo + n], b) for a, b in zip(dx, s))
+    p = pos.cpu().numpy()
+    for y, x, g, got in ((dq, q, gq, dg[0]), (dk, k, gk, dg[1])):
+        _, (ref, bound) = W.norm_rope_bwd(f64(y), f64(x), f64(g), hd, hd, p, dtype, layout)
+        # 2^18 terms at random signs: far inside the bound, which takes the worst order
+        assert (np.abs(f64(got) - ref) <= bound).all() and np.abs(f64(got) - ref).max() < 2.0 ** -12 * np.abs(ref).max()
+
+
+def test_norm_gradients_do_not_depend_on_the_workspace_s_contents_or_the_run():
+    T, hq, hk, hd = 700, 5, 3, 96
+    q, k, dq, dk = (rand(i, (T, h * hd), "bf16") for i, h in enumerate((hq, hk, hq, hk)))
+    gq, gk = gain(5, hd, "bf16"), gain(6, hd, "bf16")
+    d = cola.rope_desc(T, hq, hk, hd, 48)
+    got = []
+    for fill in (0, 0xFF, 0x7F, 0):
+        o = [torch.empty_like(q), torch.empty_like(k), torch.empty(hd, device=DEV), torch.empty(hd, device=DEV)]
+        cola.norm_rope_bwd(d, dq, dk, q, k, gq, gk, None, *o, workspace(d, fill))
+        got.append(o)
+    assert all(torch.equal(a, b) for o in got[1:] for a, b in zip(got[0], o))
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("case", [(1, 1, 1, 64, 64, 16), (19, 8, 2, 128, 128, 32), (33, 5, 5, 80, 40, 16), (7, 0, 3, 33, 0, 64),
+                                  (300, 16, 4, 64, 64, 128)], ids=str)
+def test_norm_append(case, dtype):
+    """As norm_rope_fwd's rows, in their slots; rows without a slot, and slots without a row, are left."""
+    T, hq, hk, hd, rot, page = case
+    pages = -(-T // page) + 2
+    q, k, v = (rand(i, (T, max(h, 1) * hd), dtype) for i, h in enumerate((hq, hk, hk)))
+    gq, gk = gain(4, hd, dtype), gain(5, hd, dtype)
+    rng = np.random.default_rng(T)
+    slots = rng.permutation(pages * page)[:T]
+    bad = rng.random(T) < 0.2
+    slots[bad] = rng.choice([-1, pages * page, 2 ** 31 - 1, -2 ** 31], bad.sum())
+    pos = rng.integers(0, 1 << 17, T)
+    K, V = (rand(9 + i, (pages, hk, page, hd), dtype) for i in range(2))
+    K0, V0 = K.clone(), V.clone()
+    qo = torch.full_like(q, math.nan)
+    d = cola.rope_desc(T, hq, hk, hd, rot, dtype)
+    c = cola.cache_desc(pages, page, hk, hd, dtype)
+    cola.norm_append(d, c, q if hq else None, k, v, gq, gk, i32(pos), i32(slots), qo if hq else None, K, V)
+    want = [torch.empty_like(q), torch.empty_like(k)]
+    cola.norm_rope_fwd(d, q if hq else None, k, gq, gk, i32(pos), want[0] if hq else None, want[1])
+    if hq:
+        assert torch.equal(qo, want[0])
+    for t in range(T):
+        if not bad[t]:
+            K0[slots[t] // page, :, slots[t] % page] = want[1][t].view(hk, hd)
+            V0[slots[t] // page, :, slots[t] % page] = v[t].view(hk, hd)
+    assert torch.equal(K, K0) and torch.equal(V, V0)
+
+
+# ---------------------------------------------------------------------------
+# trees
+# ---------------------------------------------------------------------------
+
+def run_tree_map(parent, kv, start, T, max_new, pos0):
+    w = -(-max_new // 64)
+    mask = torch.full((T, w), -7, dtype=torch.int64, device=DEV)
+    pos = torch.full((T,), -7, dtype=torch.int32, device=DEV)
+    n = T if start is None else len(start) - 1
+    cola.tree_map(cola.tree_map_desc(n, T, max_new, pos0), i32(parent), i32(kv), None if start is None else i32(start), mask, pos)
+    torch.cuda.synchronize()
+    m, p = W.tree_map(parent, kv, list(range(T + 1)) if start is None else start, T, max_new, pos0)
+    assert np.array_equal(mask.cpu().numpy(), W.words(m, max_new)) and pos.cpu().tolist() == p
+
+
+@pytest.mark.parametrize("max_new", (1, 2, 63, 64, 65, 128, 129, 200, 256))
+@pytest.mark.parametrize("n_req", (1, 5, 300))
+def test_tree_map(n_req, max_new):
+    rng = np.random.default_rng(n_req + max_new)
+    new = rng.integers(0, max_new + 1, n_req)
+    new[0] = max_new
+    start = np.concatenate([[3], 3 + np.cumsum(new)])
+    T = int(start[-1]) + 5
+    parent = rng.integers(-3, 300, T)                                 # rows of no request hold anything
+    for r, n in enumerate(new):
+        parent[start[r]:start[r] + n] = list(range(-1, n - 1)) if r == 1 else W.random_tree(rng, n, 1 + r % 2)
+    run_tree_map(parent, rng.integers(0, 5000, n_req) + new, start, T, max_new, 77)
+
+
+def test_tree_map_edges():
+    rng = np.random.default_rng(0)
+    # parents that are none: the node itself, a later one, anything
+    run_tree_map([0, 5, 1, -9, 2 ** 31 - 1, -2 ** 31, 4], [7], [0, 7], 7, 7, 0)
+    # more nodes than max_new, and than rows; a chain; kv_len below the nodes; positions at the ends of their range
+    chain = list(range(-1, 99))
+    run_tree_map(chain, [100], [0, 100], 100, 70, 0)
+    run_tree_map(chain[:40], [100], [0, 100], 40, 100, 3)
+    run_tree_map(chain, [3], [0, 100], 100, 100, 0)
+    run_tree_map(chain, [2 ** 31 - 1], [0, 100], 100, 128, 2 ** 31 - 1)
+    # a row each; nothing at all
+    run_tree_map(rng.integers(-2, 3, 9), rng.integers(1, 9, 9), None, 9, 4, 5)
+    run_tree_map([1, 2, 3], [], [0], 3, 64, 0)
+    run_tree_map([1, 2, 3], [5, 5], [3, 3, 3], 3, 200, 0)
+
+
+class TreeBatch(Batch):
+    """A batch whose new tokens see each other by masks: whole numbers, a bit for each."""
+
+    def __init__(self, *a, masks="trees", **kw):
+        super().__init__(*a, **kw)
+        rng = np.random.default_rng(a[0] + 1000)
+        self.masks = [0] * self.T
+        for r, n in enumerate(self.new):
+            parent = W.random_tree(rng, n, 1 + r % 3)
+            for i in range(n):
+                t = self.start[r] + i
+                up = self.masks[self.start[r] + parent[i]] if parent[i] >= 0 else 0
+                self.masks[t] = {"trees": up | 1 << i, "chains": (2 << i) - 1,
+                                 "any": int(rng.integers(0, 2 ** 62)) * 2 ** 200 // 3 ** int(rng.integers(0, 90)) % 2 ** n if (i + r) % 4 else 0}[masks]
+                if masks == "any":                                    # bits that have no token
+                    self.masks[t] |= 2 ** (64 * (-(-self.max_new // 64))) - 2 ** min(n, 64 * (-(-self.max_new // 64)))
+
+    def run(self, ws_fill=0xFF, lse=True, start=True, stream=None):
+        d, c = self.desc()
+        q = self.q if not self.ldq else pitched(self.q, self.ldq, 8)[0]
+        out = torch.full((self.T, self.ldo or self.hq * self.hd), 7.0, dtype=torch.bfloat16, device=DEV)
+        ls = torch.full((self.hq, self.T), 7.0, device=DEV) if lse else None
+        n = cola.tree_attn_workspace_bytes(d, c)
+        ws = torch.full((n,), ws_fill, dtype=torch.uint8, device=DEV) if n else None
+        cola.tree_attn(d, c, q, self.K, self.V, i32(self.ptab) if self.L else None, i32(self.tab) if self.max_kv else None,
+                       i32(self.kv) if self.max_kv else None, i32(self.start) if start else None,
+                       torch.from_numpy(W.words(self.masks[:self.T], self.max_new)).to(DEV), out, ls, ws, stream=stream)
+        torch.cuda.synchronize()
+        return out, ls
+
+    def reference(self):
+        return W.attention(f64(self.q), f64(self.K), f64(self.V), self.hq, self.ptab, self.L, self.tab, self.kv, self.start, self.page,
+                           self.masks, self.scale or None)
+
+
+TREES = {k: v for k, v in KERNELS.items() if max(v[0]) <= 256}
+
+
+@pytest.mark.parametrize("masks", ("trees", "any"))
+@pytest.mark.parametrize("hd", (64, 128))
+@pytest.mark.parametrize("name", sorted(TREES))
+def test_tree_attention_kernels(name, hd, masks):
+    new, kv, L, hq, hk = TREES[name]
+    print("trees", name, hd, masks, flush=True)
+    TreeBatch(len(name) + hd, new, kv, L, hq, hk, hd, 16 if hd == 64 else 64, pad=2, masks=masks).check()
+
+
+@pytest.mark.parametrize("name", sorted(k for k in ATTN if max(ATTN[k]["new"]) <= 256))
+def test_tree_attention(name):
+    print("trees", name, ATTN[name], flush=True)
+    TreeBatch(len(name), **ATTN[name]).check()
+
+
+# trees that begin and end everywhere in a block of 32 and a stage of 64 keys
+@pytest.mark.parametrize("hd, hq", [(64, 1), (128, 2), (64, 4), (128, 8)])
+@pytest.mark.parametrize("n", (1, 2, 7, 16, 31, 32, 33, 63, 64, 65, 100, 129, 255, 256))
+def test_tree_attention_of_every_size_and_place(n, hd, hq):
+    old = [0, 1, 31, 32, 63, 64, 65, 97]
+    TreeBatch(n, [n] * len(old), [n + o for o in old], 0, hq, 1, hd, 16, masks="any" if n % 2 else "trees").check()
+
+
+@pytest.mark.parametrize("name", ("along-one", "along-two", "along-wide", "one-one", "two-two", "wide-wide", "wide-two", "parts-own"))
+def test_a_chain_sees_what_causal_rows_see(name):
+    """Within the bounds of both (the same kernels, and so the same bits where the plan is the same)."""
+    new, kv, L, hq, hk = TREES[name]
+    b = TreeBatch(3, new, kv, L, hq, hk, 64, 16, masks="chains")
+    out, lse = b.run()
+    want, wl = Batch.run(b)
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+def test_tree_attention_without_starts_pitches_and_scale():
+    b = TreeBatch(1, [1] * 9, [4, 0, 17, 60, 33, 1, 16, 100, 12], 40, 4, 2, 64, 16, pad=3, ldq=4 * 64 + 24, ldo=4 * 64 + 8, scale=0.3)
+    a, la = b.check()
+    c, lc = b.check(start=False)
+    assert torch.equal(a, c) and torch.equal(la, lc)
+    d, _ = b.run(lse=False)
+    assert torch.equal(a, d)
+
+
+def test_tree_attention_bounds_above_the_lengths():
+    kw = dict(new=[1, 3, 2], kv=[20, 65, 2], L=50, hq=4, hk=2, hd=64, page=16)
+    for extra in (dict(max_kv=3000), dict(max_new=200), dict(max_kv=1000, max_new=256)):
+        TreeBatch(7, **kw, **extra).check()
+
+
+@pytest.mark.parametrize("max_kv", (3, 20, 40, 57))
+def test_tree_attention_of_keys_past_max_kv(max_kv):
+    """Tokens past max_kv are not seen, the tree's own among them."""
+    b = TreeBatch(3, [20, 9], [60, 30], 0, 2, 2, 64, 16, masks="any")
+    ref, rl, w = W.attention(f64(b.q), f64(b.K), f64(b.V), 2, [], 0, b.tab, b.kv, b.start, 16, b.masks, max_kv=max_kv)
+    b.max_kv = max_kv
+    b.tab = np.ascontiguousarray(b.tab[:, :-(-max_kv // 16)])
+    out, lse = b.run()
+    assert (np.abs(f64(out) - ref) <= R.attention_bound(ref, w, 60)).all()
+    fin = np.isfinite(rl)
+    assert (np.isneginf(f64(lse)) == ~fin).all() and (np.abs(f64(lse) - np.where(fin, rl, 0))[fin] <= R.lse_bound(rl[fin], 60)).all()
+
+
+def test_tree_attention_rows_past_max_new_are_left():
+    b = TreeBatch(4, [20, 9], [60, 30], 30, 2, 2, 64, 16)
+    ref, _, w = b.reference()
+    b.max_new = 12
+    out, _ = b.run()
+    keep = list(range(12)) + list(range(20, 29))
+    assert (out[12:20] == 7).all()
+    assert (np.abs(f64(out) - ref) <= R.attention_bound(ref, w, 90))[keep].all()
+
+
+@pytest.mark.parametrize("hd", (64, 128))
+@pytest.mark.parametrize("name, new, kv, L, rows", [("one", [2, 5], [9, 40], 0, 4), ("two", [5, 20], [9, 40], 1300, 12), ("wide", [30, 90], [60, 300], 0, 75),
+                                                    ("past", [4, 9, 2], [4, 20, 2], 20, 4)])
+def test_trees_of_a_batch_cut_at_its_rows(name, new, kv, L, rows, hd):
+    """Nodes that have no row are still counted, and are in the cache for the rows that name them."""
+    b = TreeBatch(30 + hd, new, kv, L, 2, 2, hd, 16, masks="any")
+    ref, rl, w = b.reference()
+    b.T, b.q = rows, b.q[:rows].contiguous()
+    out, lse = b.run()
+    keys = L + max(kv)
+    assert (np.abs(f64(out) - ref[:rows]) <= R.attention_bound(ref, w, keys)[:rows]).all()
+    fin = np.isfinite(rl[:, :rows])
+    assert (np.abs(f64(lse) - np.where(fin, rl[:, :rows], 0))[fin] <= R.lse_bound(rl[:, :rows][fin], keys)).all()
+
+
+@pytest.mark.parametrize("value", (math.inf, -math.inf, math.nan))
+@pytest.mark.parametrize("new, hq", [([3, 5], 1), ([20, 9], 1), ([70, 30], 2)])
+@pytest.mark.parametrize("hd", (64, 128))
+def test_nodes_that_a_row_does_not_see_do_not_reach_it(new, hq, hd, value):
+    """K and V of one node not finite: rows whose masks leave it out keep their bits."""
+    b = TreeBatch(11, new, [n + 37 for n in new], 20, hq, 1, hd, 16)
+    want, wl = b.run()
+    for r, j in ((0, 1), (1, 0), (1, new[1] - 1), (0, new[0] // 2)):
+        token = 37 + j
+        page, at = int(b.tab[r, token // 16]), token % 16
+        for c in (b.K, b.V):
+            keep = c[page, :, at].clone()
+            c[page, :, at] = value
+            out, lse = b.run()
+            hidden = [t for t in range(b.T) if not (b.start[r] <= t < b.start[r + 1] and b.masks[t] >> j & 1)]
+            assert torch.equal(out[hidden], want[hidden]) and torch.equal(lse[:, hidden], wl[:, hidden])
+            seen = [t for t in range(b.T) if t not in hidden]
+            if c is b.V and not math.isnan(value):
+                assert (out[seen] == value).all()
+            elif math.isnan(value):
+                assert torch.isnan(out[seen]).all()
+            c[page, :, at] = keep
+
+
+@pytest.mark.parametrize("bad", (-1, 10 ** 6, 2 ** 31 - 1, -2 ** 31))
+@pytest.mark.parametrize("new, hq", [([3, 5], 1), ([20, 9], 1), ([70, 30], 2)])
+def test_trees_over_missing_pages(new, hq, bad):
+    b = TreeBatch(12, new, [n + 100 for n in new], 40, hq, 1, 64, 16, masks="any")
+    b.tab[0, 1], b.tab[1, 100 // 16], b.tab[0, -(-b.kv[0] // 16) - 1] = bad, bad, bad
+    b.check()
+
+
+def test_tree_attention_past_4_gib():
+    """Pages of a cache of more than 2^32 bytes, at its far end."""
+    page, hk, hd = 128, 8, 128
+    pages = (1 << 32) // (page * hk * hd * 2) + 40
+    for new, kv in (([4], [300]), ([24], [300]), ([60], [300])):
+        b = TreeBatch(13, new, kv, 0, hk, hk, hd, page)
+        K, V = (torch.zeros((pages, hk, page, hd), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        far = [pages - 1 - i for i in range(b.K.shape[0])]
+        for big, small in ((K, b.K), (V, b.V)):
+            big[far] = small
+        want, wl = b.run()
+        b.tab = np.where(b.tab >= 0, pages - 1 - b.tab, b.tab)
+        b.K, b.V = K, V
+        out, lse = b.run()
+        assert torch.equal(out, want) and torch.equal(lse, wl)
+        del K, V
+        b.K = b.V = None
+
+
+def test_tree_attention_does_not_depend_on_the_workspace_s_contents_or_the_run():
+    b = TreeBatch(9, [3, 1, 20], [50, 600, 20], 700, 8, 2, 128, 16, pad=5)
+    a = b.run(ws_fill=0)
+    for fill in (0xFF, 0x7F, 0):
+        c = b.run(ws_fill=fill)
+        assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+
+# ---------------------------------------------------------------------------
+# logits
+# ---------------------------------------------------------------------------
+
+class Rows:
+    """Logits of a step and the rules on them, each left out where its name is in `without`."""
+
+    def __init__(self, seed, rows, V, dtype, max_hist=60, n_bias=9, max_new=None, pad=0, lead=0, ldl=0, ldo=0, lda=0, without=(), states=5):
+        rng = np.random.default_rng(seed)
+        n = len(rows)
+        self.start = [lead]
+        for x in rows:
+            self.start.append(self.start[-1] + x)
+        self.T, self.V, self.dtype = self.start[-1] + pad, V, dtype
+        self.max_new = max(list(rows) + [1]) if max_new is None else max_new
+        self.l = rand(seed, (self.T, V), dtype, 3.0)
+        token = lambda *s: np.where(rng.random(s) < 0.1, rng.choice([-1, V, 2 ** 31 - 1, -2 ** 31], s), rng.integers(0, min(V, 40), s) ** 2 % V)
+        self.u = dict(history=token(n, max_hist), prompt_len=rng.integers(-2, max_hist + 3, n), hist_len=rng.integers(-2, max_hist + 3, n),
+                      draft=token(self.T), repetition=np.float32(rng.choice([0.7, 1.0, 1.3], n)), presence=np.float32(rng.choice([0, 0.5, -0.25], n)),
+                      frequency=np.float32(rng.choice([0, 0.4, 1.5], n)), bias_token=token(n * n_bias), bias=np.float32(rng.standard_normal(n * n_bias) * 4),
+                      bias_start=np.concatenate([[-1 if seed % 2 else 0], np.sort(rng.integers(0, n * n_bias + 3, n))]),
+                      allowed=rng.integers(0, 2 ** 32, (states, lda or -(-V // 32)), dtype=np.uint32), allowed_row=rng.integers(-1, states + 1, self.T))
+        self.masks = [0] * self.T
+        for r, k in enumerate(rows):
+            parent = W.random_tree(rng, k)
+            for i in range(k):
+                t = self.start[r] + i
+                self.masks[t] = (1 << i | (self.masks[self.start[r] + parent[i]] if parent[i] >= 0 else 0)) & (2 ** (64 * -(-self.max_new // 64)) - 1)
+        for k in without:
+            self.u.pop(k)
+        if "bias_start" in without:
+            self.u.pop("bias", None), self.u.pop("bias_token", None)
+        self.ldl, self.ldo, self.lda, self.max_hist, self.n = ldl, ldo, lda, max_hist, n
+
+    def tensors(self):
+        u = {k: torch.from_numpy(v.view(np.int32).copy()).to(DEV) if k == "allowed" else torch.from_numpy(v).to(DEV) if v.dtype == np.float32 else i32(v)
+             for k, v in self.u.items()}
+        if "draft" in u:
+            u["mask"] = torch.from_numpy(W.words(self.masks, self.max_new)).to(DEV)
+        return u
+
+    def desc(self, ldl=None, ldo=None):
+        u = self.u
+        return cola.logits_desc(self.T, self.V, self.n, self.max_hist, self.max_new, self.dtype, len(u.get("bias", ())), len(u.get("allowed", ())),
+                                self.ldl if ldl is None else ldl, self.ldo if ldo is None else ldo, self.lda)
+
+    def run(self, start=True, in_place=False, stream=None):
+        l = pitched(self.l, self.ldl, 1)[0] if self.ldl else self.l.clone()
+        out, buf = pitched(torch.full_like(self.l, 7.0), self.ldo, 3, fill=7.0) if self.ldo else (torch.full_like(self.l, 7.0), None)
+        d = self.desc()
+        if in_place:
+            out, buf, d = l, None, self.desc(self.ldl, self.ldl)
+        cola.logits_adjust(d, cola.logits_rules(**self.tensors()), l, i32(self.start) if start else None, out, stream=stream)
+        torch.cuda.synchronize()
+        if buf is not None:
+            assert (buf == 7).sum() >= buf.numel() - out.numel(), "the padding is left"
+        return out
+
+    def check(self, **kw):
+        out = self.run(**kw)
+        kwargs = dict(self.u)
+        if "draft" in kwargs:
+            kwargs["masks"] = self.masks
+        ref, bound, touched = W.logits(f64(self.l), self.start, self.V, dtype=self.dtype, **kwargs)
+        got, lo, hi = f64(out), self.start[0], self.start[-1]
+        left = self.l if kw.get("in_place") else torch.full_like(self.l, 7.0)
+        for x in (slice(0, lo), slice(hi, self.T)):
+            assert torch.equal(out[x], left[x]), "rows of no request are left"
+        got, ref, bound, touched = got[lo:hi], ref[lo:hi], bound[lo:hi], touched[lo:hi]
+        assert (np.isneginf(got) == np.isneginf(ref)).all()
+        fin = np.isfinite(ref)
+        err = np.abs(got - np.where(fin, ref, 0))
+        assert (err[fin] <= bound[fin]).all(), (err[fin] / bound[fin]).max()
+        same = torch.from_numpy(~touched).to(DEV)
+        assert torch.equal(out[lo:hi][same], self.l[lo:hi][same]), "what no rule touches keeps its bits"
+        return out
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("V", (1, 7, 31, 32, 33, 1000, 2048, 2049, 8191, 8192, 8193, 20011))
+def test_logits(V, dtype):
+    Rows(V, [3, 1, 0, 5], V, dtype, pad=2, lead=1).check()
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_logits_pitches_and_in_place(dtype):
+    r = Rows(2, [2, 3], 4999, dtype, ldl=5003, ldo=5010, lda=160)
+    a = r.check()
+    b = r.check(in_place=True)
+    assert torch.equal(a, b)
+    r.ldl = r.ldo = 0
+    assert torch.equal(a, r.check()) and torch.equal(a, r.check(in_place=True))
+
+
+@pytest.mark.parametrize("without", [("draft",), ("history", "hist_len"), ("prompt_len",), ("repetition",), ("presence", "frequency"), ("bias_start",),
+                                     ("allowed",), ("allowed_row",), ("repetition", "presence", "frequency"), ("hist_len", "draft"),
+                                     ("repetition", "presence", "frequency", "bias_start", "allowed"), ("draft", "bias_start", "allowed"),
+                                     ("bias_start", "history", "hist_len", "allowed", "allowed_row")], ids=str)
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_logits_without_some_rules(without, dtype):
+    # hist_len without prompt_len: all of it is the answer
+    Rows(len(without) + 5, [4, 2], 3001, dtype, without=without, states=7).check()
+
+
+def test_logits_of_single_rows_without_starts():
+    r = Rows(4, [1] * 70, 1500, "f32", max_new=1, pad=3)
+    assert torch.equal(r.check(), r.check(start=False))
+    r = Rows(4, [1] * 70, 1500, "bf16", max_new=0, without=("draft",))
+    assert torch.equal(r.check(), r.check(start=False))
+
+
+@pytest.mark.parametrize("rows, max_hist", [([256, 1, 100], 5), ([65, 64, 63], 3000), ([1] * 300, 9), ([0] * 70 + [2] * 5 + [0] * 200 + [1], 40), ([20], 20000)])
+def test_logits_of_many_rows_and_long_histories(rows, max_hist):
+    Rows(len(rows), rows, 700, "f32", max_hist=max_hist).check()
+
+
+def test_logits_of_one_token_many_times():
+    """Whole counts, whatever the order of their additions: 30000 of one token."""
+    r = Rows(6, [2], 300, "f32", max_hist=30000, without=("bias_start", "allowed", "draft"))
+    r.u["history"][:] = 17
+    r.u["prompt_len"][:], r.u["hist_len"][:] = 0, 30000
+    r.u["repetition"][:], r.u["frequency"][:], r.u["presence"][:] = 1.0, 2.0, 0.5
+    out = r.run()
+    assert (np.abs(f64(out)[:, 17] - (f64(r.l)[:, 17] - 60000.5)) <= 2.0 ** -7).all()
+    out[:, 17] = r.l[:, 17]
+    assert torch.equal(out, r.l)
+
+
+def test_logits_that_are_not_numbers():
+    """A grammar that allows nothing; infinities and NaN where they are allowed, and where not."""
+    r = Rows(7, [3], 100, "f32", without=("draft", "bias_start"))
+    r.u["allowed_row"][:] = [0, 1, 2]
+    r.u["allowed"][0], r.u["allowed"][1], r.u["allowed"][2] = 0, 0xFFFFFFFF, 0x55555555
+    r.l[:, 40] = math.nan
+    r.l[:, 41] = math.inf
+    r.l[:, 42] = -math.inf
+    out = r.run()
+    assert torch.isneginf(out[0]).all()
+    assert torch.isnan(out[1, 40]) and out[1, 41] == math.inf and out[1, 42] == -math.inf and torch.isnan(out[1]).sum() == 1
+    assert torch.isnan(out[2, 40]) and torch.isneginf(out[2, 41::2]).all() and torch.isnan(out[2]).sum() == 1
+
+
+def test_logits_do_not_depend_on_the_run():
+    r = Rows(8, [40, 33, 50], 50021, "bf16", max_hist=4000, n_bias=100)
+    a = r.run()
+    for _ in range(3):
+        assert torch.equal(a, r.run())
+
+
+def test_logits_past_4_gib():
+    """Rows past 2^32 bytes: the bits that they get alone."""
+    V, T = 1 << 20, 2050
+    l = torch.zeros((T, V), dtype=torch.bfloat16, device=DEV)
+    l[-2:] = rand(1, (2, V), "bf16")
+    d = lambda T: cola.logits_desc(T, V, T, 8, 0, "bf16")
+    u = dict(history=i32([[5, 6, V - 1, 5, 70000, 3, 2, 1]]), hist_len=i32([8]), repetition=torch.full((1,), 1.3, device=DEV),
+             presence=torch.full((1,), 0.5, device=DEV))
+    many = {k: v.repeat(T, *[1] * (v.dim() - 1)) for k, v in u.items()}
+    want = torch.empty((1, V), dtype=torch.bfloat16, device=DEV)
+    cola.logits_adjust(d(1), cola.logits_rules(**u), l[-1:].clone(), None, want)
+    last = l[-2].clone()
+    cola.logits_adjust(d(T), cola.logits_rules(**many), l, None, l)
+    assert torch.equal(l[-1:], want) and not torch.equal(l[-2], last) and l[1000, 5] == -0.5 and l[1000, 9] == 0
