@@ -1,13 +1,17 @@
 // logits.hip -- penalties for repeated tokens, biases and grammar masks on the logits
 // of a step (cola_logits_adjust).
 //
-// HBM bound: each logit is read once and written once, and few are changed.  A workgroup
-// takes a chunk of the vocabulary for a run of rows: it counts the chunk's tokens in
-// the request's history in LDS (whole numbers, so that the order of the additions does
-// not matter), keeps the last bias of each token beside the counts, and sends the
-// rows through, 16 bytes a load.  The rows of one request share the counts; each adds
-// its own drafted tokens before its pass and takes them back after it.  A row's logits
-// are on their way to registers while the history is read.
+// HBM bound: each logit is read once and written once.  A workgroup takes a chunk of the
+// vocabulary for a run of rows.  It counts the chunk's tokens in the request's history
+// in LDS (whole numbers, so that the order of the additions does not matter) and turns
+// the counts into what each logit gets: y = x f + shift, f = 1, or for tokens that were
+// seen 1 / repetition or repetition by x's sign, and shift = bias - (frequency c +
+// presence), -0 where there is nothing to add.  Then the rows go through without a
+// branch for a logit, 16 bytes a load, a row ahead of the arithmetic.  The rows of one
+// request share all that but for the drafted tokens: for each of those in the chunk a
+// lane counts the nodes of the row's path that drafted it (the bits that two masks
+// share) and writes the token's shift anew.  A wave has a part of the chunk to itself,
+// so that no wave waits for another between the rows.
 #include "rows.hpp"
 #include "serve.hpp"
 
@@ -16,13 +20,11 @@ namespace {
 
 constexpr int NTHR = 256;
 constexpr uint32_t kPrompt = 0x80000000u;               // in a count: the token is in the prompt
+constexpr int kMaxRows = 16;                            // rows of a workgroup
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef i32x4 loose4 __attribute__((aligned(4)));
-
-struct LogitsGrid {
-    int rows;                                           // rows of a workgroup
-};
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Largest r with start[r] <= t, or -1 (n entries that do not fall), by all lanes of a wave.
 __device__ __forceinline__ int owner(const int32_t* start, int n, int64_t t) {
@@ -36,29 +38,99 @@ __device__ __forceinline__ int owner(const int32_t* start, int n, int64_t t) {
         lo += k;
         len = min(step, len - k);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
-template <bool BF16, int NVEC>
-__global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const LogitsGrid g) {
-    constexpr int PV = BF16 ? 8 : 4, C = NTHR * PV * NVEC;
+// LDS: a count, then a shift, for each token of the chunk; a bit for each that was seen;
+// with biases the last entry of each token; with drafted tokens their nodes.
+constexpr size_t lds_bytes(int C, bool biases, int words) {
+    return 4 * C + C / 8 + 16 + (biases ? 4 * C : 0) + 64 * words * 8 * (words + 2);
+}
+
+// A token that the request drafted: its place in the chunk (-1: another entry has it), the
+// shift that it has without the row's path, and whether the history and the answer
+// have it.
+struct Draft {
+    int32_t place;
+    float shift;
+    uint32_t seen, answer;
+};
+
+// PV NVEC elements of a row to a thread; PAST: results past the caches.
+template <bool BF16, int NVEC, bool PAST>
+__global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const int rows, const int chunks, const int64_t base) {
+    constexpr int PV = BF16 ? 8 : 4, CW = 64 * PV * NVEC, C = CW * NTHR / 64;
+    constexpr int AHEAD = 2;                            // of the history, 4 tokens each, on their way before its length is known
     typedef Vec<BF16, PV> V;
     typedef typename V::E E;
     typedef typename V::G G;
-    extern __shared__ uint32_t count[];                 // [C], then (with biases) the last entry of each token
-    int32_t* last = reinterpret_cast<int32_t*>(count) + C;
-    const int tid = threadIdx.x;
-    const int64_t c0 = (int64_t)blockIdx.x * C;
+    extern __shared__ __attribute__((aligned(16))) uint32_t count[];
+    float* shift = reinterpret_cast<float*>(count);
+    uint32_t* seen = count + C;                         // [C / 32], and a word past the end
+    uint64_t* nodes = reinterpret_cast<uint64_t*>(seen + C / 32 + 4);
+    Draft* drafts = reinterpret_cast<Draft*>(nodes + 64 * a.words * a.words);
+    uint32_t* last = reinterpret_cast<uint32_t*>(drafts + 64 * a.words);
+    __shared__ int n_drafts;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t group = (base + blockIdx.x) / chunks;
+    const int64_t c0 = (base + blockIdx.x - group * chunks) * C;
     const int width = (int)min(a.V - c0, (int64_t)C);
-    const int64_t t0 = (int64_t)blockIdx.y * g.rows, t1 = min(t0 + g.rows, a.T);
+    // this wave's part of the chunk
+    const int v0 = CW * wave, wide = min(max(width - v0, 0), CW);
+    const int64_t t0 = group * rows;
+    const int n_rows = (int)min((int64_t)rows, a.T - t0);
     const bool repeats = a.repetition || a.presence || a.frequency;
-    const bool biases = a.bias_start != nullptr;
-    const bool drafted = repeats && a.draft;
-    int r = a.start ? owner(a.start, a.n_req, t0) : (int)t0;
-    int held = -1;                                      // the request whose counts are in LDS
-    uint32_t mine = 0;                                  // this thread's node in the counts: its place + 1
+    const bool biases = a.bias_start != nullptr, changes = repeats || biases, drafted = repeats && a.draft;
 
-    for (int64_t t = t0; t < t1; ++t) {
+    // A row: `head` logits up to where out is aligned, vectors, and what is left, with a
+    // lane for each that no vector has.
+    struct Row {
+        V x[NVEC];
+        Vec<BF16, 1> edge;
+        uint32_t ok[NVEC], edge_ok;                     // bits of the allowed tokens
+        int head, full;
+        __device__ __forceinline__ int at(int k, int lane) const { return head + (64 * k + lane) * PV; }
+        __device__ __forceinline__ int edge_at(int lane) const { return lane < head ? lane : full + lane - head; }
+    };
+    // lane i has row i's place among the masks
+    int64_t state = -1;
+    if (a.allowed && lane < n_rows) state = a.allowed_row ? (int64_t)a.allowed_row[t0 + lane] : t0 + lane;
+    if (state >= a.n_allowed) state = -1;
+    auto load = [&](Row& w, int i) __attribute__((always_inline)) {
+        const E* from = (const E*)a.logits + (t0 + i) * a.ldl + c0 + v0;
+        const uint32_t off = (uint32_t)(uintptr_t)((E*)a.out + (t0 + i) * a.ldo + c0 + v0) / sizeof(E) % PV;
+        w.head = __builtin_amdgcn_readfirstlane(min((int)(off ? PV - off : 0), wide));
+        w.full = w.head + (wide - w.head) / PV * PV;
+        const int s = __builtin_amdgcn_readlane((int)state, i);
+        const uint32_t* bits = a.allowed + s * a.lda + ((c0 + v0) >> 5);
+#pragma unroll
+        for (int k = 0; k < NVEC; ++k) {
+            const int v = w.at(k, lane);
+            w.ok[k] = ~0u;
+            if (v >= w.full) continue;
+            w.x[k].load(from + v);
+            if (s >= 0) {
+                const uint32_t lo = bits[v >> 5], hi = bits[(v + PV - 1) >> 5];
+                w.ok[k] = (uint32_t)(((uint64_t)hi << 32 | lo) >> (v & 31));
+            }
+        }
+        const int v = w.edge_at(lane);
+        w.edge_ok = 1;
+        if (lane < w.head + wide - w.full) {
+            w.edge.load(from + v);
+            if (s >= 0) w.edge_ok = bits[v >> 5] >> (v & 31);
+        }
+    };
+    Row next;
+    load(next, 0);
+
+    int r = a.start ? owner(a.start, a.n_req, t0) : (int)t0;
+    int held = -1;                                      // the request whose shifts are in LDS
+    float rep = 1.0f, inv = 1.0f, pres = 0.0f, freq = 0.0f;
+    for (int i = 0; i < n_rows; ++i) {
+        const int64_t t = t0 + i;
+        Row now = next;
+        if (i + 1 < n_rows) load(next, i + 1);
         if (a.start) {
             if (r < 0 && a.start[0] <= t) r = owner(a.start, a.n_req, t);
             while (r >= 0 && r < a.n_req && a.start[r + 1] <= t) ++r;
@@ -68,32 +140,42 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
         }
         if (r >= a.n_req) break;
 
-        // this row's logits on their way
-        const E* from = (const E*)a.logits + t * a.ldl + c0;
-        V x[NVEC];
+        if (r != held && changes) {
+            const int32_t* h = a.history + (int64_t)r * a.max_hist;
+            const bool counted = repeats && a.hist_len;
+            i32x4 first[AHEAD];
+            if (counted) {
 #pragma unroll
-        for (int k = 0; k < NVEC; ++k) {
-            const int v = (k * NTHR + tid) * PV;
-            if (v + PV <= width) x[k].load(from + v);
-        }
-        float rep = 1.0f, pres = 0.0f, freq = 0.0f;
-        if (a.repetition) rep = a.repetition[r];
-        if (a.presence) pres = a.presence[r];
-        if (a.frequency) freq = a.frequency[r];
-
-        const bool fresh = r != held;
-        if (fresh && (repeats || biases)) {
-            if (held >= 0) __syncthreads();             // the row before has read its counts
-            for (int i = tid; i < C; i += NTHR) {
-                count[i] = 0;
-                if (biases) last[i] = -1;
+                for (int k = 0; k < AHEAD; ++k)
+                    if (4 * (k * NTHR + tid) + 4 <= a.max_hist) first[k] = *reinterpret_cast<const loose4*>(h + 4 * (k * NTHR + tid));
             }
-            mine = 0;
+            int64_t end = 0, past = 0, lo = 0, hi = 0;
+            if (counted) end = min(max((int64_t)a.hist_len[r], (int64_t)0), a.max_hist);
+            if (counted && a.prompt_len) past = min(max((int64_t)a.prompt_len[r], (int64_t)0), end);
+            if (biases) {
+                lo = min(max((int64_t)a.bias_start[r], (int64_t)0), a.n_bias);
+                hi = min(max((int64_t)a.bias_start[r + 1], lo), a.n_bias);
+            }
+            if (a.repetition) rep = a.repetition[r];
+            if (a.presence) pres = a.presence[r];
+            if (a.frequency) freq = a.frequency[r];
+            // this thread's node, where the chunk has its token
+            int place = -1;
+            if (drafted) {
+                const int64_t n0 = a.start ? max((int64_t)a.start[r], (int64_t)0) : t, n1 = a.start ? min((int64_t)a.start[r + 1], a.T) : t + 1;
+                if (tid < 64 * a.words && n0 + tid < n1) {
+                    const int64_t at = (int64_t)a.draft[n0 + tid] - c0;
+                    if (at >= 0 && at < width) place = (int)at;
+                }
+            }
+            if (held >= 0) __syncthreads();             // the request before has read its shifts
+            for (int j = 4 * tid; j < C; j += 4 * NTHR) {
+                *reinterpret_cast<u32x4*>(count + j) = u32x4{0, 0, 0, 0};
+                if (biases) *reinterpret_cast<u32x4*>(last + j) = u32x4{0, 0, 0, 0};
+            }
+            if (tid == 0) n_drafts = 0;
             __syncthreads();
-            if (repeats && a.hist_len) {
-                const int64_t end = min(max((int64_t)a.hist_len[r], (int64_t)0), a.max_hist);
-                const int64_t past = a.prompt_len ? min(max((int64_t)a.prompt_len[r], (int64_t)0), end) : 0;
-                const int32_t* h = a.history + r * a.max_hist;
+            if (counted) {
                 auto note = [&](int32_t token, int64_t j) __attribute__((always_inline)) {
                     const int64_t at = (int64_t)token - c0;
                     if (at >= 0 && at < width) {
@@ -101,113 +183,167 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
                         else atomicAdd(&count[at], 1u);
                     }
                 };
-                int64_t j = 4 * tid;
-                for (; j + 4 <= end; j += 4 * NTHR) {
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int64_t j = 4 * (k * NTHR + tid);
+                    if (j + 4 <= end) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) note(first[k][e], j + e);
+                    }
+                }
+                for (int64_t j = 4 * (AHEAD * NTHR + tid); j + 4 <= end; j += 4 * NTHR) {
                     const i32x4 y = *reinterpret_cast<const loose4*>(h + j);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) note(y[i], j + i);
+                    for (int e = 0; e < 4; ++e) note(y[e], j + e);
                 }
-                for (; j < end; ++j) note(h[j], j);
+                if (tid < (end & 3)) note(h[(end & ~int64_t(3)) + tid], (end & ~int64_t(3)) + tid);
             }
-            if (biases) {
-                const int64_t lo = min(max((int64_t)a.bias_start[r], (int64_t)0), a.n_bias);
-                const int64_t hi = min(max((int64_t)a.bias_start[r + 1], lo), a.n_bias);
-                for (int64_t j = lo + tid; j < hi; j += NTHR) {
-                    const int64_t at = (int64_t)a.bias_token[j] - c0;
-                    if (at >= 0 && at < width) atomicMax(&last[at], (int32_t)j);
-                }
+            // the last entry of each token, by its place in the list + 1
+            for (int64_t j = lo + tid; j < hi; j += NTHR) {
+                const int64_t at = (int64_t)a.bias_token[j] - c0;
+                if (at >= 0 && at < width) atomicMax(&last[at], (uint32_t)j + 1);
             }
-            held = r;
-            if (!drafted) __syncthreads();
-        }
-        if (drafted) {
-            // the drafted tokens that this row sees, in place of those of the row before
-            if (!fresh) __syncthreads();
-            if (mine) atomicSub(&count[mine - 1], 1u);
-            mine = 0;
-            const int64_t lo = a.start ? max((int64_t)a.start[r], (int64_t)0) : t, hi = a.start ? min((int64_t)a.start[r + 1], a.T) : t + 1;
-            if (tid < 64 * a.words && lo + tid < hi && (a.mask[t * a.words + (tid >> 6)] >> (tid & 63) & 1)) {
-                const int64_t at = (int64_t)a.draft[lo + tid] - c0;
-                if (at >= 0 && at < width) {
-                    mine = (uint32_t)at + 1;
-                    atomicAdd(&count[at], 1u);
-                }
+            int mine = -1;
+            if (place >= 0) {
+                mine = atomicAdd(&n_drafts, 1);
+                drafts[mine] = Draft{place, 0.0f, (uint32_t)tid, 0};
             }
             __syncthreads();
-        }
-        const uint32_t* ok = nullptr;
-        if (a.allowed) {
-            const int64_t s = a.allowed_row ? (int64_t)a.allowed_row[t] : t;
-            if (s >= 0 && s < a.n_allowed) ok = a.allowed + s * a.lda + (c0 >> 5);
-        }
-        auto adjust = [&](float y, int v) __attribute__((always_inline)) {
-            if (repeats) {
-                const uint32_t n = count[v];
-                if (n != 0) {
-                    y = y > 0.0f ? y / rep : y * rep;
-                    const uint32_t c = n & ~kPrompt;
-                    if (c != 0) y = y - freq * (float)c - pres;
+            if (drafted) {
+                // The nodes that drafted this thread's token; the first of them keeps it.
+                const int n = n_drafts;
+                bool keep = mine >= 0;
+                uint32_t held_count = 0;
+                if (mine >= 0) {
+                    held_count = count[place];
+                    for (int w = 0; w < a.words; ++w) {
+                        uint64_t m = 0;
+                        for (int j = 0; j < n; ++j) {
+                            const Draft d = drafts[j];
+                            if (d.place != place) continue;
+                            if ((int)d.seen < tid) keep = false;
+                            if ((int)(d.seen >> 6) == w) m |= uint64_t(1) << (d.seen & 63);
+                        }
+                        nodes[mine * a.words + w] = m;
+                    }
                 }
+                __syncthreads();
+                if (mine >= 0) drafts[mine] = Draft{keep ? place : -1, 0.0f, held_count != 0, (held_count & ~kPrompt) != 0};
             }
-            if (biases && last[v] >= 0) y += a.bias[last[v]];
-            return y;
+            inv = 1.0f / rep;
+            for (int j = 8 * tid; j < C; j += 8 * NTHR) {
+                uint32_t f = 0;
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    u32x4 n = *reinterpret_cast<const u32x4*>(count + j + e), m = {0, 0, 0, 0};
+                    if (biases) m = *reinterpret_cast<const u32x4*>(last + j + e);
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const uint32_t c = n[z] & ~kPrompt;
+                        f |= (uint32_t)(n[z] != 0) << (e + z);
+                        float y = m[z] ? a.bias[m[z] - 1] : -0.0f;
+                        if (c != 0) y -= fmaf(freq, (float)c, pres);
+                        n[z] = __float_as_uint(y);
+                    }
+                    *reinterpret_cast<u32x4*>(count + j + e) = n;
+                }
+                reinterpret_cast<uint8_t*>(seen)[j / 8] = (uint8_t)f;
+            }
+            __syncthreads();
+            if (drafted) {
+                if (mine >= 0) drafts[mine].shift = shift[place];
+                __syncthreads();
+            }
+            held = r;
+        }
+        if (drafted && n_drafts > 0) {
+            const uint64_t* mask = a.mask + t * a.words;
+            for (int j = lane; j < n_drafts; j += 64) {
+                const Draft d = drafts[j];
+                if (d.place < 0 || d.place / CW != wave) continue;
+                int c = 0;
+                for (int w = 0; w < a.words; ++w) c += __popcll(nodes[j * a.words + w] & mask[w]);
+                shift[d.place] = c != 0 ? d.shift - fmaf(freq, (float)c, d.answer ? 0.0f : pres) : d.shift;
+                const uint32_t bit = 1u << (d.place & 31);
+                if (c != 0 || d.seen) atomicOr(&seen[d.place >> 5], bit);
+                else atomicAnd(&seen[d.place >> 5], ~bit);
+            }
+            // the wave's own lanes read what it wrote
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+        auto adjust = [&](float y, float add, bool was) __attribute__((always_inline)) {
+            return fmaf(y, was ? (y > 0.0f ? inv : rep) : 1.0f, add);
         };
-        G to = (G)a.out + t * a.ldo + c0;
+        G to = (G)a.out + t * a.ldo + c0 + v0;
 #pragma unroll
         for (int k = 0; k < NVEC; ++k) {
-            const int v = (k * NTHR + tid) * PV;
-            if (v + PV <= width) {
-                uint32_t any = 0;
+            const int v = now.at(k, lane);
+            if (v >= now.full) continue;
+            float y[PV];
+            now.x[k].get(y);
+            if (changes) {
+                const uint32_t* w = seen + ((v0 + v) >> 5);
+                const uint32_t was = (uint32_t)(((uint64_t)w[1] << 32 | w[0]) >> ((v0 + v) & 31));
 #pragma unroll
-                for (int e = 0; e < PV; ++e) {
-                    if (repeats) any |= count[v + e];
-                    if (biases) any |= (uint32_t)(last[v + e] + 1);
-                }
-                const uint32_t bits = ok ? ok[v >> 5] >> (v & 31) : ~0u;
-                if (any != 0 || (~bits & ((1u << PV) - 1)) != 0) {
-                    float y[PV];
-                    x[k].get(y);
-#pragma unroll
-                    for (int e = 0; e < PV; ++e) {
-                        if (any != 0) y[e] = adjust(y[e], v + e);
-                        if (!(bits >> e & 1)) y[e] = -INFINITY;
-                    }
-                    x[k].put(y);
-                }
-                x[k].template store<false>(to + v);
-            } else {
-                for (int e = v; e < width; ++e) {
-                    Vec<BF16, 1> z;
-                    z.load(from + e);
-                    float y[1];
-                    z.get(y);
-                    y[0] = adjust(y[0], e);
-                    if (ok && !(ok[e >> 5] >> (e & 31) & 1)) y[0] = -INFINITY;
-                    z.put(y);
-                    z.template store<false>(to + e);
-                }
+                for (int e = 0; e < PV; ++e) y[e] = adjust(y[e], shift[v0 + v + e], was >> e & 1);
             }
+            if (a.allowed) {
+#pragma unroll
+                for (int e = 0; e < PV; ++e) y[e] = now.ok[k] >> e & 1 ? y[e] : -INFINITY;
+            }
+            now.x[k].put(y);
+            now.x[k].template store<PAST>(to + v);
+        }
+        if (lane < now.head + wide - now.full) {
+            const int v = now.edge_at(lane);
+            float y[1];
+            now.edge.get(y);
+            if (changes) y[0] = adjust(y[0], shift[v0 + v], seen[(v0 + v) >> 5] >> ((v0 + v) & 31) & 1);
+            if (!(now.edge_ok & 1)) y[0] = -INFINITY;
+            now.edge.put(y);
+            now.edge.template store<false>(to + v);
         }
     }
 }
 
 template <bool BF16, int NVEC>
-hipError_t go(const LogitsArgs& a, const LogitsGrid& g, hipStream_t s) {
+hipError_t go(const LogitsArgs& a, int rows, bool past, hipStream_t s) {
     constexpr int C = NTHR * (BF16 ? 8 : 4) * NVEC;
     const bool repeats = a.repetition || a.presence || a.frequency;
-    const size_t lds = a.bias_start ? 8 * C : (repeats ? 4 * C : 0);
-    const int64_t gy = (a.T + g.rows - 1) / g.rows;
-    logits_kernel<BF16, NVEC><<<dim3((unsigned)((a.V + C - 1) / C), (unsigned)gy), NTHR, lds, s>>>(a, g);
-    return hipGetLastError();
+    const size_t lds = a.bias_start || repeats ? lds_bytes(C, a.bias_start, a.words) : 0;
+    const int chunks = (int)((a.V + C - 1) / C);
+    const int64_t blocks = (a.T + rows - 1) / rows * chunks, most = int64_t(1) << 23;
+    // more than a grid may have (2^32 threads) go into launches one after the other
+    for (int64_t base = 0; base < blocks; base += most) {
+        const unsigned grid = (unsigned)(blocks - base < most ? blocks - base : most);
+        if (past) logits_kernel<BF16, NVEC, true><<<grid, NTHR, lds, s>>>(a, rows, chunks, base);
+        else logits_kernel<BF16, NVEC, false><<<grid, NTHR, lds, s>>>(a, rows, chunks, base);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
 
 hipError_t launch_logits(bool bf16, const LogitsArgs& a, hipStream_t s) {
-    LogitsGrid g{};
-    g.rows = 1;
-    while ((a.T + g.rows - 1) / g.rows > 65535) g.rows *= 2;
-    return bf16 ? go<true, 4>(a, g, s) : go<false, 8>(a, g, s);
+    // Chunks as large as leave 1024 workgroups of one row, and rows to a workgroup (of one
+    // request, so as many as it may have) while there are 2048.
+    const int pv = NTHR * (bf16 ? 8 : 4), most = bf16 ? 2 : 4;
+    int nvec = 1;
+    while (nvec < most && a.T * ((a.V + 2 * pv * nvec - 1) / (2 * pv * nvec)) >= 1024) nvec *= 2;
+    const int64_t chunks = (a.V + pv * nvec - 1) / (pv * nvec);
+    int64_t rows = a.T * chunks / 2048;
+    const int64_t of_one = a.start ? (a.max_new > 1 ? a.max_new : 1) : 1;
+    if (rows > of_one) rows = of_one;
+    if (rows > kMaxRows) rows = kMaxRows;
+    if (rows < 1) rows = 1;
+    const bool past = (double)a.T * (double)a.V * (bf16 ? 2 : 4) > 48e6;
+    if (bf16) return nvec == 1 ? go<true, 1>(a, (int)rows, past, s) : go<true, 2>(a, (int)rows, past, s);
+    if (nvec == 1) return go<false, 1>(a, (int)rows, past, s);
+    return nvec == 2 ? go<false, 2>(a, (int)rows, past, s) : go<false, 4>(a, (int)rows, past, s);
 }
 
 }  // namespace cola

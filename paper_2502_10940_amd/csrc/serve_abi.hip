@@ -469,7 +469,7 @@ int cola_logits_adjust(const cola_logits_desc* d, const cola_logits_rules* rules
     return guarded([&]() -> int {
         if (!d || !rules || !dtype_ok(d->dtype) || d->reserved != 0) return COLA_ERR_INVALID_ARG;
         if (d->T < 0 || d->T > kMaxInt || d->V < 1 || d->V > kMaxPitch || d->n_req < 0 || d->n_req > 65535 || d->max_hist < 0 ||
-            d->max_hist > kMaxKeys || d->max_new < 0 || d->max_new > COLA_TREE_MAX || d->n_bias < 0 || d->n_bias > kMaxInt ||
+            d->max_hist >= kMaxKeys || d->max_new < 0 || d->max_new > COLA_TREE_MAX || d->n_bias < 0 || d->n_bias > kMaxInt ||
             d->n_allowed < 0 || d->n_allowed > kMaxInt)
             return COLA_ERR_BAD_SHAPE;
         LogitsArgs a{};
