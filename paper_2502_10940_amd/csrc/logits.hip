@@ -6,8 +6,9 @@
 // in LDS (whole numbers, so that the order of the additions does not matter) and turns
 // the counts into what each logit gets: y = x f + shift, f = 1, or for tokens that were
 // seen 1 / repetition or repetition by x's sign, and shift = bias - (frequency c +
-// presence), -0 where there is nothing to add.  Then the rows go through without a
-// branch for a logit, 16 bytes a load, a row ahead of the arithmetic.  The rows of one
+// presence), -0 where there is nothing to add.  Then the rows go through, 16 bytes a
+// load, a row ahead of the arithmetic; bits say which vectors anything happens to (a
+// wave that read every shift would meet eight lanes on each bank of LDS).  The rows of one
 // request share all that but for the drafted tokens: for each of those in the chunk a
 // lane counts the nodes of the row's path that drafted it (the bits that two masks
 // share) and writes the token's shift anew.  A wave has a part of the chunk to itself,
@@ -25,11 +26,27 @@ constexpr int kMaxRows = 16;                            // rows of a workgroup
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef i32x4 loose4 __attribute__((aligned(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t loose_u16 __attribute__((aligned(1)));
+
+// What a wave's loads go to where it has no logits.
+__device__ const uint32_t kNowhere[4] = {0, 0, 0, 0};
+// A load from global memory, said so: a pointer picked among several loses its space.
+template <class X>
+__device__ __forceinline__ X global(const void* p) {
+    return *(const __attribute__((address_space(1))) X*)p;
+}
+
+// An entry that is the same for a wave, of arrays that this kernel only reads: by the
+// scalar unit, so that no wait for it is one for the rows in flight.
+template <class X>
+__device__ __forceinline__ X entry(const X* p, int64_t i) {
+    return ((const __attribute__((address_space(4))) X*)p)[i];
+}
 
 // Largest r with start[r] <= t, or -1 (n entries that do not fall), by all lanes of a wave.
 __device__ __forceinline__ int owner(const int32_t* start, int n, int64_t t) {
     const int lane = threadIdx.x & 63;
-    if (start[0] > t) return -1;
+    if (entry(start, 0) > t) return -1;
     int lo = 0, len = n;
     while (len > 1) {
         const int step = (len + 63) / 64, at = lane * step;
@@ -41,11 +58,20 @@ __device__ __forceinline__ int owner(const int32_t* start, int n, int64_t t) {
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// LDS: a count, then a shift, for each token of the chunk; a bit for each that was seen;
-// with biases the last entry of each token; with drafted tokens their nodes.
+// LDS: a count, then a shift, for each token of the chunk; a bit for each that was seen,
+// and for each that changes; with biases the last entry of each token; with drafted
+// tokens their nodes.
 constexpr size_t lds_bytes(int C, bool biases, int words) {
-    return 4 * C + C / 8 + 16 + (biases ? 4 * C : 0) + 64 * words * 8 * (words + 2);
+    return 4 * C + 2 * (C / 8 + 16) + (biases ? 4 * C : 0) + 64 * words * 8 * (words + 2);
 }
+// Eight bits or less from `place` on.
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int place) {
+    const uint32_t* w = words + (place >> 5);
+    return __builtin_amdgcn_alignbit(w[1], w[0], place & 31);
+}
+// All ones where bit e of x is set.
+__device__ __forceinline__ uint32_t spread(uint32_t x, int e) { return (uint32_t)((int32_t)(x << (31 - e)) >> 31); }
+__device__ __forceinline__ uint32_t pick(uint32_t m, uint32_t x, uint32_t y) { return (x & m) | (y & ~m); }
 
 // A token that the request drafted: its place in the chunk (-1: another entry has it), the
 // shift that it has without the row's path, and whether the history and the answer
@@ -67,7 +93,8 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
     extern __shared__ __attribute__((aligned(16))) uint32_t count[];
     float* shift = reinterpret_cast<float*>(count);
     uint32_t* seen = count + C;                         // [C / 32], and a word past the end
-    uint64_t* nodes = reinterpret_cast<uint64_t*>(seen + C / 32 + 4);
+    uint32_t* changed = seen + C / 32 + 4;              // the same
+    uint64_t* nodes = reinterpret_cast<uint64_t*>(changed + C / 32 + 4);
     Draft* drafts = reinterpret_cast<Draft*>(nodes + 64 * a.words * a.words);
     uint32_t* last = reinterpret_cast<uint32_t*>(drafts + 64 * a.words);
     __shared__ int n_drafts;
@@ -83,64 +110,126 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
     const bool biases = a.bias_start != nullptr, changes = repeats || biases, drafted = repeats && a.draft;
 
     // A row: `head` logits up to where out is aligned, vectors, and what is left, with a
-    // lane for each that no vector has.
+    // lane for each that no vector has.  All loads are made, by lanes that have nothing to
+    // load from where another does: a branch would have the compiler wait for them.
     struct Row {
         V x[NVEC];
         Vec<BF16, 1> edge;
-        uint32_t ok[NVEC], edge_ok;                     // bits of the allowed tokens
-        int head, full;
+        uint32_t ok[NVEC], edge_ok;                     // allowed tokens: two bytes of the bits
+        int head, full, state;
         __device__ __forceinline__ int at(int k, int lane) const { return head + (64 * k + lane) * PV; }
         __device__ __forceinline__ int edge_at(int lane) const { return lane < head ? lane : full + lane - head; }
     };
+    const bool vectors = wide >= 2 * PV;
     // lane i has row i's place among the masks
     int64_t state = -1;
     if (a.allowed && lane < n_rows) state = a.allowed_row ? (int64_t)a.allowed_row[t0 + lane] : t0 + lane;
     if (state >= a.n_allowed) state = -1;
+    // two bytes of the bits from here on end the masks' row
+    const int last_bits = (int)(4 * a.lda - ((c0 + v0) >> 3)) - 2;
+    auto bits_byte = [&](int v) __attribute__((always_inline)) { return min(v >> 3, last_bits); };
     auto load = [&](Row& w, int i) __attribute__((always_inline)) {
         const E* from = (const E*)a.logits + (t0 + i) * a.ldl + c0 + v0;
         const uint32_t off = (uint32_t)(uintptr_t)((E*)a.out + (t0 + i) * a.ldo + c0 + v0) / sizeof(E) % PV;
-        w.head = __builtin_amdgcn_readfirstlane(min((int)(off ? PV - off : 0), wide));
+        w.head = vectors ? __builtin_amdgcn_readfirstlane((int)(off ? PV - off : 0)) : wide;
         w.full = w.head + (wide - w.head) / PV * PV;
-        const int s = __builtin_amdgcn_readlane((int)state, i);
-        const uint32_t* bits = a.allowed + s * a.lda + ((c0 + v0) >> 5);
+        w.state = __builtin_amdgcn_readlane((int)state, i);
+        const uint8_t* bits = w.state >= 0 && wide > 0 ? reinterpret_cast<const uint8_t*>(a.allowed + w.state * a.lda) + ((c0 + v0) >> 3)
+                                                       : nullptr;
 #pragma unroll
         for (int k = 0; k < NVEC; ++k) {
-            const int v = w.at(k, lane);
-            w.ok[k] = ~0u;
-            if (v >= w.full) continue;
-            w.x[k].load(from + v);
-            if (s >= 0) {
-                const uint32_t lo = bits[v >> 5], hi = bits[(v + PV - 1) >> 5];
-                w.ok[k] = (uint32_t)(((uint64_t)hi << 32 | lo) >> (v & 31));
-            }
+            const int v = min(w.at(k, lane), w.full - PV);
+            w.x[k].r = global<typename V::Loose>(vectors ? (const void*)(from + v) : kNowhere);
+            w.ok[k] = global<loose_u16>(vectors && bits ? (const void*)(bits + bits_byte(v)) : kNowhere);
         }
-        const int v = w.edge_at(lane);
-        w.edge_ok = 1;
-        if (lane < w.head + wide - w.full) {
-            w.edge.load(from + v);
-            if (s >= 0) w.edge_ok = bits[v >> 5] >> (v & 31);
+        const int v = min(w.edge_at(min(lane, max(w.head + wide - w.full, 1) - 1)), wide - 1);
+        w.edge.r = global<typename Vec<BF16, 1>::Loose>(wide > 0 ? (const void*)(from + v) : kNowhere);
+        w.edge_ok = global<uint8_t>(bits ? (const void*)(bits + (v >> 3)) : kNowhere);
+    };
+    bool built = false;                                 // shifts of a request are in LDS
+    float rep = 1.0f, inv = 1.0f, pres = 0.0f, freq = 0.0f;
+    // One row from its registers, the next one on its way.
+    auto step = [&](Row& now, Row& next, int i) __attribute__((always_inline)) {
+        const int64_t t = t0 + i;
+        load(next, min(i + 1, n_rows - 1));
+        if (drafted && n_drafts > 0) {
+            const uint64_t* mask = a.mask + t * a.words;
+            for (int j = lane; j < n_drafts; j += 64) {
+                const Draft d = drafts[j];
+                if (d.place < 0 || d.place / CW != wave) continue;
+                int c = 0;
+                for (int w = 0; w < a.words; ++w) c += __popcll(nodes[j * a.words + w] & entry(mask, w));
+                shift[d.place] = c != 0 ? d.shift - fmaf(freq, (float)c, d.answer ? 0.0f : pres) : d.shift;
+                const uint32_t bit = 1u << (d.place & 31);
+                if (c != 0 || d.seen) atomicOr(&seen[d.place >> 5], bit);
+                else atomicAnd(&seen[d.place >> 5], ~bit);
+            }
+            // the wave's own lanes read what it wrote
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+        auto adjust = [&](float y, float add, bool was) __attribute__((always_inline)) {
+            return fmaf(y, was ? (y > 0.0f ? inv : rep) : 1.0f, add);
+        };
+        G to = (G)a.out + t * a.ldo + c0 + v0;
+#pragma unroll
+        for (int k = 0; k < NVEC; ++k) {
+            const int v = now.at(k, lane);
+            if (v >= now.full) continue;
+            if (changes && (bits_at(changed, v0 + v) & ((1u << PV) - 1)) != 0) {
+                const uint32_t was = bits_at(seen, v0 + v);
+                float y[PV];
+                now.x[k].get(y);
+#pragma unroll
+                for (int e = 0; e < PV; ++e) y[e] = adjust(y[e], shift[v0 + v + e], was >> e & 1);
+                now.x[k].put(y);
+            }
+            if (now.state >= 0) {
+                const uint32_t ok = now.ok[k] >> (v - 8 * bits_byte(v));
+#pragma unroll
+                for (int j = 0; j < V::N; ++j) {
+                    if constexpr (BF16)
+                        now.x[k].r[j] = pick(pick(0xffffu, spread(ok, 2 * j), spread(ok, 2 * j + 1)), now.x[k].r[j], 0xff80ff80u);
+                    else
+                        now.x[k].r[j] = pick(spread(ok, j), now.x[k].r[j], 0xff800000u);
+                }
+            }
+            now.x[k].template store<PAST>(to + v);
+        }
+        if (lane < now.head + wide - now.full) {
+            const int v = now.edge_at(lane);
+            float y[1];
+            now.edge.get(y);
+            if (changes) y[0] = adjust(y[0], shift[v0 + v], seen[(v0 + v) >> 5] >> ((v0 + v) & 31) & 1);
+            if (now.state >= 0 && !(now.edge_ok >> (v & 7) & 1)) y[0] = -INFINITY;
+            now.edge.put(y);
+            now.edge.template store<false>(to + v);
         }
     };
-    Row next;
-    load(next, 0);
 
+    Row x, y;
+    load(x, 0);
     int r = a.start ? owner(a.start, a.n_req, t0) : (int)t0;
-    int held = -1;                                      // the request whose shifts are in LDS
-    float rep = 1.0f, inv = 1.0f, pres = 0.0f, freq = 0.0f;
-    for (int i = 0; i < n_rows; ++i) {
+    for (int i = 0; i < n_rows;) {
+        // the request of row i and the end of its rows
         const int64_t t = t0 + i;
-        Row now = next;
-        if (i + 1 < n_rows) load(next, i + 1);
+        int stop = i + 1;
         if (a.start) {
-            if (r < 0 && a.start[0] <= t) r = owner(a.start, a.n_req, t);
-            while (r >= 0 && r < a.n_req && a.start[r + 1] <= t) ++r;
-            if (r < 0) continue;
+            if (r < 0) r = owner(a.start, a.n_req, t);
+            while (r >= 0 && r < a.n_req && entry(a.start, r + 1) <= t) ++r;
+            if (r < 0) {
+                load(x, min(i + 1, n_rows - 1));
+                ++i;
+                continue;
+            }
+            if (r < a.n_req) stop = (int)min((int64_t)entry(a.start, r + 1) - t0, (int64_t)n_rows);
         } else {
             r = (int)t;
         }
         if (r >= a.n_req) break;
 
-        if (r != held && changes) {
+        if (changes) {
             const int32_t* h = a.history + (int64_t)r * a.max_hist;
             const bool counted = repeats && a.hist_len;
             i32x4 first[AHEAD];
@@ -150,25 +239,25 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
                     if (4 * (k * NTHR + tid) + 4 <= a.max_hist) first[k] = *reinterpret_cast<const loose4*>(h + 4 * (k * NTHR + tid));
             }
             int64_t end = 0, past = 0, lo = 0, hi = 0;
-            if (counted) end = min(max((int64_t)a.hist_len[r], (int64_t)0), a.max_hist);
-            if (counted && a.prompt_len) past = min(max((int64_t)a.prompt_len[r], (int64_t)0), end);
+            if (counted) end = min(max((int64_t)entry(a.hist_len, r), (int64_t)0), a.max_hist);
+            if (counted && a.prompt_len) past = min(max((int64_t)entry(a.prompt_len, r), (int64_t)0), end);
             if (biases) {
-                lo = min(max((int64_t)a.bias_start[r], (int64_t)0), a.n_bias);
-                hi = min(max((int64_t)a.bias_start[r + 1], lo), a.n_bias);
+                lo = min(max((int64_t)entry(a.bias_start, r), (int64_t)0), a.n_bias);
+                hi = min(max((int64_t)entry(a.bias_start, r + 1), lo), a.n_bias);
             }
-            if (a.repetition) rep = a.repetition[r];
-            if (a.presence) pres = a.presence[r];
-            if (a.frequency) freq = a.frequency[r];
+            if (a.repetition) rep = entry(a.repetition, r);
+            if (a.presence) pres = entry(a.presence, r);
+            if (a.frequency) freq = entry(a.frequency, r);
             // this thread's node, where the chunk has its token
             int place = -1;
             if (drafted) {
-                const int64_t n0 = a.start ? max((int64_t)a.start[r], (int64_t)0) : t, n1 = a.start ? min((int64_t)a.start[r + 1], a.T) : t + 1;
+                const int64_t n0 = a.start ? max((int64_t)entry(a.start, r), (int64_t)0) : t, n1 = a.start ? min((int64_t)entry(a.start, r + 1), a.T) : t + 1;
                 if (tid < 64 * a.words && n0 + tid < n1) {
                     const int64_t at = (int64_t)a.draft[n0 + tid] - c0;
                     if (at >= 0 && at < width) place = (int)at;
                 }
             }
-            if (held >= 0) __syncthreads();             // the request before has read its shifts
+            if (built) __syncthreads();                 // the request before has read its shifts
             for (int j = 4 * tid; j < C; j += 4 * NTHR) {
                 *reinterpret_cast<u32x4*>(count + j) = u32x4{0, 0, 0, 0};
                 if (biases) *reinterpret_cast<u32x4*>(last + j) = u32x4{0, 0, 0, 0};
@@ -232,7 +321,7 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
             }
             inv = 1.0f / rep;
             for (int j = 8 * tid; j < C; j += 8 * NTHR) {
-                uint32_t f = 0;
+                uint32_t f = 0, g = 0;
 #pragma unroll
                 for (int e = 0; e < 8; e += 4) {
                     u32x4 n = *reinterpret_cast<const u32x4*>(count + j + e), m = {0, 0, 0, 0};
@@ -244,66 +333,31 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
                         float y = m[z] ? a.bias[m[z] - 1] : -0.0f;
                         if (c != 0) y -= fmaf(freq, (float)c, pres);
                         n[z] = __float_as_uint(y);
+                        g |= (uint32_t)(n[z] != 0x80000000u) << (e + z);
                     }
                     *reinterpret_cast<u32x4*>(count + j + e) = n;
                 }
                 reinterpret_cast<uint8_t*>(seen)[j / 8] = (uint8_t)f;
+                reinterpret_cast<uint8_t*>(changed)[j / 8] = (uint8_t)(f | g);
             }
             __syncthreads();
             if (drafted) {
-                if (mine >= 0) drafts[mine].shift = shift[place];
+                if (mine >= 0) {
+                    drafts[mine].shift = shift[place];
+                    atomicOr(&changed[place >> 5], 1u << (place & 31));
+                }
                 __syncthreads();
             }
-            held = r;
+            built = true;
         }
-        if (drafted && n_drafts > 0) {
-            const uint64_t* mask = a.mask + t * a.words;
-            for (int j = lane; j < n_drafts; j += 64) {
-                const Draft d = drafts[j];
-                if (d.place < 0 || d.place / CW != wave) continue;
-                int c = 0;
-                for (int w = 0; w < a.words; ++w) c += __popcll(nodes[j * a.words + w] & mask[w]);
-                shift[d.place] = c != 0 ? d.shift - fmaf(freq, (float)c, d.answer ? 0.0f : pres) : d.shift;
-                const uint32_t bit = 1u << (d.place & 31);
-                if (c != 0 || d.seen) atomicOr(&seen[d.place >> 5], bit);
-                else atomicAnd(&seen[d.place >> 5], ~bit);
-            }
-            // the wave's own lanes read what it wrote
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (; i + 1 < stop; i += 2) {
+            step(x, y, i);
+            step(y, x, i + 1);
         }
-        auto adjust = [&](float y, float add, bool was) __attribute__((always_inline)) {
-            return fmaf(y, was ? (y > 0.0f ? inv : rep) : 1.0f, add);
-        };
-        G to = (G)a.out + t * a.ldo + c0 + v0;
-#pragma unroll
-        for (int k = 0; k < NVEC; ++k) {
-            const int v = now.at(k, lane);
-            if (v >= now.full) continue;
-            float y[PV];
-            now.x[k].get(y);
-            if (changes) {
-                const uint32_t* w = seen + ((v0 + v) >> 5);
-                const uint32_t was = (uint32_t)(((uint64_t)w[1] << 32 | w[0]) >> ((v0 + v) & 31));
-#pragma unroll
-                for (int e = 0; e < PV; ++e) y[e] = adjust(y[e], shift[v0 + v + e], was >> e & 1);
-            }
-            if (a.allowed) {
-#pragma unroll
-                for (int e = 0; e < PV; ++e) y[e] = now.ok[k] >> e & 1 ? y[e] : -INFINITY;
-            }
-            now.x[k].put(y);
-            now.x[k].template store<PAST>(to + v);
-        }
-        if (lane < now.head + wide - now.full) {
-            const int v = now.edge_at(lane);
-            float y[1];
-            now.edge.get(y);
-            if (changes) y[0] = adjust(y[0], shift[v0 + v], seen[(v0 + v) >> 5] >> ((v0 + v) & 31) & 1);
-            if (!(now.edge_ok & 1)) y[0] = -INFINITY;
-            now.edge.put(y);
-            now.edge.template store<false>(to + v);
+        if (i < stop) {
+            step(x, y, i);
+            x = y;
+            ++i;
         }
     }
 }
