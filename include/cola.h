@@ -641,7 +641,7 @@ typedef struct {
     int64_t n_req;            /* 0 .. 65535 */
     int64_t max_hist;         /* entries per row of history, below 2^30 */
     int64_t max_new;          /* most rows of one request that have drafted tokens, 0 .. COLA_TREE_MAX (0: none) */
-    int64_t n_bias;           /* entries of bias_token and bias, below 2^31 */
+    int64_t n_bias;           /* entries of bias_token and bias, below 2^30 */
     int64_t n_allowed;        /* rows of allowed, below 2^31 */
     int64_t ldl, ldo;         /* row pitches of logits and out, 0 = V; at most COLA_MAX_PITCH */
     int64_t lda;              /* words per row of allowed, 0 = ceil(V / 32) */

@@ -30,6 +30,7 @@ typedef uint16_t loose_u16 __attribute__((aligned(1)));
 
 // What a wave's loads go to where it has no logits.
 __device__ const uint32_t kNowhere[4] = {0, 0, 0, 0};
+__device__ const float kOne = 1.0f;
 // A load from global memory, said so: a pointer picked among several loses its space.
 template <class X>
 __device__ __forceinline__ X global(const void* p) {
@@ -86,7 +87,7 @@ struct Draft {
 template <bool BF16, int NVEC, bool PAST>
 __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const int rows, const int chunks, const int64_t base) {
     constexpr int PV = BF16 ? 8 : 4, CW = 64 * PV * NVEC, C = CW * NTHR / 64;
-    constexpr int AHEAD = 2;                            // of the history, 4 tokens each, on their way before its length is known
+    constexpr int AHEAD = 4;                            // loads of the history that a thread has on their way, 4 tokens each
     typedef Vec<BF16, PV> V;
     typedef typename V::E E;
     typedef typename V::G G;
@@ -98,6 +99,7 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
     Draft* drafts = reinterpret_cast<Draft*>(nodes + 64 * a.words * a.words);
     uint32_t* last = reinterpret_cast<uint32_t*>(drafts + 64 * a.words);
     __shared__ int n_drafts;
+    __shared__ float value[NTHR];                       // of the first entries of the request's list
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t group = (base + blockIdx.x) / chunks;
     const int64_t c0 = (base + blockIdx.x - group * chunks) * C;
@@ -230,33 +232,38 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
         if (r >= a.n_req) break;
 
         if (changes) {
-            const int32_t* h = a.history + (int64_t)r * a.max_hist;
             const bool counted = repeats && a.hist_len;
-            i32x4 first[AHEAD];
-            if (counted) {
+            const int32_t* h = a.history + (int64_t)r * a.max_hist;
+            // The request's numbers, all on their way at once: those that are not there come
+            // from a place that is.
+            const int32_t* zero = reinterpret_cast<const int32_t*>(kNowhere);
+            const float* one = &kOne;
+            const int hist_len = entry(counted ? a.hist_len + r : zero, 0), prompt_len = entry(a.prompt_len ? a.prompt_len + r : zero, 0);
+            const int bias_lo = entry(biases ? a.bias_start + r : zero, 0), bias_hi = entry(biases ? a.bias_start + r + 1 : zero, 0);
+            const int first = entry(a.start ? a.start + r : zero, 0), past_last = entry(a.start ? a.start + r + 1 : zero, 0);
+            rep = entry(a.repetition ? a.repetition + r : one, 0);
+            pres = entry(a.presence ? a.presence + r : reinterpret_cast<const float*>(zero), 0);
+            freq = entry(a.frequency ? a.frequency + r : reinterpret_cast<const float*>(zero), 0);
+            const int end = min(max(hist_len, 0), (int)a.max_hist), past = min(max(prompt_len, 0), end);
+            const int lo = min(max(bias_lo, 0), (int)a.n_bias), hi = min(max(bias_hi, lo), (int)a.n_bias);
+            const int64_t n0 = a.start ? max(first, 0) : t, n1 = a.start ? min((int64_t)past_last, a.T) : t + 1;
+            // A thread's first entries of the lists, on their way while LDS is cleared.  The
+            // history goes four tokens a load; the last load ends with it.
+            auto read = [&](i32x4 (&y)[AHEAD], int j0) __attribute__((always_inline)) {
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k)
-                    if (4 * (k * NTHR + tid) + 4 <= a.max_hist) first[k] = *reinterpret_cast<const loose4*>(h + 4 * (k * NTHR + tid));
+                for (int k = 0; k < AHEAD; ++k) y[k] = global<loose4>(h + min(j0 + 4 * k * NTHR, end - 4));
+            };
+            i32x4 y[AHEAD];
+            if (end >= 4) read(y, 4 * tid);
+            int token = -1, node = -1;
+            float b = 0.0f;
+            if (lo + tid < hi) {
+                token = a.bias_token[lo + tid];
+                b = a.bias[lo + tid];
             }
-            int64_t end = 0, past = 0, lo = 0, hi = 0;
-            if (counted) end = min(max((int64_t)entry(a.hist_len, r), (int64_t)0), a.max_hist);
-            if (counted && a.prompt_len) past = min(max((int64_t)entry(a.prompt_len, r), (int64_t)0), end);
-            if (biases) {
-                lo = min(max((int64_t)entry(a.bias_start, r), (int64_t)0), a.n_bias);
-                hi = min(max((int64_t)entry(a.bias_start, r + 1), lo), a.n_bias);
-            }
-            if (a.repetition) rep = entry(a.repetition, r);
-            if (a.presence) pres = entry(a.presence, r);
-            if (a.frequency) freq = entry(a.frequency, r);
-            // this thread's node, where the chunk has its token
-            int place = -1;
-            if (drafted) {
-                const int64_t n0 = a.start ? max((int64_t)entry(a.start, r), (int64_t)0) : t, n1 = a.start ? min((int64_t)entry(a.start, r + 1), a.T) : t + 1;
-                if (tid < 64 * a.words && n0 + tid < n1) {
-                    const int64_t at = (int64_t)a.draft[n0 + tid] - c0;
-                    if (at >= 0 && at < width) place = (int)at;
-                }
-            }
+            if (drafted && tid < 64 * a.words && n0 + tid < n1) node = a.draft[n0 + tid];
+            // a token's place in the chunk, `width` or more: it has none
+            auto place_of = [&](int token) __attribute__((always_inline)) { return (uint32_t)token - (uint32_t)c0; };
             if (built) __syncthreads();                 // the request before has read its shifts
             for (int j = 4 * tid; j < C; j += 4 * NTHR) {
                 *reinterpret_cast<u32x4*>(count + j) = u32x4{0, 0, 0, 0};
@@ -264,36 +271,40 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
             }
             if (tid == 0) n_drafts = 0;
             __syncthreads();
-            if (counted) {
-                auto note = [&](int32_t token, int64_t j) __attribute__((always_inline)) {
-                    const int64_t at = (int64_t)token - c0;
-                    if (at >= 0 && at < width) {
-                        if (j < past) atomicOr(&count[at], kPrompt);
-                        else atomicAdd(&count[at], 1u);
-                    }
-                };
-#pragma unroll
-                for (int k = 0; k < AHEAD; ++k) {
-                    const int64_t j = 4 * (k * NTHR + tid);
-                    if (j + 4 <= end) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) note(first[k][e], j + e);
-                    }
+            auto note = [&](int token, int j) __attribute__((always_inline)) {
+                const uint32_t at = place_of(token);
+                if (at < (uint32_t)width) {
+                    if (j < past) atomicOr(&count[at], kPrompt);
+                    else atomicAdd(&count[at], 1u);
                 }
-                for (int64_t j = 4 * (AHEAD * NTHR + tid); j + 4 <= end; j += 4 * NTHR) {
-                    const i32x4 y = *reinterpret_cast<const loose4*>(h + j);
+            };
+            if (end >= 4) {
+                for (int j0 = 4 * tid;;) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) note(y[e], j + e);
+                    for (int k = 0; k < AHEAD; ++k) {
+                        const int j = j0 + 4 * k * NTHR, from = min(j, end - 4);
+                        if (j >= end) continue;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (from + e >= j) note(y[k][e], from + e);
+                    }
+                    j0 += 4 * AHEAD * NTHR;
+                    if (j0 >= end) break;
+                    read(y, j0);
                 }
-                if (tid < (end & 3)) note(h[(end & ~int64_t(3)) + tid], (end & ~int64_t(3)) + tid);
+            } else if (tid < end) {
+                note(h[tid], tid);
             }
             // the last entry of each token, by its place in the list + 1
-            for (int64_t j = lo + tid; j < hi; j += NTHR) {
-                const int64_t at = (int64_t)a.bias_token[j] - c0;
-                if (at >= 0 && at < width) atomicMax(&last[at], (uint32_t)j + 1);
+            for (int j = lo + tid; j < hi; j += NTHR) {
+                const uint32_t at = place_of(token);
+                if (at < (uint32_t)width) atomicMax(&last[at], (uint32_t)j + 1);
+                if (j + NTHR < hi) token = a.bias_token[j + NTHR];
             }
-            int mine = -1;
-            if (place >= 0) {
+            value[tid] = b;
+            int mine = -1, place = 0;
+            if (drafted && place_of(node) < (uint32_t)width) {
+                place = (int)place_of(node);
                 mine = atomicAdd(&n_drafts, 1);
                 drafts[mine] = Draft{place, 0.0f, (uint32_t)tid, 0};
             }
@@ -320,7 +331,10 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
                 if (mine >= 0) drafts[mine] = Draft{keep ? place : -1, 0.0f, held_count != 0, (held_count & ~kPrompt) != 0};
             }
             inv = 1.0f / rep;
-            for (int j = 8 * tid; j < C; j += 8 * NTHR) {
+#pragma unroll
+            for (int j0 = 0; j0 < C; j0 += 8 * NTHR) {
+                const int j = j0 + 8 * tid;
+                if (C < 8 * NTHR && j >= C) break;
                 uint32_t f = 0, g = 0;
 #pragma unroll
                 for (int e = 0; e < 8; e += 4) {
@@ -330,7 +344,8 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
                     for (int z = 0; z < 4; ++z) {
                         const uint32_t c = n[z] & ~kPrompt;
                         f |= (uint32_t)(n[z] != 0) << (e + z);
-                        float y = m[z] ? a.bias[m[z] - 1] : -0.0f;
+                        float y = -0.0f;
+                        if (m[z]) y = (int)m[z] - 1 - lo < NTHR ? value[m[z] - 1 - lo] : a.bias[m[z] - 1];
                         if (c != 0) y -= fmaf(freq, (float)c, pres);
                         n[z] = __float_as_uint(y);
                         g |= (uint32_t)(n[z] != 0x80000000u) << (e + z);

@@ -469,7 +469,7 @@ int cola_logits_adjust(const cola_logits_desc* d, const cola_logits_rules* rules
     return guarded([&]() -> int {
         if (!d || !rules || !dtype_ok(d->dtype) || d->reserved != 0) return COLA_ERR_INVALID_ARG;
         if (d->T < 0 || d->T > kMaxInt || d->V < 1 || d->V > kMaxPitch || d->n_req < 0 || d->n_req > 65535 || d->max_hist < 0 ||
-            d->max_hist >= kMaxKeys || d->max_new < 0 || d->max_new > COLA_TREE_MAX || d->n_bias < 0 || d->n_bias > kMaxInt ||
+            d->max_hist >= kMaxKeys || d->max_new < 0 || d->max_new > COLA_TREE_MAX || d->n_bias < 0 || d->n_bias >= kMaxKeys ||
             d->n_allowed < 0 || d->n_allowed > kMaxInt)
             return COLA_ERR_BAD_SHAPE;
         LogitsArgs a{};
@@ -495,7 +495,7 @@ int cola_logits_adjust(const cola_logits_desc* d, const cola_logits_rules* rules
         if (u.hist_len || u.draft) {
             a.repetition = u.repetition; a.presence = u.presence; a.frequency = u.frequency;
         }
-        a.bias_start = u.bias_start; a.bias_token = u.bias_token; a.bias = u.bias;
+        a.bias_start = d->n_bias > 0 ? u.bias_start : nullptr; a.bias_token = u.bias_token; a.bias = u.bias;
         a.allowed = d->n_allowed > 0 ? u.allowed : nullptr; a.allowed_row = u.allowed_row;
         a.T = d->T; a.V = d->V; a.max_hist = d->max_hist; a.n_bias = d->n_bias; a.n_allowed = d->n_allowed;
         a.n_req = (int)d->n_req; a.max_new = (int)d->max_new; a.words = (int)((d->max_new + 63) / 64);
