@@ -14,7 +14,7 @@ __global__ __launch_bounds__(NTHR) void prefix_join_few_kernel(const Args a) {
     const int e = 4 * (threadIdx.x % TPR);
     for (int r = blockIdx.y; r < a.n_req; r += gridDim.y) {
         const Span s = span_of(a, r);
-        const int parts = a.splits_p + parts_of(a, s.end);
+        const int parts = a.splits_p + parts_of(a, s.end, a.slots > 0 ? entry(a.chunk, 0) : a.chunk_s);
         for (int64_t j = (int64_t)blockIdx.x * (NTHR / TPR) + threadIdx.x / TPR; j < (int64_t)s.n * a.hq;
              j += (int64_t)gridDim.x * (NTHR / TPR)) {
             const int64_t id = (int64_t)s.row * a.hq + j;
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(NTHR) void prefix_join_kernel(const Args a) {
     const int sub = lane / LP, e = 4 * (lane % LP);
     for (int r = blockIdx.y; r < a.n_req; r += gridDim.y) {
         const Span s = span_of(a, r);
-        const int parts = a.splits_p + parts_of(a, s.end);
+        const int parts = a.splits_p + parts_of(a, s.end, a.slots > 0 ? entry(a.chunk, 0) : a.chunk_s);
         for (int64_t j = (int64_t)blockIdx.x * NW + wave; j < (int64_t)s.n * a.hq; j += (int64_t)gridDim.x * NW) {
             const int64_t id = (int64_t)s.row * a.hq + j;
             float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(NTHR) void prefix_join_kernel(const Args a) {
 template <int HD>
 hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t s) {
 #define COLA_GO(P, S) \
-    if (p.kind_p == P && p.kind_s == S) prefix_attn_kernel<HD, P, S, SEE_CAUSAL><<<grid, NTHR, 0, s>>>(a)
+    if (p.kind_p == P && p.kind_s == S) prefix_attn_kernel<HD, P, S, SEE_CAUSAL, false><<<grid, NTHR, 0, s>>>(a)
     COLA_GO(ALONG, ONE);
     else COLA_GO(ALONG, TWO);
     else COLA_GO(ALONG, FLAT);
@@ -165,10 +165,11 @@ constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
 constexpr int64_t kWideOwnBytes = 128000000;  // of partial rows, where these parts are more than the chip needs
 constexpr int64_t kWideOwnTurns = 1 << 16;   // workgroups up to which there are such parts: 1.3 ns for each that has no rows
+constexpr int64_t kTreeOwn = 8;            // the same of trees' tiles, at the least
 constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
-int kind_of(int64_t rows) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : WIDE); }
+int kind_of(int64_t rows, bool wider) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : (wider && rows > 128 ? WIDER : WIDE)); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
@@ -176,17 +177,17 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     const int64_t g = sh.hq / sh.hk;
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
     p.rows = sh.T * sh.hq;
-    p.kind_s = kind_of(new_rows * g);
-    p.kind_p = kind_of(sh.T * g);                              // never below kind_s
+    p.kind_s = kind_of(new_rows * g, tree && sh.hd == 64);
+    p.kind_p = kind_of(sh.T * g, p.kind_s == WIDER);                              // never below kind_s
     p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.kind_p));
     p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.kind_s));
     if (p.kind_s == ONE && sh.max_new == 1 && !tree)
         p.kind_s = sh.n_req * sh.hk >= kSoloItems && (sh.prefix == 0 || p.kind_p == WIDE) ? SOLO : FLAT;
     // without a prefix, the kernel whose prefix part asks for least
-    if (sh.prefix == 0) p.kind_p = p.kind_s == TWO || p.kind_s == WIDE ? p.kind_s : ONE;
+    if (sh.prefix == 0) p.kind_p = p.kind_s == TWO || is_wide(p.kind_s) ? p.kind_s : ONE;
     // Short prefixes and few requests: the prefix's bytes come from L2 for each of them,
     // which costs less than a launch that joins.
-    const bool wide = p.kind_s == WIDE;
+    const bool wide = is_wide(p.kind_s);
     if (sh.prefix > 0 && sh.prefix + sh.max_kv <= (wide ? kWideAlongKeys : kAlongKeys) && p.kind_s != SOLO &&
         sh.n_req * p.tiles_s * sh.prefix * sh.hk * sh.hd * 4 <= (wide ? kWideAlongBytes : kAlongBytes)) {
         p.kind_p = ALONG;
@@ -204,7 +205,7 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     // and 141.
     const int64_t base_p = (int64_t)p.tiles_p * sh.hk, base_s = sh.n_req * p.tiles_s * sh.hk;
     const int64_t blocks_p = base_p * ceil_div(sh.prefix, KB), blocks_s = base_s * ceil_div(sh.max_kv, KB);
-    const int64_t items = sh.hd == 128 ? 512 : 1024;
+    const int64_t items = full_chip(sh.hd, p.kind_s);
     int64_t chunk = ceil_div(blocks_p + blocks_s, items);
     if (chunk < 8) chunk = 8;
     // The prefix's length is known, max_kv only bounds the requests': their keys count
@@ -248,17 +249,23 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     // 8 behind 4096 + 4000 134, 146, 127; 5 of up to 3000, 512 queries, 88, 111, 125.
     parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
     int64_t own = chunk;
-    if (wide && sh.n_req >= 4 && chunk > kWideOwn) {
+    // Trees' lengths are counted on the GPU (own_chunk), which makes the parts even; these
+    // are the least.
+    const int64_t kv_blocks = ceil_div(sh.max_kv, KB);
+    const bool counted = wide && tree && sh.n_req <= kCounted && base_s < items / 2;
+    const int64_t least = counted ? kTreeOwn : kWideOwn;
+    if (counted || (wide && sh.n_req >= 4 && chunk > least)) {
         int64_t fit = kWideOwnBytes / (p.rows * (sh.hd + 2) * 4) - p.splits_p;
         if (fit > kWideOwnTurns / base_s) fit = kWideOwnTurns / base_s;
-        own = ceil_div(ceil_div(sh.max_kv, KB), fit < 1 ? 1 : fit);
-        if (own < kWideOwn) own = kWideOwn;
-        if (own > chunk) own = chunk;
+        own = ceil_div(kv_blocks, fit < 1 ? 1 : fit);
+        if (own < least) own = least;
+        if (own > chunk && !counted) own = chunk;
     }
     parts(sh.max_kv, own, sh.prefix == 0, &p.splits_s, &p.chunk_s);
     const int64_t n = (p.splits_p + p.splits_s) * p.rows;
     p.direct = p.splits_p == 0 && p.splits_s == 1;
     p.ws_bytes = p.direct || n == 0 ? 0 : (size_t)((2 * n + 63) / 64 * 64 + n * sh.hd) * 4;
+    if (tree && p.ws_bytes > 0 && counts_lengths(sh, p)) p.ws_bytes += 64;
     return p;
 }
 

@@ -7,17 +7,22 @@ namespace {
 
 template <int HD>
 hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t s) {
-#define COLA_GO(P, S) \
-    if (p.kind_p == P && p.kind_s == S) prefix_attn_kernel<HD, P, S, SEE_TREE><<<grid, NTHR, 0, s>>>(a)
-    COLA_GO(ALONG, ONE);
-    else COLA_GO(ALONG, TWO);
-    else COLA_GO(ALONG, WIDE);
-    else COLA_GO(ONE, ONE);
-    else COLA_GO(TWO, ONE);
-    else COLA_GO(TWO, TWO);
-    else COLA_GO(WIDE, ONE);
-    else COLA_GO(WIDE, TWO);
-    else COLA_GO(WIDE, WIDE);
+#define COLA_GO(P, S, C)                                      \
+    if (p.kind_p == P && p.kind_s == S && (a.slots > 0) == C) \
+    prefix_attn_kernel<HD, P, S, SEE_TREE, C><<<grid, S == WIDER ? 2 * NTHR : NTHR, 0, s>>>(a)
+    COLA_GO(ALONG, ONE, false);
+    else COLA_GO(ALONG, TWO, false);
+    else COLA_GO(ALONG, WIDE, false);
+    else COLA_GO(ALONG, WIDER, false);
+    else COLA_GO(ONE, ONE, false);
+    else COLA_GO(TWO, ONE, false);
+    else COLA_GO(TWO, TWO, false);
+    else COLA_GO(WIDE, ONE, false);
+    else COLA_GO(WIDE, TWO, false);
+    else COLA_GO(WIDE, WIDE, false);
+    else COLA_GO(WIDE, WIDE, true);
+    else COLA_GO(WIDER, WIDER, false);
+    else COLA_GO(WIDER, WIDER, true);
     else return hipErrorInvalidValue;
 #undef COLA_GO
     return hipGetLastError();
