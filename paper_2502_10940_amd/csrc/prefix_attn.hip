@@ -165,11 +165,19 @@ constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
 constexpr int64_t kWideOwnBytes = 128000000;  // of partial rows, where these parts are more than the chip needs
 constexpr int64_t kWideOwnTurns = 1 << 16;   // workgroups up to which there are such parts: 1.3 ns for each that has no rows
-constexpr int64_t kTreeOwn = 8;            // the same of trees' tiles, at the least
+constexpr int64_t kTreeOwn = 8;            // the same where they are cut by the lengths, at the least
 constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
-int kind_of(int64_t rows, bool wider) { return rows <= 16 ? ONE : (rows <= 32 ? TWO : (wider && rows > 128 ? WIDER : WIDE)); }
+// Trees of heads of 64 have two more kinds.  64 rows in registers: 24 trees of up to 64
+// nodes over 4000 keys, 32 heads, 96 us against 104 in tiles of 128; 8 of up to 40 over
+// 8000, 16 heads, 40 against 49; one of 60, 300 keys, 10 against 13.5.  256 rows, which
+// fetch the keys once: 32 of up to 40 nodes over 4000 keys, 16 heads over 2, 33 against
+// 36.  At heads of 128 neither fits the registers (256 rows: 369 us against 175).
+int kind_of(int64_t rows, bool trees) {
+    if (rows <= 32) return rows <= 16 ? ONE : TWO;
+    return trees && rows <= 64 ? FOUR : trees && rows > 128 ? WIDER : WIDE;
+}
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
@@ -178,18 +186,24 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
     p.rows = sh.T * sh.hq;
     p.kind_s = kind_of(new_rows * g, tree && sh.hd == 64);
-    p.kind_p = kind_of(sh.T * g, p.kind_s == WIDER);                              // never below kind_s
+    p.kind_p = kind_of(sh.T * g, p.kind_s == WIDER || (p.kind_s == FOUR && sh.T * g <= 64));   // never below kind_s
     p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.kind_p));
     p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.kind_s));
     if (p.kind_s == ONE && sh.max_new == 1 && !tree)
         p.kind_s = sh.n_req * sh.hk >= kSoloItems && (sh.prefix == 0 || p.kind_p == WIDE) ? SOLO : FLAT;
     // without a prefix, the kernel whose prefix part asks for least
-    if (sh.prefix == 0) p.kind_p = p.kind_s == TWO || is_wide(p.kind_s) ? p.kind_s : ONE;
+    if (sh.prefix == 0) p.kind_p = p.kind_s == TWO || p.kind_s == FOUR || is_wide(p.kind_s) ? p.kind_s : ONE;
     // Short prefixes and few requests: the prefix's bytes come from L2 for each of them,
     // which costs less than a launch that joins.
+    auto along = [&](bool wide) {
+        return sh.prefix > 0 && sh.prefix + sh.max_kv <= (wide ? kWideAlongKeys : kAlongKeys) && p.kind_s != SOLO &&
+               sh.n_req * p.tiles_s * sh.prefix * sh.hk * sh.hd * 4 <= (wide ? kWideAlongBytes : kAlongBytes);
+    };
+    // FOUR beside wide tiles of a prefix leaves its kernel half the waves (24 trees of up to
+    // 48 nodes behind 2048 tokens, 32 heads: 62.7 us against 59.9)
+    if (p.kind_s == FOUR && p.kind_p == WIDE && !along(false)) p.kind_s = WIDE;
     const bool wide = is_wide(p.kind_s);
-    if (sh.prefix > 0 && sh.prefix + sh.max_kv <= (wide ? kWideAlongKeys : kAlongKeys) && p.kind_s != SOLO &&
-        sh.n_req * p.tiles_s * sh.prefix * sh.hk * sh.hd * 4 <= (wide ? kWideAlongBytes : kAlongBytes)) {
+    if (along(wide)) {
         p.kind_p = ALONG;
         p.tiles_p = 1;
         p.chunk_p = kRound;
@@ -249,10 +263,13 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     // 8 behind 4096 + 4000 134, 146, 127; 5 of up to 3000, 512 queries, 88, 111, 125.
     parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
     int64_t own = chunk;
-    // Trees' lengths are counted on the GPU (own_chunk), which makes the parts even; these
-    // are the least.
+    // Few requests' trees are cut by their lengths on the GPU (counted_item); these parts
+    // are the least, and say how many the workspace has room for.  8 requests of up to
+    // 32000 keys, 64 nodes of 32 heads over 8 of 128: 175 us against 205 with parts of 1536;
+    // 4 of up to 8000, 200 nodes: 72 against 78.  Where the tiles fill half of the chip as
+    // they are it costs more than it gives (32 of up to 4000, 32 nodes: 75 against 72).
     const int64_t kv_blocks = ceil_div(sh.max_kv, KB);
-    const bool counted = wide && tree && sh.n_req <= kCounted && base_s < items / 2;
+    const bool counted = tree && counts_lengths(sh, p.kind_s, p.tiles_s);
     const int64_t least = counted ? kTreeOwn : kWideOwn;
     if (counted || (wide && sh.n_req >= 4 && chunk > least)) {
         int64_t fit = kWideOwnBytes / (p.rows * (sh.hd + 2) * 4) - p.splits_p;
@@ -265,7 +282,7 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     const int64_t n = (p.splits_p + p.splits_s) * p.rows;
     p.direct = p.splits_p == 0 && p.splits_s == 1;
     p.ws_bytes = p.direct || n == 0 ? 0 : (size_t)((2 * n + 63) / 64 * 64 + n * sh.hd) * 4;
-    if (tree && p.ws_bytes > 0 && counts_lengths(sh, p)) p.ws_bytes += 64;
+    if (counted && p.ws_bytes > 0 && p.splits_s > 1) p.ws_bytes += 64;
     return p;
 }
 

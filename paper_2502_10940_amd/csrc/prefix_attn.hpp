@@ -891,14 +891,15 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
 }
 
 // Kinds of tiles: 16 or 32 rows whose keys a workgroup's waves share (ONE, TWO); 128
-// rows against keys in LDS (WIDE), of trees 256 too (WIDER).  On the requests' own keys, where each has one
+// rows against keys in LDS (WIDE).  Trees have two more: 64 rows as ONE and TWO (FOUR),
+// 256 rows as WIDE (WIDER).  On the requests' own keys, where each has one
 // token, all rows of a tile see the same: ONE becomes FLAT, or SOLO with a tile to
 // a wave.
 // Behind a short prefix there are no tiles for it: each request's own items take its
 // keys ALONG, and nothing is left to join.
-enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, ALONG = 5, WIDE = 8, WIDER = 16 };
+enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, ALONG = 5, FOUR = 6, WIDE = 8, WIDER = 16 };
 constexpr bool is_wide(int k) { return k == WIDE || k == WIDER; }
-constexpr int kind_rows(int k) { return k == SOLO || k == FLAT ? 16 : 16 * k; }
+constexpr int kind_rows(int k) { return k == SOLO || k == FLAT ? 16 : k == FOUR ? 64 : 16 * k; }
 // Parts of `chunk` keys that a request of `end` own tokens has.
 __device__ __forceinline__ int parts_of(const Args& a, int end, int chunk) {
     return a.splits_s > 0 ? min((end + chunk - 1) / chunk, a.splits_s) : 0;
@@ -997,7 +998,7 @@ constexpr int kLdsBytes = is_wide(N) ? kWideBytes<HD> : (N == SOLO || N == ALONG
 // behind 32768 tokens 101 us against 114, 200 of 32 heads 123 against 140; one request
 // behind 100 tokens 4.9 against 4.7, behind 1024 8.7 against 7.8).
 template <int HD, int N, int NP>
-constexpr bool kAhead = !is_wide(NP) && !(HD == 128 && N == TWO);
+constexpr bool kAhead = !is_wide(NP) && !(HD == 128 && N == TWO) && N != FOUR;
 
 template <int HD, int N, int NP, int SEE>
 __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
@@ -1011,13 +1012,13 @@ __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t
         item<HD, 1, NW, SEE_ALL, ALONG_P, kAhead<HD, N, NP>>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0,
                                chunk, slot);
     else
-        item<HD, N, NW, SEE, ALONG_P, kAhead<HD, N, NP>>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+        item<HD, kind_rows(N) / 16, NW, SEE, ALONG_P, kAhead<HD, N, NP>>(a, reinterpret_cast<float*>(lds), table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
 }
 
 // NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
 // SEE: causal, or trees.  COUNTED: the own keys are cut by the lengths.
 template <int HD, int NP, int NS, int SEE, bool COUNTED>
-__global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER ? 4 : NP == WIDE || NS == WIDE ? 2 : 1)) void prefix_attn_kernel(const Args a) {
+__global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER ? 4 : NP == WIDE || NS == WIDE || NS == FOUR ? 2 : 1)) void prefix_attn_kernel(const Args a) {
     constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     const int64_t at = a.base + blockIdx.x;
@@ -1068,10 +1069,10 @@ __global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER ? 4 : N
 // Workgroups of the wide kernels that the chip holds at once (two a CU at heads of 128
 // and of eight waves, four else).
 constexpr int64_t full_chip(int hd, int kind) { return hd == 128 || kind == WIDER ? 512 : 1024; }
-// Whether a launch for trees cuts the own keys by the lengths: wide tiles, parts to choose
-// from, and as many requests as a workgroup counts in a few loads.
-inline bool counts_lengths(const PrefixAttnShape& sh, const PrefixAttnPlan& p) {
-    return is_wide(p.kind_s) && p.splits_s > 1 && sh.n_req <= kCounted && sh.n_req * p.tiles_s * sh.hk < full_chip(sh.hd, p.kind_s) / 2;
+// Whether a launch for trees cuts the own keys by the lengths: wide tiles, fewer than
+// fill half of the chip, and as many requests as a workgroup counts in a few loads.
+inline bool counts_lengths(const PrefixAttnShape& sh, int kind, int tiles) {
+    return is_wide(kind) && sh.n_req <= kCounted && sh.n_req * tiles * sh.hk < full_chip(sh.hd, kind) / 2;
 }
 
 inline Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAttnPtrs& t) {
@@ -1095,7 +1096,7 @@ inline Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const Pr
     a.direct = p.direct;
     a.mask = t.mask;
     a.words = (int)((sh.max_new + 63) / 64);
-    a.slots = t.mask && counts_lengths(sh, p) ? (int)full_chip(sh.hd, p.kind_s) : 0;
+    a.slots = t.mask && p.splits_s > 1 && counts_lengths(sh, p.kind_s, p.tiles_s) ? (int)full_chip(sh.hd, p.kind_s) : 0;
     // parts as counted_item cuts them are at most the slots and one for each tile, and a
     // request's units are filled up to whole rounds of eight
     const int64_t base_s = sh.n_req * p.tiles_s * sh.hk;

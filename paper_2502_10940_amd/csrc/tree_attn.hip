@@ -13,7 +13,6 @@ hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t
     COLA_GO(ALONG, ONE, false);
     else COLA_GO(ALONG, TWO, false);
     else COLA_GO(ALONG, WIDE, false);
-    else COLA_GO(ALONG, WIDER, false);
     else COLA_GO(ONE, ONE, false);
     else COLA_GO(TWO, ONE, false);
     else COLA_GO(TWO, TWO, false);
@@ -21,9 +20,14 @@ hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t
     else COLA_GO(WIDE, TWO, false);
     else COLA_GO(WIDE, WIDE, false);
     else COLA_GO(WIDE, WIDE, true);
-    else COLA_GO(WIDER, WIDER, false);
-    else COLA_GO(WIDER, WIDER, true);
-    else return hipErrorInvalidValue;
+    else if constexpr (HD == 64) {
+        COLA_GO(ALONG, FOUR, false);
+        else COLA_GO(FOUR, FOUR, false);
+        else COLA_GO(ALONG, WIDER, false);
+        else COLA_GO(WIDER, WIDER, false);
+        else COLA_GO(WIDER, WIDER, true);
+        else return hipErrorInvalidValue;
+    } else return hipErrorInvalidValue;
 #undef COLA_GO
     return hipGetLastError();
 }
