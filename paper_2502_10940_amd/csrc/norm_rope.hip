@@ -190,12 +190,9 @@ __global__ __launch_bounds__(NTHR) void norm_rope_kernel(const NormRopeArgs a) {
     constexpr int NV = P::NV, NP = P::NP;
     constexpr int CH = MU > 1 ? 1 : 8 / NV;             // heads whose loads a thread has in flight
     const int L = a.group, per = a.lanes * L;           // threads of one row
-    int tl = 0, rem = (int)(blockIdx.y * NTHR + threadIdx.x);
-    if (per < NTHR) {
-        tl = rem / per;
-        rem -= tl * per;
-    }
-    if (tl >= a.tpw || rem >= per) return;              // whole groups
+    int rem = (int)(blockIdx.y * NTHR + threadIdx.x);
+    const int tl = rem / per;
+    rem -= tl * per;
     const int hl = rem / L, u0 = rem & (L - 1);
     typename P::At w;
     w.set(a, u0, L);
@@ -275,12 +272,9 @@ __global__ __launch_bounds__(NTHR) void norm_rope_bwd_kernel(const NormRopeArgs 
     constexpr int CH = MU > 1 ? 1 : 4 / NV;
     extern __shared__ float sums[];                     // [NTHR / 64][2][hd]
     const int L = a.group, per = a.lanes * L;
-    int tl = 0, rem = (int)(blockIdx.y * NTHR + threadIdx.x);
-    if (per < NTHR) {
-        tl = rem / per;
-        rem -= tl * per;
-    }
-    const bool active = tl < a.tpw && rem < per;
+    int rem = (int)(blockIdx.y * NTHR + threadIdx.x);
+    const int tl = rem / per;
+    rem -= tl * per;
     const int hl = rem / L, u0 = rem & (L - 1);
     typename P::At w;
     w.set(a, u0, L);
@@ -289,65 +283,64 @@ __global__ __launch_bounds__(NTHR) void norm_rope_bwd_kernel(const NormRopeArgs 
     if (a.gk) gk.load((const E*)a.gk, w);
     const int H = a.hq + a.hk;
     float dgq[MU][NV][PV] = {}, dgk[MU][NV][PV] = {};
-    if (active)
-        for (int64_t t = (int64_t)blockIdx.x * a.tpw + tl; t < a.T; t += (int64_t)gridDim.x * a.tpw) {
-            P x[CH], y[CH];
-            auto load = [&](int h0) __attribute__((always_inline)) {
+    for (int64_t t = (int64_t)blockIdx.x * a.tpw + tl; t < a.T; t += (int64_t)gridDim.x * a.tpw) {
+        P x[CH], y[CH];
+        auto load = [&](int h0) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                    const int h = h0 + j * a.lanes;
-                    if (h >= H) continue;
-                    x[j].load(source<E, false>(a, t, h), w);
-                    y[j].load(h < a.hq ? (const E*)a.dqo + t * a.ldqo + (int64_t)h * a.hd
-                                       : (const E*)a.dko + t * a.ldko + (int64_t)(h - a.hq) * a.hd, w);
-                }
-            };
-            load(hl);
-            Turn<BF16, MU, NP> turn;
-            turn.set(a, w, u0, L, t);
-            for (int h0 = hl; h0 < H; h0 += CH * a.lanes) {
-                if (h0 != hl) load(h0);
+            for (int j = 0; j < CH; ++j) {
+                const int h = h0 + j * a.lanes;
+                if (h >= H) continue;
+                x[j].load(source<E, false>(a, t, h), w);
+                y[j].load(h < a.hq ? (const E*)a.dqo + t * a.ldqo + (int64_t)h * a.hd
+                                   : (const E*)a.dko + t * a.ldko + (int64_t)(h - a.hq) * a.hd, w);
+            }
+        };
+        load(hl);
+        Turn<BF16, MU, NP> turn;
+        turn.set(a, w, u0, L, t);
+        for (int h0 = hl; h0 < H; h0 += CH * a.lanes) {
+            if (h0 != hl) load(h0);
 #pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                    const int h = h0 + j * a.lanes;
-                    if (h >= H) continue;
-                    float n[MU][NV][PV], z[MU][NV][PV];
-                    x[j].get(n);
-                    y[j].get(z);
-                    turn.template apply<INTER>(z, w);   // back: the sine has its sign
-                    const float r = inv_sqrt<BF16>(fmaf(group_sum(dot(n, n), L), a.inv_hd, a.eps));
-                    const bool is_q = h < a.hq;
-                    const bool scaled = (is_q ? a.gq : a.gk) != nullptr;
+            for (int j = 0; j < CH; ++j) {
+                const int h = h0 + j * a.lanes;
+                if (h >= H) continue;
+                float n[MU][NV][PV], z[MU][NV][PV];
+                x[j].get(n);
+                y[j].get(z);
+                turn.template apply<INTER>(z, w);   // back: the sine has its sign
+                const float r = inv_sqrt<BF16>(fmaf(group_sum(dot(n, n), L), a.inv_hd, a.eps));
+                const bool is_q = h < a.hq;
+                const bool scaled = (is_q ? a.gq : a.gk) != nullptr;
 #pragma unroll
-                    for (int m = 0; m < MU; ++m)
+                for (int m = 0; m < MU; ++m)
 #pragma unroll
-                        for (int v = 0; v < NV; ++v) {
-                            typename P::V g;
-                            g.r = is_q ? gq.x[m][v].r : gk.x[m][v].r;
-                            float s[PV];
-                            g.get(s);
+                    for (int v = 0; v < NV; ++v) {
+                        typename P::V g;
+                        g.r = is_q ? gq.x[m][v].r : gk.x[m][v].r;
+                        float s[PV];
+                        g.get(s);
 #pragma unroll
-                            for (int e = 0; e < PV; ++e) {
-                                n[m][v][e] *= r;
-                                const float d = z[m][v][e] * n[m][v][e];
-                                dgq[m][v][e] += is_q ? d : 0.0f;
-                                dgk[m][v][e] += is_q ? 0.0f : d;
-                                z[m][v][e] *= scaled ? s[e] : 1.0f;
-                            }
+                        for (int e = 0; e < PV; ++e) {
+                            n[m][v][e] *= r;
+                            const float d = z[m][v][e] * n[m][v][e];
+                            dgq[m][v][e] += is_q ? d : 0.0f;
+                            dgk[m][v][e] += is_q ? 0.0f : d;
+                            z[m][v][e] *= scaled ? s[e] : 1.0f;
                         }
-                    const float mean = group_sum(dot(n, z), L) * a.inv_hd;
+                    }
+                const float mean = group_sum(dot(n, z), L) * a.inv_hd;
 #pragma unroll
-                    for (int m = 0; m < MU; ++m)
+                for (int m = 0; m < MU; ++m)
 #pragma unroll
-                        for (int v = 0; v < NV; ++v)
+                    for (int v = 0; v < NV; ++v)
 #pragma unroll
-                            for (int e = 0; e < PV; ++e) z[m][v][e] = r * fmaf(-mean, n[m][v][e], z[m][v][e]);
-                    x[j].put(z);
-                    x[j].store(is_q ? (G)a.qo + t * a.ldq + (int64_t)h * a.hd
-                                    : (G)a.ko + t * a.ldk + (int64_t)(h - a.hq) * a.hd, w, a.past);
-                }
+                        for (int e = 0; e < PV; ++e) z[m][v][e] = r * fmaf(-mean, n[m][v][e], z[m][v][e]);
+                x[j].put(z);
+                x[j].store(is_q ? (G)a.qo + t * a.ldq + (int64_t)h * a.hd
+                                : (G)a.ko + t * a.ldk + (int64_t)(h - a.hq) * a.hd, w, a.past);
             }
         }
+    }
     // The groups of each wave, then the waves.
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -448,10 +441,13 @@ dim3 shape(bool bf16, NormKind kind, NormRopeArgs& a) {
     if (lanes < (H + CH - 1) / CH) lanes = (H + CH - 1) / CH;
     if (lanes > H) lanes = H;
     a.lanes = (int)lanes;
+    // as many rows as fill whole workgroups: the groups of a row may lie in two (1536 rows of
+    // 32 + 8 + 8 heads: 176 threads a row, 16 rows in 11 workgroups)
     const int64_t per = lanes * a.group;
-    a.tpw = per < NTHR ? (int)(NTHR / per) : 1;
+    const int64_t low = per & -per;                     // its power of two
+    a.tpw = low < NTHR ? (int)(NTHR / low) : 1;
+    const int64_t gy = a.tpw * per / NTHR;
     int64_t gx = (a.T + a.tpw - 1) / a.tpw;
-    const int64_t gy = per < NTHR ? 1 : (per + NTHR - 1) / NTHR;
     int64_t most = int64_t(1) << 20;
     if (kind == NORM_BWD) most = kParts / gy > 1 ? kParts / gy : 1;
     if (gx > most) gx = most;
