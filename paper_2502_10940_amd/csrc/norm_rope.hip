@@ -44,6 +44,26 @@ __device__ __forceinline__ float group_sum(float x, int L) {
     return x;
 }
 
+// The sum over a wave's groups of L lanes: lanes of one place in their group.
+__device__ __forceinline__ float across_groups(float x, int L) {
+    auto ror = [](float v, auto n) __attribute__((always_inline)) {
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + decltype(n)::value, 0xf, 0xf, true));
+    };
+    if (L < 64) {
+        const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    }
+    if (L < 32) {
+        const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    }
+    if (L < 16) x += ror(x, std::integral_constant<int, 8>{});
+    if (L < 8) x += ror(x, std::integral_constant<int, 4>{});
+    if (L < 4) x += ror(x, std::integral_constant<int, 2>{});
+    if (L < 2) x += ror(x, std::integral_constant<int, 1>{});
+    return x;
+}
+
 // 1 / sqrt(x): the hardware's (1 ulp) under a bf16 result, the rounded one under fp32.
 template <bool BF16>
 __device__ __forceinline__ float inv_sqrt(float x) {
@@ -351,8 +371,7 @@ __global__ __launch_bounds__(NTHR) void norm_rope_bwd_kernel(const NormRopeArgs 
             for (int v = 0; v < NV; ++v)
 #pragma unroll
                 for (int e = 0; e < PV; ++e) {
-                    float x = k ? dgk[m][v][e] : dgq[m][v][e];
-                    for (int d = L; d < 64; d <<= 1) x += __shfl_xor(x, d);
+                    const float x = across_groups(k ? dgk[m][v][e] : dgq[m][v][e], L);
                     const int at = w.at[m][v] + e;
                     if (lane < L && (v ? w.two[m] : w.one[m]) && at < a.hd) sums[(wave * 2 + k) * a.hd + at] = x;
                 }
