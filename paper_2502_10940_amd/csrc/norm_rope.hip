@@ -301,65 +301,62 @@ __global__ __launch_bounds__(NTHR) void norm_rope_bwd_kernel(const NormRopeArgs 
     P gq, gk;
     if (a.gq) gq.load((const E*)a.gq, w);
     if (a.gk) gk.load((const E*)a.gk, w);
-    const int H = a.hq + a.hk;
     float dgq[MU][NV][PV] = {}, dgk[MU][NV][PV] = {};
     for (int64_t t = (int64_t)blockIdx.x * a.tpw + tl; t < a.T; t += (int64_t)gridDim.x * a.tpw) {
-        P x[CH], y[CH];
-        auto load = [&](int h0) __attribute__((always_inline)) {
+        Turn<BF16, MU, NP> turn;
+        // This group's heads of q, or of k: one after the other, for each has its own gain.
+        auto heads = [&](const E* from, const E* grad, G to, int H, const P& gain, bool scaled, float (&dg)[MU][NV][PV],
+                         auto first) __attribute__((always_inline)) {
+            P x[CH], y[CH];
+            auto load = [&](int h0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < CH; ++j) {
-                const int h = h0 + j * a.lanes;
-                if (h >= H) continue;
-                x[j].load(source<E, false>(a, t, h), w);
-                y[j].load(h < a.hq ? (const E*)a.dqo + t * a.ldqo + (int64_t)h * a.hd
-                                   : (const E*)a.dko + t * a.ldko + (int64_t)(h - a.hq) * a.hd, w);
+                for (int j = 0; j < CH; ++j) {
+                    const int h = h0 + j * a.lanes;
+                    if (h >= H) continue;
+                    x[j].load(from + (int64_t)h * a.hd, w);
+                    y[j].load(grad + (int64_t)h * a.hd, w);
+                }
+            };
+            load(hl);
+            if constexpr (decltype(first)::value) turn.set(a, w, u0, L, t);
+            for (int h0 = hl; h0 < H; h0 += CH * a.lanes) {
+                if (h0 != hl) load(h0);
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    const int h = h0 + j * a.lanes;
+                    if (h >= H) continue;
+                    float n[MU][NV][PV], z[MU][NV][PV];
+                    x[j].get(n);
+                    y[j].get(z);
+                    turn.template apply<INTER>(z, w);   // back: the sine has its sign
+                    const float r = inv_sqrt<BF16>(fmaf(group_sum(dot(n, n), L), a.inv_hd, a.eps));
+#pragma unroll
+                    for (int m = 0; m < MU; ++m)
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            float s[PV];
+                            gain.x[m][v].get(s);
+#pragma unroll
+                            for (int e = 0; e < PV; ++e) {
+                                n[m][v][e] *= r;
+                                dg[m][v][e] = fmaf(z[m][v][e], n[m][v][e], dg[m][v][e]);
+                                if (scaled) z[m][v][e] *= s[e];
+                            }
+                        }
+                    const float mean = group_sum(dot(n, z), L) * a.inv_hd;
+#pragma unroll
+                    for (int m = 0; m < MU; ++m)
+#pragma unroll
+                        for (int v = 0; v < NV; ++v)
+#pragma unroll
+                            for (int e = 0; e < PV; ++e) z[m][v][e] = r * fmaf(-mean, n[m][v][e], z[m][v][e]);
+                    x[j].put(z);
+                    x[j].store(to + (int64_t)h * a.hd, w, a.past);
+                }
             }
         };
-        load(hl);
-        Turn<BF16, MU, NP> turn;
-        turn.set(a, w, u0, L, t);
-        for (int h0 = hl; h0 < H; h0 += CH * a.lanes) {
-            if (h0 != hl) load(h0);
-#pragma unroll
-            for (int j = 0; j < CH; ++j) {
-                const int h = h0 + j * a.lanes;
-                if (h >= H) continue;
-                float n[MU][NV][PV], z[MU][NV][PV];
-                x[j].get(n);
-                y[j].get(z);
-                turn.template apply<INTER>(z, w);   // back: the sine has its sign
-                const float r = inv_sqrt<BF16>(fmaf(group_sum(dot(n, n), L), a.inv_hd, a.eps));
-                const bool is_q = h < a.hq;
-                const bool scaled = (is_q ? a.gq : a.gk) != nullptr;
-#pragma unroll
-                for (int m = 0; m < MU; ++m)
-#pragma unroll
-                    for (int v = 0; v < NV; ++v) {
-                        typename P::V g;
-                        g.r = is_q ? gq.x[m][v].r : gk.x[m][v].r;
-                        float s[PV];
-                        g.get(s);
-#pragma unroll
-                        for (int e = 0; e < PV; ++e) {
-                            n[m][v][e] *= r;
-                            const float d = z[m][v][e] * n[m][v][e];
-                            dgq[m][v][e] += is_q ? d : 0.0f;
-                            dgk[m][v][e] += is_q ? 0.0f : d;
-                            z[m][v][e] *= scaled ? s[e] : 1.0f;
-                        }
-                    }
-                const float mean = group_sum(dot(n, z), L) * a.inv_hd;
-#pragma unroll
-                for (int m = 0; m < MU; ++m)
-#pragma unroll
-                    for (int v = 0; v < NV; ++v)
-#pragma unroll
-                        for (int e = 0; e < PV; ++e) z[m][v][e] = r * fmaf(-mean, n[m][v][e], z[m][v][e]);
-                x[j].put(z);
-                x[j].store(is_q ? (G)a.qo + t * a.ldq + (int64_t)h * a.hd
-                                : (G)a.ko + t * a.ldk + (int64_t)(h - a.hq) * a.hd, w, a.past);
-            }
-        }
+        heads((const E*)a.q + t * a.ldq, (const E*)a.dqo + t * a.ldqo, (G)a.qo + t * a.ldq, a.hq, gq, a.gq != nullptr, dgq, std::true_type{});
+        heads((const E*)a.k + t * a.ldk, (const E*)a.dko + t * a.ldko, (G)a.ko + t * a.ldk, a.hk, gk, a.gk != nullptr, dgk, std::false_type{});
     }
     // The groups of each wave, then the waves.
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -449,13 +446,14 @@ dim3 shape(bool bf16, NormKind kind, NormRopeArgs& a) {
     a.units = a.turning + (a.interleaved ? copied : (copied + 1) / 2);
     a.group = 1;
     while (a.group < a.units && a.group < 64) a.group *= 2;
-    const int H = a.hq + (kind == NORM_APPEND ? 2 : 1) * a.hk;
+    // the heads that a row's groups share out: backward those of q, then those of k
+    const int H = kind == NORM_BWD ? (a.hq > a.hk ? a.hq : a.hk) : a.hq + (kind == NORM_APPEND ? 2 : 1) * a.hk;
     const int CH = a.units > 64 ? 1 : (kind == NORM_BWD ? 4 : 8) / (a.interleaved ? 1 : 2);
     const int es = bf16 ? 2 : 4;
     // large results past the caches, as in rope.hip
     const int64_t pq = kind == NORM_BWD ? a.ldq : a.ldqo, pk = kind == NORM_BWD ? a.ldk : a.ldko;
     a.past = ((pq * es | pk * es | (int64_t)(uintptr_t)a.qo | (int64_t)(uintptr_t)a.ko) & 63) == 0 &&
-             (double)a.T * H * a.hd * es > 48e6;
+             (double)a.T * (a.hq + a.hk) * a.hd * es > 48e6;
     int64_t lanes = (int64_t(1) << 18) / (a.T * a.group) + 1;
     if (lanes < (H + CH - 1) / CH) lanes = (H + CH - 1) / CH;
     if (lanes > H) lanes = H;
