@@ -457,6 +457,9 @@ dim3 shape(bool bf16, NormKind kind, NormRopeArgs& a) {
     int64_t lanes = (int64_t(1) << 18) / (a.T * a.group) + 1;
     if (lanes < (H + CH - 1) / CH) lanes = (H + CH - 1) / CH;
     if (lanes > H) lanes = H;
+    // Rows of many heads take whole workgroups each (some groups then have no head), or the
+    // rows that fill them would ask for a grid past its second axis.
+    if (lanes * a.group > 8 * NTHR) lanes = (lanes + NTHR / a.group - 1) / (NTHR / a.group) * (NTHR / a.group);
     a.lanes = (int)lanes;
     // as many rows as fill whole workgroups: the groups of a row may lie in two (1536 rows of
     // 32 + 8 + 8 heads: 176 threads a row, 16 rows in 11 workgroups)

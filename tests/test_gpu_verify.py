@@ -221,6 +221,23 @@ def test_large_norm_results_are_the_small_ones(dtype, layout):
         assert (np.abs(f64(got) - ref) <= bound).all() and np.abs(f64(got) - ref).max() < 2.0 ** -12 * np.abs(ref).max()
 
 
+# rows of many heads, an odd number of them; single rows; one element a head
+@pytest.mark.parametrize("T, hq, hk, hd, rot", [(1, 4099, 3, 64, 64), (3, 1025, 1026, 8, 8), (2, 70001, 5, 1, 0), (5, 129, 700, 80, 40), (1, 1, 9001, 3, 2)])
+def test_norm_rope_of_many_heads(T, hq, hk, hd, rot):
+    q, k, dq, dk = (rand(i, (T, h * hd), "bf16") for i, h in enumerate((hq, hk, hq, hk)))
+    gq, gk = gain(5, hd, "bf16"), gain(6, hd, "bf16")
+    pos = np.random.default_rng(T).integers(0, 5000, T)
+    d = cola.rope_desc(T, hq, hk, hd, rot)
+    o, dx, dg = [torch.empty_like(q), torch.empty_like(k)], [torch.empty_like(q), torch.empty_like(k)], [torch.empty(hd, device=DEV) for _ in range(2)]
+    cola.norm_rope_fwd(d, q, k, gq, gk, i32(pos), *o)
+    cola.norm_rope_bwd(d, dq, dk, q, k, gq, gk, i32(pos), *dx, *dg, workspace(d))
+    for x, dy, g, y, u, v in ((q, dq, gq, o[0], dx[0], dg[0]), (k, dk, gk, o[1], dx[1], dg[1])):
+        ref, bound = W.norm_rope(f64(x), f64(g), hd, rot, pos, "bf16")
+        assert (np.abs(f64(y) - ref) <= bound).all()
+        (rx, bx), (rg, bg) = W.norm_rope_bwd(f64(dy), f64(x), f64(g), hd, rot, pos, "bf16")
+        assert (np.abs(f64(u) - rx) <= bx).all() and (np.abs(f64(v) - rg) <= bg).all()
+
+
 def test_norm_gradients_do_not_depend_on_the_workspace_s_contents_or_the_run():
     T, hq, hk, hd = 700, 5, 3, 96
     q, k, dq, dk = (rand(i, (T, h * hd), "bf16") for i, h in enumerate((hq, hk, hq, hk)))
@@ -382,15 +399,23 @@ def test_a_chain_sees_what_causal_rows_see(name):
         assert torch.equal(out, want) and torch.equal(lse, wl)
 
 
-# few requests with long caches: parts cut by the lengths, under bounds near and far; the
-# largest number of requests that are counted, and one more
+# Few requests with long caches: parts cut by the lengths, under bounds near and far; the
+# largest number of requests that are counted, and one more; and kinds that no other case has
+CUT = {"near": ([40, 100, 7], [5000, 300, 7000], 0, 2, 1, None), "far": ([40, 100, 7], [5000, 300, 7000], 0, 2, 1, 60000),
+       "empty": ([129, 0, 35], [3000, 40, 35], 0, 1, 1, 9000), "prefix": ([70, 33], [2500, 6000], 1300, 2, 2, None), "one": ([200], [9000], 0, 4, 2, None),
+       "mixed": ([34, 256, 1, 90], [34, 4000, 5000, 90], 0, 1, 1, None), "256": ([5] * 255 + [36], [5 + 3 * i for i in range(255)] + [1500], 0, 1, 1, 4000),
+       "257": ([5] * 256 + [36], [5 + i for i in range(256)] + [1500], 0, 1, 1, 4000), "wide": ([100, 80], [5000, 3000], 0, 1, 1, None),
+       "wide-prefix": ([100, 80], [900, 300], 1300, 1, 1, None), "wider-prefix": ([200, 180], [500, 700], 1300, 1, 1, None),
+       "along-four": ([40, 60, 9], [70, 60, 30], 90, 1, 1, None), "along-wider": ([200, 150], [220, 150], 90, 1, 1, None), "four-prefix": ([40, 9], [900, 300], 1300, 1, 1, None),
+       "wider-many": ([130] * 40, [130 + 20 * i for i in range(40)], 0, 8, 8, None),
+       "wide-direct": ([70, 80], [200, 90], 0, 1, 1, None), "wider-direct": ([150, 80], [200, 90], 0, 1, 1, None)}
+
+
 @pytest.mark.parametrize("hd", (64, 128))
-@pytest.mark.parametrize("new, kv, L, hq, hk, max_kv", [
-    ([40, 100, 7], [5000, 300, 7000], 0, 2, 1, None), ([40, 100, 7], [5000, 300, 7000], 0, 2, 1, 60000), ([129, 0, 35], [3000, 40, 35], 0, 1, 1, 9000),
-    ([70, 33], [2500, 6000], 1300, 2, 2, None), ([200], [9000], 0, 4, 2, None), ([34, 256, 1, 90], [34, 4000, 5000, 0], 0, 1, 1, None),
-    ([5] * 255 + [36], [5 + 3 * i for i in range(255)] + [1500], 0, 1, 1, 4000), ([5] * 256 + [36], [5 + i for i in range(256)] + [1500], 0, 1, 1, 4000)],
-    ids=("near", "far", "empty", "prefix", "one", "mixed", "256", "257"))
-def test_tree_attention_cut_by_the_lengths(new, kv, L, hq, hk, max_kv, hd):
+@pytest.mark.parametrize("name", sorted(CUT))
+def test_tree_attention_cut_by_the_lengths(name, hd):
+    new, kv, L, hq, hk, max_kv = CUT[name]
+    print("trees", name, hd, flush=True)
     TreeBatch(40 + hd, new, kv, L, hq, hk, hd, 64, masks="any", max_kv=max_kv, pad=3).check()
 
 
@@ -655,6 +680,41 @@ def test_logits_do_not_depend_on_the_run():
         assert torch.equal(a, r.run())
 
 
+def test_logits_with_long_lists_of_biases():
+    """More entries than a workgroup has threads, most tokens named several times: the last counts."""
+    Rows(9, [3, 2], 3001, "f32", n_bias=1500, without=("allowed",)).check()
+    Rows(10, [1, 4], 50, "bf16", n_bias=700).check()
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_large_logits_are_the_small_ones(dtype):
+    """Many rows of a large vocabulary, several to a workgroup and past the caches: each
+    request's rows have the bits that they get alone."""
+    rows = [(7 * i) % 49 for i in range(60)]
+    r = Rows(12, rows, 90001, dtype, max_hist=700, n_bias=40)
+    out = r.run()
+    whole, start = r.tensors(), r.start
+    for q in (1, 20, 48, 59):
+        lo, hi = start[q], start[q + 1]
+        if lo == hi:
+            continue
+        u = {k: v for k, v in whole.items()}
+        for k in ("history", "prompt_len", "hist_len", "repetition", "presence", "frequency"):
+            u[k] = whole[k][q:q + 1].contiguous()
+        u["bias_start"] = whole["bias_start"][q:q + 2].contiguous()
+        for k in ("draft", "mask", "allowed_row"):
+            u[k] = whole[k][lo:hi].contiguous()
+        d = cola.logits_desc(hi - lo, r.V, 1, r.max_hist, r.max_new, dtype, len(r.u["bias"]), len(r.u["allowed"]))
+        got = torch.empty((hi - lo, r.V), dtype=DT[dtype], device=DEV)
+        cola.logits_adjust(d, cola.logits_rules(**u), r.l[lo:hi].contiguous(), i32([0, hi - lo]), got)
+        assert torch.equal(torch.nan_to_num(out[lo:hi].float()), torch.nan_to_num(got.float()))
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_logits_of_a_vocabulary_of_many_chunks(dtype):
+    Rows(13, [48, 3], 90001, dtype, max_hist=300, n_bias=30, ldl=90013, ldo=90010).check()
+
+
 def test_logits_past_4_gib():
     """Rows past 2^32 bytes: the bits that they get alone."""
     V, T = 1 << 20, 2050
@@ -669,3 +729,278 @@ def test_logits_past_4_gib():
     last = l[-2].clone()
     cola.logits_adjust(d(T), cola.logits_rules(**many), l, None, l)
     assert torch.equal(l[-1:], want) and not torch.equal(l[-2], last) and l[1000, 5] == -0.5 and l[1000, 9] == 0
+
+
+# ---------------------------------------------------------------------------
+# together
+# ---------------------------------------------------------------------------
+
+class Verifier:
+    """A layer's cache, requests and their trees: tables, masks, append, attention and
+    logits of a step that verifies drafted tokens, and the kept path's way to its place."""
+
+    def __init__(self, n, hq, hk, hd, page, L, cap, max_new, V=500, seed=0):
+        self.n, self.hq, self.hk, self.hd, self.page, self.L, self.cap, self.max_new, self.V = n, hq, hk, hd, page, L, cap, max_new, V
+        self.rng = np.random.default_rng(seed)
+        self.width = 8
+        shared = -(-L // page)
+        self.pages = shared + n * self.width
+        ids = self.rng.permutation(self.pages)
+        self.K = torch.full((self.pages, hk, page, hd), math.nan, dtype=torch.bfloat16, device=DEV)
+        self.V_ = self.K.clone()
+        self.ptab, self.free = i32(ids[:shared]), i32(ids[shared:])
+        z = lambda *s, dt=torch.int32: torch.zeros(s, dtype=dt, device=DEV)
+        self.kv, self.new, self.table, self.start = z(n), z(n), z(n, self.width) - 1, z(n + 1)
+        self.slots, self.rows, self.pos, self.at, self.next = z(cap), z(cap), z(cap), z(1), z(1)
+        self.parent, self.draft, self.kept = z(cap), z(cap), z(cap) - 1
+        self.mask = z(cap, -(-max_new // 64), dt=torch.int64)
+        self.x = z(cap, (hq + 2 * hk) * hd, dt=torch.bfloat16)
+        self.qr, self.out, self.lse = z(cap, hq * hd, dt=torch.bfloat16), z(cap, hq * hd, dt=torch.bfloat16), z(hq, cap, dt=torch.float32)
+        self.gq, self.gk = gain(seed + 1, hd, "bf16"), gain(seed + 2, hd, "bf16")
+        self.l, self.chosen = z(cap, V, dt=torch.float32), z(cap, V, dt=torch.float32)
+        self.c = cola.cache_desc(self.pages, page, hk, hd)
+        ld = self.x.stride(0)
+        self.rd = cola.rope_desc(cap, hq, hk, hd, ldq=ld, ldk=ld, ldv=ld)
+        self.again = cola.rope_desc(cap, 0, hk, hd, ldk=ld, ldv=ld)
+        self.md = cola.page_map_desc(n, cap, page, self.width, self.free.numel(), L)
+        self.td = cola.tree_map_desc(n, cap, max_new, L)
+        self.ad = cola.prefix_attn_desc(n, cap, hq, L, self.width * page, max_new)
+        self.ws = torch.empty(max(1, cola.tree_attn_workspace_bytes(self.ad, self.c)), dtype=torch.uint8, device=DEV)
+        self.history, self.hist_len = i32(self.rng.integers(0, V, (n, 300))), z(n)
+        self.ld = cola.logits_desc(cap, V, n, 300, max_new)
+        self.rules = cola.logits_rules(history=self.history, hist_len=self.hist_len, draft=self.draft, mask=self.mask,
+                                       repetition=torch.full((n,), 1.2, device=DEV), presence=torch.full((n,), 0.3, device=DEV))
+        self.past = [(np.zeros((0, hk * hd)), np.zeros((0, hk * hd)))] * n      # each request's normalised, turned keys, and values
+        if L:
+            k, v = rand(seed + 3, (L, hk * hd), "bf16"), rand(seed + 4, (L, hk * hd), "bf16")
+            j = torch.arange(L, device=DEV)
+            slots = (self.ptab.long()[j // page] * page + j % page).int()
+            cola.norm_append(cola.rope_desc(L, 0, hk, hd), self.c, None, k, v, None, self.gk, None, slots, None, self.K, self.V_)
+            self.past = [(self.key(f64(k), np.arange(L)), f64(v))] * n
+
+    def part(self, name):
+        a, b = self.hq * self.hd, (self.hq + self.hk) * self.hd
+        return {"q": self.x[:, :a], "k": self.x[:, a:b], "v": self.x[:, b:]}[name]
+
+    def key(self, k, pos):
+        return W.norm_rope(k, f64(self.gk), self.hd, self.hd, pos, "bf16")[0]
+
+    def feed(self, new, seed):
+        """Trees of `new` nodes, their rows, and logits."""
+        rng = np.random.default_rng(seed)
+        self.new.copy_(i32(new))
+        self.kv += self.new
+        self.trees = [W.random_tree(rng, n) for n in new]
+        parent = np.concatenate([np.asarray(t, int) for t in self.trees] + [np.full(self.cap - sum(new), 99)])
+        self.parent.copy_(i32(parent))
+        self.draft.copy_(i32(rng.integers(0, self.V, self.cap)))
+        self.x.copy_(rand(seed, tuple(self.x.shape), "bf16"))
+        self.l.copy_(rand(seed + 1, tuple(self.l.shape), "f32"))
+        self.hist_len.copy_(i32(rng.integers(0, 300, self.n)))
+
+    def step(self, stream=None):
+        cola.page_map(self.md, self.kv, self.new, self.free, self.at, self.table, self.start, self.slots, self.rows, self.next, stream=stream)
+        cola.tree_map(self.td, self.parent, self.kv, self.start, self.mask, self.pos, stream=stream)
+        cola.norm_append(self.rd, self.c, self.part("q"), self.part("k"), self.part("v"), self.gq, self.gk, self.pos, self.slots, self.qr,
+                         self.K, self.V_, stream=stream)
+        cola.tree_attn(self.ad, self.c, self.qr, self.K, self.V_, self.ptab if self.L else None, self.table, self.kv, self.start, self.mask,
+                       self.out, self.lse, self.ws, stream=stream)
+        cola.logits_adjust(self.ld, self.rules, self.l, self.start, self.chosen, stream=stream)
+
+    def keep(self, paths):
+        """The path's j-th node into the slot of node j: rows' k and v once more."""
+        slots, kept = self.slots.cpu().numpy(), np.full(self.cap, -1)
+        row = 0
+        for tree, path in zip(self.trees, paths):
+            for j, i in enumerate(path):
+                kept[row + i] = slots[row + j]
+            row += len(tree)
+        self.kept.copy_(i32(kept))
+        cola.norm_append(self.again, self.c, None, self.part("k"), self.part("v"), None, self.gk, self.pos, self.kept, None, self.K, self.V_)
+        self.kv += i32([len(p) for p in paths]) - self.new
+        self.at.copy_(self.next)
+
+    def path(self, r, i):
+        """Node i of request r and its ancestors, the root first."""
+        p = [i]
+        while self.trees[r][p[0]] >= 0:
+            p.insert(0, self.trees[r][p[0]])
+        return p
+
+    def check(self, paths):
+        """Each row against its request's sequence as it would be after its path, in 64 bits."""
+        torch.cuda.synchronize()
+        q, k, v = (f64(self.part(x).contiguous()) for x in "qkv")
+        row = 0
+        for r, tree in enumerate(self.trees):
+            ks, vs = self.past[r]
+            p0 = len(ks)
+            for i in range(len(tree)):
+                path = self.path(r, i)
+                pos = p0 + np.arange(len(path))
+                assert int(self.pos[row + i]) == pos[-1]
+                at = [row + j for j in path]
+                kk, vv = np.concatenate([ks, self.key(k[at], pos)]), np.concatenate([vs, v[at]])
+                qs = W.norm_rope(q[row + i:row + i + 1], f64(self.gq), self.hd, self.hd, pos[-1:], "bf16")[0][0]
+                for h in range(self.hq):
+                    x, y = slice(h * self.hd, (h + 1) * self.hd), h // (self.hq // self.hk)
+                    y = slice(y * self.hd, (y + 1) * self.hd)
+                    s = kk[:, y] @ qs[x] / math.sqrt(self.hd)
+                    w = np.exp(s - s.max())
+                    w /= w.sum()
+                    # q and k rounded to bf16: scores to 2^-7 of |q||k|/sqrt(hd) a product, weights by e^that
+                    ds = 2.0 ** -7 * (np.abs(kk[:, y]) @ np.abs(qs[x]) / math.sqrt(self.hd)).max()
+                    tol = (2 * (math.exp(ds) - 1) + 2.0 ** -6) * (w @ np.abs(vv[:, y])) + 2.0 ** -8
+                    assert (np.abs(f64(self.out[row + i, x]) - w @ vv[:, y]) <= tol).all(), (r, i, h)
+            at = [row + j for j in paths[r]]
+            self.past[r] = (np.concatenate([ks, self.key(k[at], p0 + np.arange(len(at)))]), np.concatenate([vs, v[at]]))
+            row += len(tree)
+        assert (self.out[row:] == 0).all() and (self.chosen[row:] == 0).all(), "idle rows are left"
+        history, n = self.history.cpu().numpy(), self.hist_len.cpu().numpy()
+        ref, bound, _ = W.logits(f64(self.l), self.start.cpu().tolist(), self.V, history=history, hist_len=n, draft=self.draft.cpu().numpy(),
+                                 masks=[int(w[0]) & 2 ** 64 - 1 for w in self.mask.cpu().tolist()], repetition=np.full(self.n, np.float32(1.2)),
+                                 presence=np.full(self.n, np.float32(0.3)))
+        assert (np.abs(f64(self.chosen[:row]) - ref[:row]) <= bound[:row]).all()
+
+
+@pytest.mark.parametrize("shape", [(5, 4, 2, 64, 16, 21, 60, 12), (3, 2, 2, 128, 32, 0, 40, 20), (2, 8, 2, 64, 16, 40, 120, 50)], ids=str)
+def test_verifying_steps(shape):
+    """Trees, a path kept of each, and on from there: five steps."""
+    s = Verifier(*shape)
+    rng = np.random.default_rng(shape[0])
+    for i in range(5):
+        new = rng.integers(1, shape[-1] + 1, s.n)
+        if i == 2:
+            new[-1] = 0
+        if i == 3:
+            new[:] = 1
+        s.out.zero_(), s.chosen.zero_()
+        s.feed(new, 100 + i)
+        s.step()
+        paths = [s.path(r, int(rng.integers(0, n))) if n else [] for r, n in enumerate(new)]
+        s.check(paths)
+        s.keep(paths)
+
+
+def test_verifying_step_in_a_graph():
+    """One captured step replayed: it follows lengths, trees, tables and histories; eager
+    work and synchronisations between the replays."""
+    s, e = (Verifier(4, 4, 2, 64, 16, 33, 64, 16) for _ in range(2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for x in (s, e):
+        x.feed([1, 2, 3, 4], 1)
+    with torch.cuda.stream(side):
+        s.step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.step()
+    rng = np.random.default_rng(9)
+    e.step()
+    for i, new in enumerate(([16, 1, 7, 1], [1, 1, 1, 1], [0, 9, 16, 1], [5, 5, 5, 5])):
+        paths = [x.path(r, int(rng.integers(0, len(t)))) if t else [] for r, t in enumerate(e.trees) for x in (e,)]
+        for x in (s, e):
+            x.keep(paths)
+            x.out.zero_(), x.chosen.zero_()
+            x.feed(new, 60 + i)
+        g.replay()
+        e.step()
+        torch.cuda.synchronize()
+        for a, b in ((s.out, e.out), (s.mask, e.mask), (s.pos, e.pos), (s.slots, e.slots), (s.chosen, e.chosen), (s.table, e.table)):
+            assert torch.equal(a, b)
+        assert torch.equal(torch.nan_to_num(s.K), torch.nan_to_num(e.K)) and torch.equal(torch.nan_to_num(s.V_), torch.nan_to_num(e.V_))
+
+
+def test_norm_gradients_in_a_graph():
+    """Captured with its two launches, replayed on other rows."""
+    T, hq, hk, hd = 500, 6, 2, 64
+    q, k, dq, dk = (rand(i, (T, h * hd), "bf16") for i, h in enumerate((hq, hk, hq, hk)))
+    gq, gk = gain(5, hd, "bf16"), gain(6, hd, "bf16")
+    d = cola.rope_desc(T, hq, hk, hd, seq_len=100)
+    ws = workspace(d)
+    o = [torch.empty_like(q), torch.empty_like(k), torch.empty(hd, device=DEV), torch.empty(hd, device=DEV)]
+    e = [torch.empty_like(t) for t in o]
+    cola.norm_rope_bwd(d, dq, dk, q, k, gq, gk, None, *o, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cola.norm_rope_bwd(d, dq, dk, q, k, gq, gk, None, *o, ws)
+    for i in range(4):
+        q.copy_(rand(20 + i, (T, hq * hd), "bf16"))
+        for t in o:
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        cola.norm_rope_bwd(d, dq, dk, q, k, gq, gk, None, *e, workspace(d))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(o, e))
+
+
+def test_two_graphs_of_trees_share_a_workspace():
+    """Replayed one after the other, each leaves what it leaves alone."""
+    made = []
+    for seed, new, kv, hd in ((20, [5, 60], [200, 3000], 64), (21, [40, 35], [2500, 90], 64)):
+        b = TreeBatch(seed, new, kv, 0, 4, 2, hd, 16)
+        made.append((b, b.run()))
+    n = max(cola.tree_attn_workspace_bytes(*b.desc()) for b, _ in made)
+    assert n > 0
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    graphs = []
+    for b, _ in made:
+        d, c = b.desc()
+        t = [i32(x) for x in (b.tab, b.kv, b.start)] + [torch.from_numpy(W.words(b.masks, b.max_new)).to(DEV)]
+        out, lse = torch.zeros_like(b.q), torch.zeros((b.hq, b.T), device=DEV)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cola.tree_attn(d, c, b.q, b.K, b.V, None, *t, out, lse, ws)
+        graphs.append((g, out, lse, t))
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1), (1, 0, 1, 0)):
+        for g, out, lse, _ in graphs:
+            out.zero_(), lse.zero_()
+        for i in order:
+            graphs[i][0].replay()
+        torch.cuda.synchronize()
+        for (_, out, lse, _), (b, (want, wl)) in zip(graphs, made):
+            assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+def test_two_streams_verify_at_once():
+    """Two programs on two streams, each with its own buffers: the serial results."""
+    a, b = Verifier(6, 8, 2, 128, 16, 50, 100, 16), Verifier(6, 8, 2, 128, 16, 50, 100, 16, seed=5)
+    want = []
+    for s in (a, b):
+        s.feed([16, 3, 9, 1, 12, 16], 7)
+        s.step()
+        torch.cuda.synchronize()
+        want.append((s.out.clone(), s.chosen.clone()))
+        s.out.zero_(), s.chosen.zero_()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, st in zip((a, b), streams):
+            s.step(stream=st)
+    torch.cuda.synchronize()
+    for s, (out, chosen) in zip((a, b), want):
+        assert torch.equal(s.out, out) and torch.equal(s.chosen, chosen)
+
+
+def test_timing_classes_count_the_launches_of_a_verifying_step():
+    s = Verifier(2, 2, 2, 64, 16, 20, 16, 8)
+    s.feed([5, 8], 3)
+    d = cola.rope_desc(4, 2, 2, 64)
+    x = [rand(i, (4, 128), "bf16") for i in range(6)]
+    dg = [torch.empty(64, device=DEV) for _ in range(2)]
+    cola.timing_enable(True)
+    cola.timing_reset()
+    try:
+        s.step()
+        cola.norm_rope_fwd(d, x[0], x[1], None, None, None, x[2], x[3])
+        cola.norm_rope_bwd(d, x[2], x[3], x[0], x[1], None, None, None, x[4], x[5], *dg, workspace(d))
+        n = {k: cola.timing_read(i)[0] for i, k in enumerate(cola.KERNEL_CLASSES)}
+    finally:
+        cola.timing_enable(False)
+        cola.timing_reset()
+    assert n["pointwise"] == 3 and n["attn_fwd"] == 1 and n["norm"] == 2 and n["norm_bwd"] == 2 and sum(n.values()) == 8

@@ -11,7 +11,7 @@ import torch
 import serve_ref as R
 import verify_ref as W
 from paper_2502_10940_amd import cola
-from test_serve_abi import BF, FAKE, I32, attn_args, refused
+from test_serve_abi import BF, FAKE, I32, KINDS, Plan, Shape, attn_args, refused
 
 
 # ---- norms ----
@@ -166,6 +166,38 @@ def test_reference_masks_and_attention():
     assert W.words([1 << 70 | 5], 100).tolist() == [[5, 64]]
 
 
+def tree_plan(n_req, T, hq, hk, hd, prefix, max_kv, max_new, page=16):
+    f = cola.lib()._ZN4cola14plan_tree_attnERKNS_15PrefixAttnShapeE
+    f.restype, f.argtypes = Plan, [ctypes.POINTER(Shape)]
+    p = f(ctypes.byref(Shape(n_req, T, max_new, prefix, max_kv, -(-max_kv // page), 1 << 20, page, hq, hk, hd, hq * hd, hq * hd, hd ** -0.5)))
+    d, c = cola.prefix_attn_desc(n_req, T, hq, prefix, max_kv, max_new), cola.cache_desc(1 << 20, page, hk, hd)
+    assert p.rows == T * hq and p.ws_bytes == cola.tree_attn_workspace_bytes(d, c)
+    return p
+
+
+@pytest.mark.parametrize("hd", (64, 128))
+def test_gpu_tests_of_trees_run_every_kernel(hd):
+    """The plans of the GPU tests' batches: every pair of kinds that there is a kernel for,
+    the parts cut by the lengths among them."""
+    from test_gpu_verify import CUT, TREES
+    seen = set()
+    cases = [(len(new), sum(new) + 2, hq, hk, L, max(kv), max(new)) for new, kv, L, hq, hk in TREES.values()]
+    cases += [(len(new), sum(new) + 3, hq, hk, L, max_kv or max(kv), max(new)) for new, kv, L, hq, hk, max_kv in CUT.values()]
+    for n, T, hq, hk, L, max_kv, max_new in cases:
+        p = tree_plan(n, T, hq, hk, hd, L, max_kv, max_new, 16 if hd == 64 else 64)
+        wide = p.kind_s in (8, 16)
+        full = 512 if hd == 128 or p.kind_s == 16 else 1024
+        counted = wide and p.splits_s > 1 and n <= 256 and n * p.tiles_s * hk < full // 2
+        seen.add((p.kind_p, p.kind_s, counted))
+    k = dict(KINDS, four=6, wider=16)
+    every = [("along", "one"), ("along", "two"), ("along", "wide"), ("one", "one"), ("two", "one"), ("two", "two"), ("wide", "one"), ("wide", "two"),
+             ("wide", "wide"), ("wide", "wide", True)]
+    if hd == 64:
+        every += [("along", "four"), ("four", "four"), ("along", "wider"), ("wider", "wider"), ("wider", "wider", True)]
+    every = {(k[x[0]], k[x[1]], len(x) > 2) for x in every}
+    assert seen == every, (sorted(every - seen), sorted(seen - every))
+
+
 # ---- logits ----
 
 def test_logits_refusals():
@@ -174,8 +206,8 @@ def test_logits_refusals():
     def call(d, logits=FAKE, start=None, out=FAKE + 4096, rules=None, **u):
         cola.logits_adjust(d, cola.logits_rules(**u) if rules is None else rules, logits, start, out, 0)
 
-    for bad in (D(-1, 8, 1), D(4, 0, 1), D(4, (1 << 22) + 1, 1), D(4, 8, -1), D(4, 8, 65536), D(4, 8, 1, -1), D(4, 8, 1, 1 << 31),
-                D(4, 8, 1, 4, -1), D(4, 8, 1, 4, 257), D(4, 8, 1, n_bias=-1), D(4, 8, 1, n_allowed=-1), D(4, 8, 1, ldl=7),
+    for bad in (D(-1, 8, 1), D(4, 0, 1), D(4, (1 << 22) + 1, 1), D(4, 8, -1), D(4, 8, 65536), D(4, 8, 1, -1), D(4, 8, 1, 1 << 30),
+                D(4, 8, 1, 4, -1), D(4, 8, 1, 4, 257), D(4, 8, 1, n_bias=-1), D(4, 8, 1, n_bias=1 << 30), D(4, 8, 1, n_allowed=-1), D(4, 8, 1, ldl=7),
                 D(4, 8, 1, ldo=7), D(4, 64, 1, lda=1), D(1 << 31, 8, 1), D(4, 8, 1, ldl=(1 << 22) + 1)):
         refused(cola.ERR_BAD_SHAPE, call, bad)
     refused(cola.ERR_INVALID_ARG, call, D(4, 8, 1, dtype=9))

@@ -12,7 +12,8 @@ TRIG = {"bf16": 2.0 ** -17, "f32": 2.0 ** -21}
 
 
 def heads(x, hd):
-    return np.array(x, dtype=np.float64).reshape(len(x), -1, hd)
+    x = np.array(x, dtype=np.float64)
+    return x.reshape(len(x), x.shape[1] // hd, hd)
 
 
 def normed(x, g, hd, eps):
@@ -35,7 +36,7 @@ def norm_rope(x, g, hd, rot, pos, dtype, layout="half", eps=1e-6, mscale=0.0, **
     to hd 2^-24, r to half of that and its own instruction's 2^-23; two products, 2^-24
     each: (hd / 2 + 6) 2^-24 in all; then the turn (serve_ref.rope_bound)."""
     _, z, _ = normed(x, g, hd, eps)
-    flat = z.reshape(len(z), -1)
+    flat = z.reshape(len(z), z.shape[1] * hd)
     y = R.rope(flat, z.shape[1], hd, rot, pos, layout, False, mscale, **scaling)
     m = mscale or R.frequencies(max(rot, 4), **scaling)[1]
     rel = (hd / 2 + 6) * 2.0 ** -24
@@ -179,8 +180,8 @@ def logits(l, start, V, history=None, prompt_len=None, hist_len=None, draft=None
             if allowed is not None:
                 s = t if allowed_row is None else int(allowed_row[t])
                 if 0 <= s < len(allowed):
-                    for v in range(V):
-                        if not int(allowed[s][v // 32]) >> (v % 32) & 1:
-                            x[v], e[v], touched[t, v] = -np.inf, 0.0, True
+                    bits = np.unpackbits(np.asarray(allowed[s], dtype="<u4").view(np.uint8), bitorder="little")[:V]
+                    hidden = bits == 0
+                    x[hidden], e[hidden], touched[t, hidden] = -np.inf, 0.0, True
             y[t], err[t] = x, e
     return y, err, touched
