@@ -1018,7 +1018,7 @@ __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t
 // NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
 // SEE: causal, or trees.  COUNTED: the own keys are cut by the lengths.
 template <int HD, int NP, int NS, int SEE, bool COUNTED>
-__global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER ? 4 : NP == WIDE || NS == WIDE || NS == FOUR ? 2 : 1)) void prefix_attn_kernel(const Args a) {
+__global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER || (SEE == SEE_TREE && HD == 64 && NS == WIDE) ? 4 : NP == WIDE || NS == WIDE || NS == FOUR ? 2 : 1)) void prefix_attn_kernel(const Args a) {
     constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     const int64_t at = a.base + blockIdx.x;
