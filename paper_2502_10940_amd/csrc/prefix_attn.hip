@@ -169,14 +169,15 @@ constexpr int64_t kTreeOwn = 8;            // the same where they are cut by the
 constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
-// Trees of heads of 64 have two more kinds.  64 rows in registers: 24 trees of up to 64
-// nodes over 4000 keys, 32 heads, 96 us against 104 in tiles of 128; 8 of up to 40 over
-// 8000, 16 heads, 40 against 49; one of 60, 300 keys, 10 against 13.5.  256 rows, which
-// fetch the keys once: 32 of up to 40 nodes over 4000 keys, 16 heads over 2, 33 against
-// 36.  At heads of 128 neither fits the registers (256 rows: 369 us against 175).
-int kind_of(int64_t rows, bool trees) {
+// Trees of heads of 64 have one more kind, 64 rows in registers, where tiles are few: its
+// waves share the keys, so that a tile takes a fourth of the turns (one request of 60
+// nodes and 300 keys, 8 heads: 10.2 us against 12.9 in a tile of 128; two of 3000 keys 14.7
+// against 18.6; 8 of up to 40 nodes over 8000 keys, 16 heads, 41.0 against 39.8; 24 of up to
+// 48 over 1500, 32 heads, 37.5 against 34.2).
+constexpr int64_t kFourTiles = 64;
+int kind_of(int64_t rows, bool four) {
     if (rows <= 32) return rows <= 16 ? ONE : TWO;
-    return trees && rows <= 64 ? FOUR : trees && rows > 128 ? WIDER : WIDE;
+    return four && rows <= 64 ? FOUR : WIDE;
 }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -185,14 +186,14 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     const int64_t g = sh.hq / sh.hk;
     const int64_t new_rows = sh.max_new < sh.T ? sh.max_new : sh.T;
     p.rows = sh.T * sh.hq;
-    p.kind_s = kind_of(new_rows * g, tree && sh.hd == 64);
-    p.kind_p = kind_of(sh.T * g, p.kind_s == WIDER || (p.kind_s == FOUR && sh.T * g <= 64));   // never below kind_s
+    p.kind_s = kind_of(new_rows * g, tree && sh.hd == 64 && sh.n_req * sh.hk <= kFourTiles);
+    p.kind_p = kind_of(sh.T * g, p.kind_s == FOUR);   // never below kind_s
     p.tiles_p = (int)ceil_div(sh.T * g, kind_rows(p.kind_p));
     p.tiles_s = (int)ceil_div(new_rows * g, kind_rows(p.kind_s));
     if (p.kind_s == ONE && sh.max_new == 1 && !tree)
         p.kind_s = sh.n_req * sh.hk >= kSoloItems && (sh.prefix == 0 || p.kind_p == WIDE) ? SOLO : FLAT;
     // without a prefix, the kernel whose prefix part asks for least
-    if (sh.prefix == 0) p.kind_p = p.kind_s == TWO || p.kind_s == FOUR || is_wide(p.kind_s) ? p.kind_s : ONE;
+    if (sh.prefix == 0) p.kind_p = p.kind_s == TWO || p.kind_s == FOUR || p.kind_s == WIDE ? p.kind_s : ONE;
     // Short prefixes and few requests: the prefix's bytes come from L2 for each of them,
     // which costs less than a launch that joins.
     auto along = [&](bool wide) {
@@ -202,7 +203,7 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     // FOUR beside wide tiles of a prefix leaves its kernel half the waves (24 trees of up to
     // 48 nodes behind 2048 tokens, 32 heads: 62.7 us against 59.9)
     if (p.kind_s == FOUR && p.kind_p == WIDE && !along(false)) p.kind_s = WIDE;
-    const bool wide = is_wide(p.kind_s);
+    const bool wide = p.kind_s == WIDE;
     if (along(wide)) {
         p.kind_p = ALONG;
         p.tiles_p = 1;
@@ -219,7 +220,7 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     // and 141.
     const int64_t base_p = (int64_t)p.tiles_p * sh.hk, base_s = sh.n_req * p.tiles_s * sh.hk;
     const int64_t blocks_p = base_p * ceil_div(sh.prefix, KB), blocks_s = base_s * ceil_div(sh.max_kv, KB);
-    const int64_t items = full_chip(sh.hd, p.kind_s);
+    const int64_t items = full_chip(sh.hd);
     int64_t chunk = ceil_div(blocks_p + blocks_s, items);
     if (chunk < 8) chunk = 8;
     // The prefix's length is known, max_kv only bounds the requests': their keys count

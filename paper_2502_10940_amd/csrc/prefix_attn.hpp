@@ -566,19 +566,19 @@ __device__ __forceinline__ void item(const Args& a, float* lds, const int32_t* t
 // product O^T += V^T P^T wants from that lane when V's rows come in the same
 // order, which the transposing LDS reads give.
 
+constexpr int WROWS = 32 * NW;            // rows of a wide tile
 constexpr int STG = 64;                   // keys of a stage (32: 5 to 10 % slower)
 
 // A stage's keys or values in LDS: [STG][HD] bf16, 16-byte chunk c of row r at chunk
 // c ^ swz(r).  The swizzle gives 16 rows of one chunk, and four neighbouring rows of
 // 64 bytes, all 64 banks once: the reads of the two products.
-// W: waves that load it.
-template <int HD, int W = NW>
+template <int HD>
 struct KeyTile {
     static constexpr int NB = STG / 32, TILES = STG / 16;
     static constexpr int ROW = 2 * HD, BYTES = STG * ROW;
     static constexpr int CPR = HD / 8;                 // chunks per row
     static constexpr int RPI = 64 / CPR;               // rows of a 1 KB load
-    static constexpr int RW = STG / W;                 // rows that a wave loads, in NL loads
+    static constexpr int RW = STG / NW;                // rows that a wave loads, in NL loads
     static constexpr int NL = RW / RPI;
     __device__ static __forceinline__ int swz(int row) {
         const int x = HD == 128 ? row & 15 : (row >> 1) & 7;
@@ -686,11 +686,11 @@ __device__ __forceinline__ void wide_block(WideWave<HD>& w, const char* kt, int 
 template <int HD>
 constexpr int kWideBytes = 4 * KeyTile<HD>::BYTES + 16;
 
-// item() for a tile of 32 rows to each of W waves: the same rows, keys and results.
-template <int HD, int SEE, bool ALONG, int W>
+// item() for a tile of 128 rows: the same rows, keys and results.
+template <int HD, int SEE, bool ALONG>
 __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
                                           int n_rows, int first, int end, int k0, int chunk, int slot) {
-    typedef KeyTile<HD, W> Tile;
+    typedef KeyTile<HD> Tile;
     constexpr int B = Tile::BYTES;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     auto seen = [&](int rho) { return SEE == SEE_CAUSAL ? (int)min((int64_t)first + 1 + rho / a.g, (int64_t)end) : end; };
@@ -844,22 +844,26 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
         w.lim = lim;
     }
     {
-        const int any = uniform(a.n_pages > 0 ? min(seen(min(tile0 + 32 * W, n_rows) - 1), k0 + chunk) : 0);
+        const int any = uniform(a.n_pages > 0 ? min(seen(min(tile0 + WROWS, n_rows) - 1), k0 + chunk) : 0);
         const int all = uniform(min(SEE == SEE_TREE ? first : seen(tile0), any));
         const int w_any = uniform(w0 < n_rows ? min(seen(min(w0 + 32, n_rows) - 1), any) : 0);
         const int w_all = uniform(w0 < n_rows ? min(SEE == SEE_TREE ? first : seen(w0), any) : 0);
         walk(std::integral_constant<int, SEE>{}, table, k0, any, all, w_any, w_all);
     }
     // Lane (hh, row) has the elements 32 u + 8 j + 4 hh .. + 3 in o[u][4 j ..].  They go
-    // out by way of LDS, a region for each wave, so that a store covers whole rows (eight
-    // waves: halves of rows, one after the other): four elements at chunk c of row r lie
-    // at chunk c ^ (r % 16), or % 8 of 8 chunks.
-    constexpr int P = W / NW, CH = HD / 4 / P, RS = 64 / CH;   // passes; chunks of a row, rows of a store
-    constexpr int SW = CH < 16 ? CH - 1 : 15;
+    // out by way of LDS, a region for each wave, so that a store covers whole rows:
+    // four elements at chunk c of row r lie at chunk c ^ (r % 16).
+    constexpr int CH = HD / 4, RS = 64 / CH;           // chunks of a row, rows of a store
     float l = w.l + __shfl_xor(w.l, 32);
     f32x4* mine = reinterpret_cast<f32x4*>(lds) + 32 * CH * wave;
     const int rr = lane & 31;
     const float scale = a.direct ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+#pragma unroll
+    for (int u = 0; u < HD / 32; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            mine[CH * rr + ((8 * u + 2 * j + hh) ^ (rr & 15))] =
+                f32x4{w.o[u][4 * j], w.o[u][4 * j + 1], w.o[u][4 * j + 2], w.o[u][4 * j + 3]} * scale;
     const int64_t id = row * a.hq + h;
     if (live && hh == 0) {
         if (!a.direct) *reinterpret_cast<float2*>(a.ml + 2 * (slot * a.rows + id)) = make_float2(w.m, l);
@@ -867,38 +871,26 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
     }
     const int c = lane % CH;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-#pragma unroll
-        for (int v = 0; v < HD / 32 / P; ++v)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x16& o = w.o[HD / 32 / P * p + v];
-                mine[CH * rr + ((8 * v + 2 * j + hh) ^ (rr & SW))] = f32x4{o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]} * scale;
-            }
-#pragma unroll
-        for (int i = 0; i < 32; i += RS) {
-            const int r = i + lane / CH;
-            if (w0 + r >= n_rows) continue;
-            const f32x4 x = mine[CH * r + (c ^ (r & SW))];
-            const int t = (w0 + r) / a.g, hd = head * a.g + (w0 + r - t * a.g), e = 4 * (CH * p + c);
-            if (a.direct)
-                *reinterpret_cast<u32x2*>(a.out + (row0 + t) * a.ldo + hd * HD + e) =
-                    u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-            else
-                *reinterpret_cast<f32x4*>(a.part + (slot * a.rows + (int64_t)(row0 + t) * a.hq + hd) * HD + e) = x;
-        }
+    for (int i = 0; i < 32; i += RS) {
+        const int r = i + lane / CH;
+        if (w0 + r >= n_rows) continue;
+        const f32x4 x = mine[CH * r + (c ^ (r & 15))];
+        const int t = (w0 + r) / a.g, hd = head * a.g + (w0 + r - t * a.g);
+        if (a.direct)
+            *reinterpret_cast<u32x2*>(a.out + (row0 + t) * a.ldo + hd * HD + 4 * c) =
+                u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        else
+            *reinterpret_cast<f32x4*>(a.part + (slot * a.rows + (int64_t)(row0 + t) * a.hq + hd) * HD + 4 * c) = x;
     }
 }
 
 // Kinds of tiles: 16 or 32 rows whose keys a workgroup's waves share (ONE, TWO); 128
-// rows against keys in LDS (WIDE).  Trees have two more: 64 rows as ONE and TWO (FOUR),
-// 256 rows as WIDE (WIDER).  On the requests' own keys, where each has one
+// rows against keys in LDS (WIDE); for trees 64 rows as ONE and TWO, too (FOUR).  On the requests' own keys, where each has one
 // token, all rows of a tile see the same: ONE becomes FLAT, or SOLO with a tile to
 // a wave.
 // Behind a short prefix there are no tiles for it: each request's own items take its
 // keys ALONG, and nothing is left to join.
-enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, ALONG = 5, FOUR = 6, WIDE = 8, WIDER = 16 };
-constexpr bool is_wide(int k) { return k == WIDE || k == WIDER; }
+enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, ALONG = 5, FOUR = 6, WIDE = 8 };
 constexpr int kind_rows(int k) { return k == SOLO || k == FLAT ? 16 : k == FOUR ? 64 : 16 * k; }
 // Parts of `chunk` keys that a request of `end` own tokens has.
 __device__ __forceinline__ int parts_of(const Args& a, int end, int chunk) {
@@ -931,7 +923,7 @@ constexpr int kCounted = 256;
 struct Counted {
     int r, head, split, tile, chunk;       // r < 0: past the last item
 };
-__device__ __forceinline__ Counted counted_item(const Args& a, int64_t turn, int rows) {
+__device__ __forceinline__ Counted counted_item(const Args& a, int64_t turn) {
     constexpr int PER = kCounted / 64;
     const int lane = threadIdx.x & 63;
     int tiles[PER], end[PER], all = 0;
@@ -940,7 +932,7 @@ __device__ __forceinline__ Counted counted_item(const Args& a, int64_t turn, int
     for (int q = 0; q < PER; ++q) {
         const int r = PER * lane + q;
         const Span s = span_of(a, min(r, a.n_req - 1));
-        tiles[q] = r < a.n_req ? (s.n * a.g + rows - 1) / rows : 0;
+        tiles[q] = r < a.n_req ? (s.n * a.g + WROWS - 1) / WROWS : 0;
         end[q] = s.end;
         all += tiles[q];
         work += (int64_t)tiles[q] * ((s.end + STG - 1) / STG);
@@ -991,21 +983,21 @@ __device__ __forceinline__ Counted counted_item(const Args& a, int64_t turn, int
 }
 
 template <int HD, int N>
-constexpr int kLdsBytes = is_wide(N) ? kWideBytes<HD> : (N == SOLO || N == ALONG ? 16 : 8 * kStateFloats<HD, kind_rows(N) / 16>);
+constexpr int kLdsBytes = N == WIDE ? kWideBytes<HD> : (N == SOLO || N == ALONG ? 16 : 8 * kStateFloats<HD, kind_rows(N) / 16>);
 
 // AHEAD costs registers: heads of 128 with 32 rows have none to spare, and beside
 // wide tiles, which leave two workgroups a CU, the plain loop is faster (64 requests
 // behind 32768 tokens 101 us against 114, 200 of 32 heads 123 against 140; one request
 // behind 100 tokens 4.9 against 4.7, behind 1024 8.7 against 7.8).
 template <int HD, int N, int NP>
-constexpr bool kAhead = !is_wide(NP) && !(HD == 128 && N == TWO) && N != FOUR;
+constexpr bool kAhead = NP != WIDE && !(HD == 128 && N == TWO) && N != FOUR;
 
 template <int HD, int N, int NP, int SEE>
 __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t* table, int head, int row0, int tile0,
                                          int n_rows, int first, int end, int k0, int chunk, int slot) {
     constexpr bool ALONG_P = NP == ALONG;
-    if constexpr (is_wide(N))
-        wide_item<HD, SEE, ALONG_P, N / 2>(a, lds, table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
+    if constexpr (N == WIDE)
+        wide_item<HD, SEE, ALONG_P>(a, lds, table, head, row0, tile0, n_rows, first, end, k0, chunk, slot);
     else if constexpr (N == SOLO)
         item<HD, 1, 1, SEE_ALL, false, kAhead<HD, N, NP>>(a, nullptr, table, head, row0, tile0, n_rows, 0, min(first + 1, end), k0, chunk, slot);
     else if constexpr (N == FLAT)
@@ -1018,7 +1010,7 @@ __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t
 // NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
 // SEE: causal, or trees.  COUNTED: the own keys are cut by the lengths.
 template <int HD, int NP, int NS, int SEE, bool COUNTED>
-__global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER || (SEE == SEE_TREE && HD == 64 && NS == WIDE) ? 4 : NP == WIDE || NS == WIDE || NS == FOUR ? 2 : 1)) void prefix_attn_kernel(const Args a) {
+__global__ __launch_bounds__(NTHR, (SEE == SEE_TREE && HD == 64 && NS == WIDE ? 4 : NP == WIDE || NS == WIDE || NS == FOUR ? 2 : 1)) void prefix_attn_kernel(const Args a) {
     constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     const int64_t at = a.base + blockIdx.x;
@@ -1036,7 +1028,7 @@ __global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER || (SEE
     } else {
         int64_t b = at - a.items_p;
         if constexpr (COUNTED) {
-            const Counted c = counted_item(a, b, kind_rows(NS));
+            const Counted c = counted_item(a, b);
             if (b == 0 && threadIdx.x == 0) *a.chunk = c.chunk;
             if (c.r < 0) return;
             const Span s = span_of(a, c.r);
@@ -1066,13 +1058,13 @@ __global__ __launch_bounds__(NS == WIDER ? 2 * NTHR : NTHR, (NS == WIDER || (SEE
     }
 }
 
-// Workgroups of the wide kernels that the chip holds at once (two a CU at heads of 128
-// and of eight waves, four else).
-constexpr int64_t full_chip(int hd, int kind) { return hd == 128 || kind == WIDER ? 512 : 1024; }
+// Workgroups of the wide kernels that the chip holds at once (two a CU at heads of 128,
+// four at 64).
+constexpr int64_t full_chip(int hd) { return hd == 128 ? 512 : 1024; }
 // Whether a launch for trees cuts the own keys by the lengths: wide tiles, fewer than
 // fill half of the chip, and as many requests as a workgroup counts in a few loads.
 inline bool counts_lengths(const PrefixAttnShape& sh, int kind, int tiles) {
-    return is_wide(kind) && sh.n_req <= kCounted && sh.n_req * tiles * sh.hk < full_chip(sh.hd, kind) / 2;
+    return kind == WIDE && sh.n_req <= kCounted && sh.n_req * tiles * sh.hk < full_chip(sh.hd) / 2;
 }
 
 inline Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const PrefixAttnPtrs& t) {
@@ -1096,7 +1088,7 @@ inline Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const Pr
     a.direct = p.direct;
     a.mask = t.mask;
     a.words = (int)((sh.max_new + 63) / 64);
-    a.slots = t.mask && p.splits_s > 1 && counts_lengths(sh, p.kind_s, p.tiles_s) ? (int)full_chip(sh.hd, p.kind_s) : 0;
+    a.slots = t.mask && p.splits_s > 1 && counts_lengths(sh, p.kind_s, p.tiles_s) ? (int)full_chip(sh.hd) : 0;
     // parts as counted_item cuts them are at most the slots and one for each tile, and a
     // request's units are filled up to whole rounds of eight
     const int64_t base_s = sh.n_req * p.tiles_s * sh.hk;

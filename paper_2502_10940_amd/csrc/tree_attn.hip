@@ -9,7 +9,7 @@ template <int HD>
 hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t s) {
 #define COLA_GO(P, S, C)                                      \
     if (p.kind_p == P && p.kind_s == S && (a.slots > 0) == C) \
-    prefix_attn_kernel<HD, P, S, SEE_TREE, C><<<grid, S == WIDER ? 2 * NTHR : NTHR, 0, s>>>(a)
+    prefix_attn_kernel<HD, P, S, SEE_TREE, C><<<grid, NTHR, 0, s>>>(a)
     COLA_GO(ALONG, ONE, false);
     else COLA_GO(ALONG, TWO, false);
     else COLA_GO(ALONG, WIDE, false);
@@ -23,9 +23,6 @@ hipError_t go(const PrefixAttnPlan& p, const Args& a, unsigned grid, hipStream_t
     else if constexpr (HD == 64) {
         COLA_GO(ALONG, FOUR, false);
         else COLA_GO(FOUR, FOUR, false);
-        else COLA_GO(ALONG, WIDER, false);
-        else COLA_GO(WIDER, WIDER, false);
-        else COLA_GO(WIDER, WIDER, true);
         else return hipErrorInvalidValue;
     } else return hipErrorInvalidValue;
 #undef COLA_GO

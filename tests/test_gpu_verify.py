@@ -405,10 +405,10 @@ CUT = {"near": ([40, 100, 7], [5000, 300, 7000], 0, 2, 1, None), "far": ([40, 10
        "empty": ([129, 0, 35], [3000, 40, 35], 0, 1, 1, 9000), "prefix": ([70, 33], [2500, 6000], 1300, 2, 2, None), "one": ([200], [9000], 0, 4, 2, None),
        "mixed": ([34, 256, 1, 90], [34, 4000, 5000, 90], 0, 1, 1, None), "256": ([5] * 255 + [36], [5 + 3 * i for i in range(255)] + [1500], 0, 1, 1, 4000),
        "257": ([5] * 256 + [36], [5 + i for i in range(256)] + [1500], 0, 1, 1, 4000), "wide": ([100, 80], [5000, 3000], 0, 1, 1, None),
-       "wide-prefix": ([100, 80], [900, 300], 1300, 1, 1, None), "wider-prefix": ([200, 180], [500, 700], 1300, 1, 1, None),
-       "along-four": ([40, 60, 9], [70, 60, 30], 90, 1, 1, None), "along-wider": ([200, 150], [220, 150], 90, 1, 1, None), "four-prefix": ([40, 9], [900, 300], 1300, 1, 1, None),
-       "wider-many": ([130] * 40, [130 + 20 * i for i in range(40)], 0, 8, 8, None),
-       "wide-direct": ([70, 80], [200, 90], 0, 1, 1, None), "wider-direct": ([150, 80], [200, 90], 0, 1, 1, None)}
+       "wide-prefix": ([100, 80], [900, 300], 1300, 1, 1, None), "tiles-prefix": ([200, 180], [500, 700], 1300, 1, 1, None),
+       "along-four": ([40, 60, 9], [70, 60, 30], 90, 1, 1, None), "along-tiles": ([200, 150], [220, 150], 90, 1, 1, None), "four-prefix": ([40, 9], [900, 300], 1300, 1, 1, None),
+       "tiles-many": ([130] * 40, [130 + 20 * i for i in range(40)], 0, 8, 8, None),
+       "wide-direct": ([70, 80], [200, 90], 0, 1, 1, None), "tiles-direct": ([150, 80], [200, 90], 0, 1, 1, None)}
 
 
 @pytest.mark.parametrize("hd", (64, 128))

@@ -185,15 +185,14 @@ def test_gpu_tests_of_trees_run_every_kernel(hd):
     cases += [(len(new), sum(new) + 3, hq, hk, L, max_kv or max(kv), max(new)) for new, kv, L, hq, hk, max_kv in CUT.values()]
     for n, T, hq, hk, L, max_kv, max_new in cases:
         p = tree_plan(n, T, hq, hk, hd, L, max_kv, max_new, 16 if hd == 64 else 64)
-        wide = p.kind_s in (8, 16)
-        full = 512 if hd == 128 or p.kind_s == 16 else 1024
-        counted = wide and p.splits_s > 1 and n <= 256 and n * p.tiles_s * hk < full // 2
+        full = 512 if hd == 128 else 1024
+        counted = p.kind_s == 8 and p.splits_s > 1 and n <= 256 and n * p.tiles_s * hk < full // 2
         seen.add((p.kind_p, p.kind_s, counted))
-    k = dict(KINDS, four=6, wider=16)
+    k = dict(KINDS, four=6)
     every = [("along", "one"), ("along", "two"), ("along", "wide"), ("one", "one"), ("two", "one"), ("two", "two"), ("wide", "one"), ("wide", "two"),
              ("wide", "wide"), ("wide", "wide", True)]
     if hd == 64:
-        every += [("along", "four"), ("four", "four"), ("along", "wider"), ("wider", "wider"), ("wider", "wider", True)]
+        every += [("along", "four"), ("four", "four")]
     every = {(k[x[0]], k[x[1]], len(x) > 2) for x in every}
     assert seen == every, (sorted(every - seen), sorted(seen - every))
 
