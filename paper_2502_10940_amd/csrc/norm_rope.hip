@@ -454,15 +454,21 @@ dim3 shape(bool bf16, NormKind kind, NormRopeArgs& a) {
     const int64_t pq = kind == NORM_BWD ? a.ldq : a.ldqo, pk = kind == NORM_BWD ? a.ldk : a.ldko;
     a.past = ((pq * es | pk * es | (int64_t)(uintptr_t)a.qo | (int64_t)(uintptr_t)a.ko) & 63) == 0 &&
              (double)a.T * (a.hq + a.hk) * a.hd * es > 48e6;
-    int64_t lanes = (int64_t(1) << 18) / (a.T * a.group) + 1;
-    if (lanes < (H + CH - 1) / CH) lanes = (H + CH - 1) / CH;
+    // Groups of a row: as many as leave each two rounds of loads, for every group forms the
+    // row's cosines again (16000 rows of 20 + 5 heads of 80: 34 us against 40 with one round,
+    // backward 68 against 74), up to a head each where rows are few (2^18 threads fill the
+    // chip), in powers of two (1536 rows into the cache: 12.5 us with 16, 14.8 with 22).
+    int64_t lanes = 1;
+    while (2 * lanes <= (int64_t(1) << 18) / (a.T * a.group) + 1) lanes *= 2;
+    if (lanes < (H + 2 * CH - 1) / (2 * CH)) lanes = (H + 2 * CH - 1) / (2 * CH);
     if (lanes > H) lanes = H;
     // Rows of many heads take whole workgroups each (some groups then have no head), or the
     // rows that fill them would ask for a grid past its second axis.
     if (lanes * a.group > 8 * NTHR) lanes = (lanes + NTHR / a.group - 1) / (NTHR / a.group) * (NTHR / a.group);
     a.lanes = (int)lanes;
-    // as many rows as fill whole workgroups: the groups of a row may lie in two (1536 rows of
-    // 32 + 8 + 8 heads: 176 threads a row, 16 rows in 11 workgroups)
+    // as many rows as fill whole workgroups: the groups of a row may lie in two (20 heads of
+    // 80: 5 groups of 8 lanes a row, 32 rows in 5 workgroups; with the rest of each workgroup
+    // idle instead, 8191 rows of 32 + 8 heads of 128 took 109 us against 70)
     const int64_t per = lanes * a.group;
     const int64_t low = per & -per;                     // its power of two
     a.tpw = low < NTHR ? (int)(NTHR / low) : 1;
