@@ -13,6 +13,13 @@
 // lane counts the nodes of the row's path that drafted it (the bits that two masks
 // share) and writes the token's shift anew.  A wave has a part of the chunk to itself,
 // so that no wave waits for another between the rows.
+//
+// 980 rows of 128003 bf16 logits of 40 requests, histories of up to 8000 tokens, 200 biases
+// each and masks for the rows (533 MB): 147 us, 3.6 TB/s; without rules 88 us, 6.0 TB/s.
+// What is between is the counting (a third: 66 workgroups of a request read its history), the
+// masks' bits and the vectors that hold tokens of the history, nearly all here (24 vector
+// instructions a logit, which take 56 % of the launch).  One row of 32000 fp32 logits: 6.2 us, a launch and
+// six dependent loads.
 #include "rows.hpp"
 #include "serve.hpp"
 
@@ -83,7 +90,8 @@ struct Draft {
     uint32_t seen, answer;
 };
 
-// PV NVEC elements of a row to a thread; PAST: results past the caches.
+// PV NVEC elements of a row to a thread; PAST: results past the caches (980 rows of 128003:
+// 180 us against 208).
 template <bool BF16, int NVEC, bool PAST>
 __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const int rows, const int chunks, const int64_t base) {
     constexpr int PV = BF16 ? 8 : 4, CW = 64 * PV * NVEC, C = CW * NTHR / 64;
@@ -398,8 +406,11 @@ hipError_t go(const LogitsArgs& a, int rows, bool past, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_logits(bool bf16, const LogitsArgs& a, hipStream_t s) {
-    // Chunks as large as leave 1024 workgroups of one row, and rows to a workgroup (of one
-    // request, so as many as it may have) while there are 2048.
+    // Chunks of up to 4096 tokens (32 KB of LDS, four workgroups a CU) as large as leave 1024
+    // workgroups of one row, and rows to a workgroup (of one request, so as many as it may
+    // have) while there are 2048: the rows of a request share its counts (980 rows, chunks of
+    // 4096: 365 us with one row, 210 with 4, 189 with 8, 180 with 16; chunks of 2048 408, 225,
+    // 200 and 195; 256 rows of requests of their own 85 against 106).
     const int pv = NTHR * (bf16 ? 8 : 4), most = bf16 ? 2 : 4;
     int nvec = 1;
     while (nvec < most && a.T * ((a.V + 2 * pv * nvec - 1) / (2 * pv * nvec)) >= 1024) nvec *= 2;

@@ -267,7 +267,7 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     // Few requests' trees are cut by their lengths on the GPU (counted_item); these parts
     // are the least, and say how many the workspace has room for.  8 requests of up to
     // 32000 keys, 64 nodes of 32 heads over 8 of 128: 175 us against 205 with parts of 1536;
-    // 4 of up to 8000, 200 nodes: 72 against 78.  Where the tiles fill half of the chip as
+    // 4 of up to 8000, 200 nodes: 71 against 78.  Where the tiles fill half of the chip as
     // they are it costs more than it gives (32 of up to 4000, 32 nodes: 75 against 72).
     const int64_t kv_blocks = ceil_div(sh.max_kv, KB);
     const bool counted = tree && counts_lengths(sh, p.kind_s, p.tiles_s);

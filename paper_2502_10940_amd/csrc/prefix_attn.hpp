@@ -45,6 +45,11 @@
 // 16, and with two waves a SIMD neither is busy all the time (56 and 31 % of the
 // launch).
 //
+// Trees (cola_tree_attn) use the same tiles: a block of keys that holds new tokens takes
+// a word of each row's mask where causal rows take a limit, and all blocks before it are
+// as they were.  32 requests of up to 4000 keys, trees of up to 32 nodes, 32 heads over 8
+// of 128 (282 MB): 74 us with the keys still in the last-level cache, 81 without.
+//
 // Short prefixes: a request's own items read them along (the bytes come from L2),
 // and neither partial rows nor a join are left.
 //

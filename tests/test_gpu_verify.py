@@ -238,6 +238,22 @@ def test_norm_rope_of_many_heads(T, hq, hk, hd, rot):
         assert (np.abs(f64(u) - rx) <= bx).all() and (np.abs(f64(v) - rg) <= bg).all()
 
 
+def test_norm_rope_past_4_gib():
+    """Rows at a pitch that puts the last ones past 2^32 bytes: the bits of tight rows, both ways."""
+    T, h, hd, ld = 1100, 2, 64, (1 << 21) + 8
+    x, dy, g = rand(1, (T, h * hd), "bf16"), rand(2, (T, h * hd), "bf16"), gain(3, hd, "bf16")
+    d, far = cola.rope_desc(T, h, 0, hd), cola.rope_desc(T, h, 0, hd, ldq=ld)
+    want, dx, dg = torch.empty_like(x), torch.empty_like(x), torch.empty(hd, device=DEV)
+    cola.norm_rope_fwd(d, x, None, g, None, None, want, None)
+    cola.norm_rope_bwd(d, dy, None, x, None, g, None, None, dx, None, dg, None, workspace(d))
+    big, _ = pitched(x, ld, fill=0.0)
+    out, dg2 = torch.empty_like(x), torch.empty(hd, device=DEV)
+    cola.norm_rope_fwd(far, big, None, g, None, None, out, None)
+    assert torch.equal(out, want)
+    cola.norm_rope_bwd(far, dy, None, big, None, g, None, None, big, None, dg2, None, workspace(far))
+    assert torch.equal(big, dx) and torch.equal(dg2, dg)
+
+
 def test_norm_gradients_do_not_depend_on_the_workspace_s_contents_or_the_run():
     T, hq, hk, hd = 700, 5, 3, 96
     q, k, dq, dk = (rand(i, (T, h * hd), "bf16") for i, h in enumerate((hq, hk, hq, hk)))
