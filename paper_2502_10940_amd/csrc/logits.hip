@@ -15,11 +15,11 @@
 // so that no wave waits for another between the rows.
 //
 // 980 rows of 128003 bf16 logits of 40 requests, histories of up to 8000 tokens, 200 biases
-// each and masks for the rows (533 MB): 147 us, 3.6 TB/s; without rules 88 us, 6.0 TB/s.
+// each and masks for the rows (533 MB): 142 us, 3.8 TB/s; without rules 88 us, 6.0 TB/s.
 // What is between is the counting (a third: 66 workgroups of a request read its history), the
-// masks' bits and the vectors that hold tokens of the history, nearly all here (24 vector
-// instructions a logit, which take 56 % of the launch).  One row of 32000 fp32 logits: 6.2 us, a launch and
-// six dependent loads.
+// masks' bits and the vectors that hold tokens of the history, nearly all here (21 vector
+// instructions a logit, which take 52 % of the launch).  One row of 32000 fp32 logits: 5.4
+// us, a launch and five loads one after the other.
 #include "rows.hpp"
 #include "serve.hpp"
 
@@ -91,7 +91,7 @@ struct Draft {
 };
 
 // PV NVEC elements of a row to a thread; PAST: results past the caches (980 rows of 128003:
-// 180 us against 208).
+// 121 us against 128).
 template <bool BF16, int NVEC, bool PAST>
 __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const int rows, const int chunks, const int64_t base) {
     constexpr int PV = BF16 ? 8 : 4, CW = 64 * PV * NVEC, C = CW * NTHR / 64;
@@ -156,13 +156,13 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
         w.edge.r = global<typename Vec<BF16, 1>::Loose>(wide > 0 ? (const void*)(from + v) : kNowhere);
         w.edge_ok = global<uint8_t>(bits ? (const void*)(bits + (v >> 3)) : kNowhere);
     };
-    bool built = false;                                 // shifts of a request are in LDS
+    bool built = false, own_drafts = false;             // shifts of a request are in LDS; drafted tokens in this wave's part
     float rep = 1.0f, inv = 1.0f, pres = 0.0f, freq = 0.0f;
     // One row from its registers, the next one on its way.
     auto step = [&](Row& now, Row& next, int i) __attribute__((always_inline)) {
         const int64_t t = t0 + i;
         load(next, min(i + 1, n_rows - 1));
-        if (drafted && n_drafts > 0) {
+        if (own_drafts) {
             const uint64_t* mask = a.mask + t * a.words;
             for (int j = lane; j < n_drafts; j += 64) {
                 const Draft d = drafts[j];
@@ -240,21 +240,27 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
         if (r >= a.n_req) break;
 
         if (changes) {
-            const bool counted = repeats && a.hist_len;
-            const int32_t* h = a.history + (int64_t)r * a.max_hist;
+            // The arguments that only this part needs, read here: held through the rows they
+            // take scalar registers, which are spilled to and fetched from vector ones (256 rows
+            // of requests of their own 86 us against 78, one row 6.2 against 5.4).
+            const __attribute__((address_space(4))) LogitsArgs* here = (const __attribute__((address_space(4))) LogitsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+            asm volatile("" : "+s"(here));
+            const __attribute__((address_space(4))) LogitsArgs& z = *here;
+            const bool counted = repeats && z.hist_len;
+            const int32_t* h = z.history + (int64_t)r * z.max_hist;
             // The request's numbers, all on their way at once: those that are not there come
             // from a place that is.
             const int32_t* zero = reinterpret_cast<const int32_t*>(kNowhere);
             const float* one = &kOne;
-            const int hist_len = entry(counted ? a.hist_len + r : zero, 0), prompt_len = entry(a.prompt_len ? a.prompt_len + r : zero, 0);
-            const int bias_lo = entry(biases ? a.bias_start + r : zero, 0), bias_hi = entry(biases ? a.bias_start + r + 1 : zero, 0);
-            const int first = entry(a.start ? a.start + r : zero, 0), past_last = entry(a.start ? a.start + r + 1 : zero, 0);
-            rep = entry(a.repetition ? a.repetition + r : one, 0);
-            pres = entry(a.presence ? a.presence + r : reinterpret_cast<const float*>(zero), 0);
-            freq = entry(a.frequency ? a.frequency + r : reinterpret_cast<const float*>(zero), 0);
-            const int end = min(max(hist_len, 0), (int)a.max_hist), past = min(max(prompt_len, 0), end);
-            const int lo = min(max(bias_lo, 0), (int)a.n_bias), hi = min(max(bias_hi, lo), (int)a.n_bias);
-            const int64_t n0 = a.start ? max(first, 0) : t, n1 = a.start ? min((int64_t)past_last, a.T) : t + 1;
+            const int hist_len = entry(counted ? z.hist_len + r : zero, 0), prompt_len = entry(z.prompt_len ? z.prompt_len + r : zero, 0);
+            const int bias_lo = entry(biases ? z.bias_start + r : zero, 0), bias_hi = entry(biases ? z.bias_start + r + 1 : zero, 0);
+            const int first = entry(z.start ? z.start + r : zero, 0), past_last = entry(z.start ? z.start + r + 1 : zero, 0);
+            rep = entry(z.repetition ? z.repetition + r : one, 0);
+            pres = entry(z.presence ? z.presence + r : reinterpret_cast<const float*>(zero), 0);
+            freq = entry(z.frequency ? z.frequency + r : reinterpret_cast<const float*>(zero), 0);
+            const int end = min(max(hist_len, 0), (int)z.max_hist), past = min(max(prompt_len, 0), end);
+            const int lo = min(max(bias_lo, 0), (int)z.n_bias), hi = min(max(bias_hi, lo), (int)z.n_bias);
+            const int64_t n0 = z.start ? max(first, 0) : t, n1 = z.start ? min((int64_t)past_last, z.T) : t + 1;
             // A thread's first entries of the lists, on their way while LDS is cleared.  The
             // history goes four tokens a load; the last load ends with it.
             auto read = [&](i32x4 (&y)[AHEAD], int j0) __attribute__((always_inline)) {
@@ -266,10 +272,10 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
             int token = -1, node = -1;
             float b = 0.0f;
             if (lo + tid < hi) {
-                token = a.bias_token[lo + tid];
-                b = a.bias[lo + tid];
+                token = z.bias_token[lo + tid];
+                b = z.bias[lo + tid];
             }
-            if (drafted && tid < 64 * a.words && n0 + tid < n1) node = a.draft[n0 + tid];
+            if (drafted && tid < 64 * a.words && n0 + tid < n1) node = z.draft[n0 + tid];
             // a token's place in the chunk, `width` or more: it has none
             auto place_of = [&](int token) __attribute__((always_inline)) { return (uint32_t)token - (uint32_t)c0; };
             if (built) __syncthreads();                 // the request before has read its shifts
@@ -307,7 +313,7 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
             for (int j = lo + tid; j < hi; j += NTHR) {
                 const uint32_t at = place_of(token);
                 if (at < (uint32_t)width) atomicMax(&last[at], (uint32_t)j + 1);
-                if (j + NTHR < hi) token = a.bias_token[j + NTHR];
+                if (j + NTHR < hi) token = z.bias_token[j + NTHR];
             }
             value[tid] = b;
             int mine = -1, place = 0;
@@ -349,14 +355,14 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
                     u32x4 n = *reinterpret_cast<const u32x4*>(count + j + e), m = {0, 0, 0, 0};
                     if (biases) m = *reinterpret_cast<const u32x4*>(last + j + e);
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) {
-                        const uint32_t c = n[z] & ~kPrompt;
-                        f |= (uint32_t)(n[z] != 0) << (e + z);
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const uint32_t c = n[i4] & ~kPrompt;
+                        f |= (uint32_t)(n[i4] != 0) << (e + i4);
                         float y = -0.0f;
-                        if (m[z]) y = (int)m[z] - 1 - lo < NTHR ? value[m[z] - 1 - lo] : a.bias[m[z] - 1];
+                        if (m[i4]) y = (int)m[i4] - 1 - lo < NTHR ? value[m[i4] - 1 - lo] : z.bias[m[i4] - 1];
                         if (c != 0) y -= fmaf(freq, (float)c, pres);
-                        n[z] = __float_as_uint(y);
-                        g |= (uint32_t)(n[z] != 0x80000000u) << (e + z);
+                        n[i4] = __float_as_uint(y);
+                        g |= (uint32_t)(n[i4] != 0x80000000u) << (e + i4);
                     }
                     *reinterpret_cast<u32x4*>(count + j + e) = n;
                 }
@@ -370,6 +376,11 @@ __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const 
                     atomicOr(&changed[place >> 5], 1u << (place & 31));
                 }
                 __syncthreads();
+            }
+            own_drafts = false;
+            if (drafted) {
+                for (int j = lane; j < n_drafts; j += 64) own_drafts |= drafts[j].place >= 0 && drafts[j].place / CW == wave;
+                own_drafts = __ballot(own_drafts) != 0;
             }
             built = true;
         }
@@ -409,8 +420,8 @@ hipError_t launch_logits(bool bf16, const LogitsArgs& a, hipStream_t s) {
     // Chunks of up to 4096 tokens (32 KB of LDS, four workgroups a CU) as large as leave 1024
     // workgroups of one row, and rows to a workgroup (of one request, so as many as it may
     // have) while there are 2048: the rows of a request share its counts (980 rows, chunks of
-    // 4096: 365 us with one row, 210 with 4, 189 with 8, 180 with 16; chunks of 2048 408, 225,
-    // 200 and 195; 256 rows of requests of their own 85 against 106).
+    // 4096: 333 us with one row, 155 with 4, 129 with 8, 121 with 16; chunks of 2048 349, 158,
+    // 130 and 124; 256 rows of requests of their own 78 against 93).
     const int pv = NTHR * (bf16 ? 8 : 4), most = bf16 ? 2 : 4;
     int nvec = 1;
     while (nvec < most && a.T * ((a.V + 2 * pv * nvec - 1) / (2 * pv * nvec)) >= 1024) nvec *= 2;
