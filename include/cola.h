@@ -546,7 +546,7 @@ int cola_prefix_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* c
  * element-aligned; NULL: ones).  desc is cola_rope_fwd's: rot_dim, layouts, scalings,
  * pitches, positions, alignment and overlap as there.  The sum of squares, the norm
  * and the products are fp32 whatever the dtype, and each result is rounded once.  eps
- * is positive and finite.  mscale multiplies the rotated elements only.
+ * is a positive normal fp32 number (1.18e-38 and more, finite).  mscale multiplies the rotated elements only.
  * ------------------------------------------------------------------------ */
 int cola_norm_rope_fwd(const cola_rope_desc* desc, double eps, const void* q, const void* k, const void* g_q,
                        const void* g_k, const int32_t* positions, void* q_out, void* k_out, cola_stream_t stream);

@@ -4,6 +4,7 @@
 // cola_tree_attn and cola_logits_adjust.  Argument checks, frequencies and launches; the
 // kernels are in rope.hip, page_map.hip, prefix_attn.hip, norm_rope.hip, tree_map.hip,
 // tree_attn.hip and logits.hip.
+#include <float.h>
 #include <math.h>
 
 #include "block.hpp"
@@ -177,7 +178,8 @@ int check_norm(const cola_rope_desc* d, bool cache, double eps, const void* g_q,
     const int st = check_rope(d, cache, a);
     if (st != COLA_OK) return st;
     const float e = (float)eps;
-    if (!(e > 0.0f) || !isfinite(e)) return COLA_ERR_INVALID_ARG;
+    // below the normal numbers the hardware's 1 / sqrt may take it for zero: NaN for a head of zeros
+    if (!(e >= FLT_MIN) || !isfinite(e)) return COLA_ERR_INVALID_ARG;
     if (!aligned(g_q, d->dtype) || !aligned(g_k, d->dtype)) return COLA_ERR_INVALID_ARG;
     a->gq = g_q; a->gk = g_k;
     a->eps = e;

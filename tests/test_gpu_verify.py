@@ -86,6 +86,25 @@ def test_norm_rope(case, dtype, layout):
 
 
 @pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_norm_rope_of_zeros_at_the_least_eps(dtype):
+    """2^-126, the smallest eps there is: a head of zeros gives zeros, and gradients of
+    dz 2^63 (exact; the hardware's 1 / sqrt is off by an ulp of 2^-23, the result is
+    rounded)."""
+    T, h, hd = 5, 3, 64
+    d = cola.rope_desc(T, h, 0, hd, 0, dtype=dtype)                      # nothing turns
+    q, dy = torch.zeros(T, h * hd, dtype=DT[dtype], device=DEV), rand(1, (T, h * hd), dtype)
+    out, dx = torch.full_like(q, math.nan), torch.full_like(q, math.nan)
+    dg = torch.full((hd,), math.nan, device=DEV)
+    cola.norm_rope_fwd(d, q, None, None, None, None, out, None, eps=2.0 ** -126)
+    cola.norm_rope_bwd(d, dy, None, q, None, None, None, None, dx, None, dg, None, workspace(d), eps=2.0 ** -126)
+    torch.cuda.synchronize()
+    assert (out == 0).all() and (dg == 0).all()
+    want = f64(dy) * 2.0 ** 63
+    tol = 2.0 ** -22 + torch.finfo(DT[dtype]).eps / 2
+    assert (np.abs(f64(dx) - want) <= tol * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
 @pytest.mark.parametrize("layout", ("half", "interleaved"))
 def test_norm_rope_pitches_alignment_and_in_place(dtype, layout):
     """Slices of one buffer at an odd pitch and start: the bits of tight rows, nothing else

@@ -34,7 +34,7 @@ def test_norm_refusals(fn):
         assert cola.norm_rope_workspace_bytes(d) == 0
     refused(cola.ERR_INVALID_ARG, fn, D(4, 2, 2, 64, dtype=7))
     d = D(4, 2, 2, 64)
-    for eps in (0.0, -1.0, math.nan, math.inf, 1e300, 1e-60):
+    for eps in (0.0, -1.0, math.nan, math.inf, 1e300, 1e-60, 1e-45, 1.1e-38):
         refused(cola.ERR_INVALID_ARG, lambda: fn(d, eps=eps))
     for key in ("q", "k"):
         refused(cola.ERR_INVALID_ARG, lambda: fn(d, **{key: None}))
