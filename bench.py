@@ -401,6 +401,12 @@ def assign_streams(works, nstreams):
     return out
 
 
+def step_ms(ms):
+    """A step's time as the line states it: to 1 ns, so that flops over it is the stated
+    TFLOP/s to its last digit (0.01) for steps of tens of us, too."""
+    return round(ms, 6)
+
+
 def timed_steps(step, steps, warmup):
     import torch
     for _ in range(warmup):
@@ -740,7 +746,7 @@ def workload_record(cfg, args):
         for mode in modes:
             ms = timed_steps_median(h.step(mode), args.sub_steps, args.sub_warmup)
             fl = h.flops_dense if mode == "dense" else h.flops_cola
-            rec["modes"][mode] = {"ms_per_step": round(ms, 4), "tflops": round(fl / (ms * 1e9), 2),
+            rec["modes"][mode] = {"ms_per_step": step_ms(ms), "tflops": round(fl / (ms * 1e9), 2),
                                   "pct_of_peak": round(100.0 * fl / (ms * 1e9) / peak, 2),
                                   "tokens_per_s": round(h.T / (ms / 1e3), 1)}
     rec["sclk_mhz"] = sc.median()
@@ -804,7 +810,7 @@ def block_record(cfg, args):
     with SclkSampler() as sc:
         for m in ("cola", "cola_m"):
             ms = timed_steps_median(step(m), args.sub_steps, args.sub_warmup)
-            rec["modes"][m] = {"ms_per_step": round(ms, 4), "tokens_per_s": round(T / (ms / 1e3), 1),
+            rec["modes"][m] = {"ms_per_step": step_ms(ms), "tokens_per_s": round(T / (ms / 1e3), 1),
                                "tflops": round((lin + attn) / (ms * 1e9), 2)}
     rec["sclk_mhz"] = sc.median()
     rec["power_w"] = sc.power()
@@ -983,7 +989,7 @@ def main():
         "n_gpus": 1,
         "steps": args.steps,
         "warmup": args.warmup,
-        "ms_per_step": round(ms, 4),
+        "ms_per_step": step_ms(ms),
         "higher_is_better": True,
         "scaling": "weak",
         "vs_baseline": None,
@@ -1005,22 +1011,22 @@ def main():
         # the target: 60 % of the bf16 dense MFMA peak on this block; how far
         # the step is from it, as a time ratio and in ms
         target_ms = flops_cola / (0.6 * peak * 1e9)
-        out["target"] = {"pct_of_peak": 60.0, "ms_per_step": round(target_ms, 4),
+        out["target"] = {"pct_of_peak": 60.0, "ms_per_step": step_ms(target_ms),
                          "step_over_target": round(ms / target_ms, 3), "ms_above_target": round(ms - target_ms, 4)}
     if "cola_median" in res:
         out["median_ms_per_step"] = {"steps": max(args.steps, 50), "warmup": 10,
-                                     "ms": round(res["cola_median"], 4),
+                                     "ms": step_ms(res["cola_median"]),
                                      "tflops": round(flops_cola / (res["cola_median"] * 1e9), 2)}
     if "cola_events" in res:
-        out["cola_with_kernel_events"] = {"ms_per_step": round(res["cola_events"], 4),
+        out["cola_with_kernel_events"] = {"ms_per_step": step_ms(res["cola_events"]),
                                           "tflops": round(flops_cola / (res["cola_events"] * 1e9), 2),
                                           "streams": 1}
     if "cola_m" in res:
-        out["cola_m"] = {"ms_per_step": round(res["cola_m"], 4),
+        out["cola_m"] = {"ms_per_step": step_ms(res["cola_m"]),
                          "tflops": round(flops_cola / (res["cola_m"] * 1e9), 2),
                          "tokens_per_s": round(T / (res["cola_m"] / 1e3), 1)}
     if "dense" in res:
-        out["dense"] = {"ms_per_step": round(res["dense"], 4),
+        out["dense"] = {"ms_per_step": step_ms(res["dense"]),
                         "tflops": round(flops_dense / (res["dense"] * 1e9), 2),
                         "tokens_per_s": round(T / (res["dense"] / 1e3), 1)}
         if "cola" in res:
@@ -1030,13 +1036,13 @@ def main():
         if dtype == "bf16" and "cola" in res and not args.only:
             # the same dense step on the vendor library, as context
             vms = vendor_dense_step_ms(args.workload)
-            out["dense_hipblaslt"] = {"ms_per_step": round(vms, 4),
+            out["dense_hipblaslt"] = {"ms_per_step": step_ms(vms),
                                       "tflops": round(flops_dense / (vms * 1e9), 2),
                                       "speedup_cola_vs_it": round(vms / res["cola"], 3),
                                       "how": "sum of per-shape medians of torch.matmul, 20 launches each"}
     if "fused" in res:
         # same algorithmic flops; q, k, v read one X and gate, up another
-        out["fused_block"] = {"ms_per_step": round(res["fused"], 4),
+        out["fused_block"] = {"ms_per_step": step_ms(res["fused"]),
                               "tflops": round(flops_cola / (res["fused"] * 1e9), 2),
                               "tokens_per_s": round(T / (res["fused"] / 1e3), 1),
                               "groups": ["q+k+v", "o", "gate+up", "down"]}
@@ -1044,7 +1050,7 @@ def main():
             out["fused_block"]["speedup_vs_dense"] = round(res["dense"] / res["fused"], 3)
     if "infer" in res:
         # forward only, nothing kept for a backward pass; grouped as fused_block
-        out["inference"] = {"ms_per_step": round(res["infer"], 4),
+        out["inference"] = {"ms_per_step": step_ms(res["infer"]),
                             "tflops": round(h.flops_infer / (res["infer"] * 1e9), 2),
                             "tokens_per_s": round(T / (res["infer"] / 1e3), 1)}
         if "dense_infer" in res:

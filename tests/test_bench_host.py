@@ -269,3 +269,34 @@ def test_power_sampler_reads_sensor_files(tmp_path):
     assert s.power() == {"median": 1200.0, "max": 1300.0, "cap": 1400.0, "samples": 3}
     s.pfiles = [str(tmp_path / "missing")]
     assert s.read_power() is None
+
+
+def test_line_s_value_is_its_flops_over_its_time(monkeypatch, capsys):
+    """The single fp32 layer takes some 0.06 ms a step: the printed time has to be fine enough
+    that the printed value follows from it to its own last digit.  The value is off by at most
+    half of 0.01; a half step of 5e-7 ms of the time moves v = flops / time by v 5e-7 / ms = v^2
+    2.5e-6, below 1e-4 for the values here (5 TFLOP/s at most)."""
+    from paper_2502_10940_amd import inputs as I
+    w = I.WORKLOADS[1]
+    flops = sum(6.0 * w["T"] * w["r"] * (a + b) for _, _, a, b in I.projections(1))
+
+    class Steps:
+        nstreams, projs, flops_cola, flops_dense = 1, [], flops, flops
+
+        def __init__(self, *a):
+            pass
+
+        def step(self, mode):
+            return None
+
+    monkeypatch.setattr(bench, "Harness", Steps)
+    monkeypatch.setattr(bench, "kernel_table", lambda cola: {})
+    argv = ["bench.py", "--workload", "1", "--no-dense", "--no-cola-m", "--no-cpu-baseline", "--no-block", "--no-workloads"]
+    monkeypatch.setattr(sys, "argv", argv)
+    for i in range(60):
+        ms = flops / 1e9 / (0.5 + 0.0749 * i)
+        monkeypatch.setattr(bench, "timed_steps", lambda *a: ms)
+        monkeypatch.setattr(bench, "timed_steps_median", lambda *a: ms)
+        bench.main()
+        d = json.loads(capsys.readouterr().out.splitlines()[-1])
+        assert abs(d["value"] - flops / (d["ms_per_step"] * 1e9)) <= 0.005 + 1e-4
