@@ -1002,6 +1002,51 @@ def test_two_graphs_of_trees_share_a_workspace():
             assert torch.equal(out, want) and torch.equal(lse, wl)
 
 
+@pytest.mark.parametrize("L, hd", [(0, 64), (0, 128), (1300, 64), (1300, 128)])
+def test_a_captured_tree_attention_follows_the_lengths(L, hd):
+    """One captured call whose own keys are cut by the lengths, replayed on other lengths, starts, tables and masks in
+    the same places: shorter and longer ones, empty requests, none at all.  The part's length, which the first launch
+    leaves in the workspace for the second, is each replay's own; eager work and synchronisations between them."""
+    from test_verify_abi import cut_by_lengths, tree_plan
+    b = TreeBatch(50 + hd, [40, 130, 7, 60], [7000, 2000, 5000, 60], L, 16, 16, hd, 64, pad=3)
+    d, c = b.desc()
+    n = cola.tree_attn_workspace_bytes(d, c)
+    plan = tree_plan(4, b.T, 16, 16, hd, L, b.max_kv, b.max_new, 64)
+    words = lambda: torch.from_numpy(W.words(b.masks, b.max_new)).to(DEV)
+    ptab, tab, kv, start, mask = i32(b.ptab) if L else None, i32(b.tab), i32(b.kv), i32(b.start), words()
+    out, lse = torch.zeros_like(b.q), torch.zeros((b.hq, b.T), device=DEV)
+    ws = torch.zeros(n, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cola.tree_attn(d, c, b.q, b.K, b.V, ptab, tab, kv, start, mask, out, lse, ws)
+    whole, rng, lengths = b.tab.copy(), np.random.default_rng(hd), set()
+    for new, old in (([40, 130, 7, 60], [7000, 2000, 5000, 60]), ([1, 2, 1, 3], [300, 64, 1, 3]), ([130, 0, 0, 100], [7000, 0, 0, 100]),
+                     ([0, 0, 0, 0], [0, 0, 0, 0]), ([7, 60, 130, 40], [65, 1999, 4000, 40]), ([40, 130, 7, 60], [7000, 2000, 5000, 60])):
+        b.new, b.kv = new, old
+        b.start = [0] + np.cumsum(new).tolist()
+        b.masks = [0] * b.T
+        for r, k in enumerate(new):
+            parent = W.random_tree(rng, k)
+            for i in range(k):
+                t = b.start[r] + i
+                b.masks[t] = (b.masks[b.start[r] + parent[i]] if parent[i] >= 0 else 0) | 1 << i
+        # pages that no token lies in are named by no one
+        b.tab = np.where(np.arange(whole.shape[1]) < -(-np.asarray(old)[:, None] // 64), whole, -1)
+        for to, x in ((tab, i32(b.tab)), (kv, i32(old)), (start, i32(b.start)), (mask, words())):
+            to.copy_(x)
+        out.fill_(7.0), lse.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        lengths.add(int(ws[-64:-60].view(torch.int32)[0]))
+        assert int(ws[-64:-60].view(torch.int32)[0]) == cut_by_lengths(plan, hd, 16, 1, L, b.max_new, b.max_kv, list(zip(new, old)))[0]
+        # bits: of the hundred tokens of one request forty were never written, and give NaN
+        want, wl = b.check() if old == [300, 64, 1, 3] else b.run()
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(lse.view(torch.int32), wl.view(torch.int32)), old
+        assert not torch.isnan(out[:b.start[3]].float()).any()
+    assert len(lengths) > 1
+
+
 def test_two_streams_verify_at_once():
     """Two programs on two streams, each with its own buffers: the serial results."""
     a, b = Verifier(6, 8, 2, 128, 16, 50, 100, 16), Verifier(6, 8, 2, 128, 16, 50, 100, 16, seed=5)

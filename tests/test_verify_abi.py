@@ -197,6 +197,61 @@ def test_gpu_tests_of_trees_run_every_kernel(hd):
     assert seen == every, (sorted(every - seen), sorted(seen - every))
 
 
+def cut_by_lengths(p, hd, hk, g, prefix, max_new, max_kv, lens):
+    """What the kernels make of lengths (rows, own tokens) on the GPU where they cut the own keys by them, step for step:
+    (the part's length, the item of each turn behind the prefix's or None)."""
+    stage, slots = 64, 512 if hd == 128 else 1024
+    tiles = [-(-min(n, max_new) * g // 128) for n, _ in lens]
+    ends = [min(kv, max_kv) for _, kv in lens]
+    parts = max(slots - sum(tiles) * hk // 2, slots // 2)
+    work = sum(t * -(-e // stage) for t, e in zip(tiles, ends)) * hk
+    if p.splits_p:
+        work += hk * p.tiles_p * -(-prefix // stage)
+    chunk = min(max(-(-work // parts) * stage, p.chunk_s), 1 << 30)
+    items = []
+    for r, (t, e) in enumerate(zip(tiles, ends)):
+        units = min(-(-e // chunk), p.splits_s) * hk
+        for j in range(units if t == 1 else -(-units // 8) * 8 * t):
+            unit, tile = (j, 0) if t == 1 else ((j >> 3) // t * 8 + (j & 7), (j >> 3) % t)
+            items.append((r, unit % hk, unit // hk, tile) if unit < units else None)
+    return chunk, items
+
+
+def test_trees_cut_by_their_lengths_fit_the_launch_and_the_workspace():
+    """Whatever the lengths: every item that the join reads has a turn of the launch, once, and its
+    part a place in the workspace.  Bounds near the lengths and far above them, launches of just under
+    half of the chip, several tiles to a request, empty requests and such that see nothing."""
+    rng = np.random.default_rng(5)
+    cut, most = 0, 0.0
+    for i in range(1500):
+        hd = int(rng.choice([64, 128]))
+        hk, g = int(rng.choice([1, 2, 4, 8, 16])), int(rng.choice([1, 2, 4, 8]))
+        full = 512 if hd == 128 else 1024
+        max_new = int(rng.integers(1, 257))
+        t_s = -(-max_new * g // 128)
+        n = int(min(256, max(1, (full // 2 - 1) // (t_s * hk)))) if i % 2 else int(rng.integers(1, 33))
+        longest = int(2 ** rng.uniform(8, 15))
+        max_kv = longest if i % 3 else int(min(1 << 20, longest * 2 ** rng.uniform(0, 8)))
+        prefix = int(rng.choice([0, 0, 1, 700, 5000]))
+        T = n * max_new + int(rng.integers(0, 5))
+        p = tree_plan(n, T, hk * g, hk, hd, prefix, max_kv, max_new)
+        if not (p.kind_s == 8 and p.splits_s > 1 and n * p.tiles_s * hk < full // 2):
+            continue
+        cut += 1
+        turns = full + n * p.tiles_s * hk + (8 * n * p.tiles_s if p.tiles_s > 1 else 0)       # the launch, without the prefix's
+        for spread in range(3):
+            rows = rng.integers(0, max_new + 9, n) if spread else np.full(n, max_new)
+            kv = (longest * rng.random(n) ** spread).astype(int) + 1
+            chunk, items = cut_by_lengths(p, hd, hk, g, prefix, max_new, max_kv, list(zip(rows.tolist(), kv.tolist())))
+            assert chunk % 64 == 0 and len(items) <= turns
+            most = max(most, len(items) / turns)
+            there = [x for x in items if x is not None]
+            want = {(r, h, s, t) for r in range(n) for h in range(hk) for s in range(-(-min(int(kv[r]), max_kv) // chunk))
+                    for t in range(-(-min(int(rows[r]), max_new) * g // 128))}
+            assert len(there) == len(set(there)) and set(there) == want and all(x[2] < p.splits_s for x in there)
+    assert cut > 300 and most > 0.9
+
+
 # ---- logits ----
 
 def test_logits_refusals():
