@@ -165,7 +165,6 @@ constexpr int64_t kWideAlongKeys = 1024, kWideAlongBytes = 150000000;
 constexpr int64_t kWideOwn = 48;           // blocks of KB own keys in a part of several requests' chunks
 constexpr int64_t kWideOwnBytes = 128000000;  // of partial rows, where these parts are more than the chip needs
 constexpr int64_t kWideOwnTurns = 1 << 16;   // workgroups up to which there are such parts: 1.3 ns for each that has no rows
-constexpr int64_t kTreeOwn = 8;            // the same where they are cut by the lengths, at the least
 constexpr int64_t kPrefixOwn = 32;         // least blocks of a part of the prefix that is cut against a loose max_kv
 constexpr int64_t kMaxGrid = 1 << 23;      // workgroups (2^32 threads are the limit)
 constexpr int kRound = 64;                 // parts end where a stage of any kernel does
@@ -265,7 +264,7 @@ PrefixAttnPlan plan_of(const PrefixAttnShape& sh, bool tree) {
     parts(sh.prefix, chunk_p, false, &p.splits_p, &p.chunk_p);
     int64_t own = chunk;
     // Few requests' trees are cut by their lengths on the GPU (counted_item); these parts
-    // are the least, and say how many the workspace has room for.  8 requests of up to
+    // say how many the workspace has room for.  8 requests of up to
     // 32000 keys, 64 nodes of 32 heads over 8 of 128: 175 us against 205 with parts of 1536;
     // 4 of up to 8000, 200 nodes: 71 against 78.  Where the tiles fill half of the chip as
     // they are it costs more than it gives (32 of up to 4000, 32 nodes: 75 against 72).

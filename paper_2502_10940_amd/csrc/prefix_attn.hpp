@@ -921,17 +921,20 @@ __host__ __device__ constexpr int64_t turns(int64_t units, int tiles) { return t
 // the lengths of all requests, at most 256, a wave's lanes four each, and comes to the
 // same list: parts as long as gives a.slots workgroups, what they all do shared out
 // evenly, with the half part that each tile ends with on the average, and no shorter
-// than the plan's, which the workspace is sized for; then the requests' items one after
-// the other, a unit's tiles eight turns apart (turn_of).  So no workgroup is spent on
-// parts that are not there, whatever max_kv is.
+// than leaves the longest request as many as the workspace has room for; then the
+// requests' items one after the other, a unit's tiles eight turns apart (turn_of).  So
+// no workgroup is spent on parts that are not there, and max_kv decides how many parts
+// there may be, not where they end (8 requests of up to 32000 keys, 64 nodes, 32 heads
+// over 8 of 128: 166 us under a max_kv of 2^20, too, where 19 parts of it took 680).
 constexpr int kCounted = 256;
+constexpr int64_t kTreeOwn = 8;            // blocks of KB keys that such a part has at the least
 struct Counted {
     int r, head, split, tile, chunk;       // r < 0: past the last item
 };
 __device__ __forceinline__ Counted counted_item(const Args& a, int64_t turn) {
     constexpr int PER = kCounted / 64;
     const int lane = threadIdx.x & 63;
-    int tiles[PER], end[PER], all = 0;
+    int tiles[PER], end[PER], all = 0, longest = 0;
     int64_t work = 0;
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
@@ -940,17 +943,20 @@ __device__ __forceinline__ Counted counted_item(const Args& a, int64_t turn) {
         tiles[q] = r < a.n_req ? (s.n * a.g + WROWS - 1) / WROWS : 0;
         end[q] = s.end;
         all += tiles[q];
+        longest = max(longest, tiles[q] > 0 ? s.end : 0);
         work += (int64_t)tiles[q] * ((s.end + STG - 1) / STG);
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) {
         work += __shfl_xor(work, d);
         all += __shfl_xor(all, d);
+        longest = max(longest, __shfl_xor(longest, d));
     }
     work = uniform64(work) * a.hk + a.work_p;
     const int64_t parts = max(a.slots - (int64_t)uniform(all) * a.hk / 2, (int64_t)a.slots / 2);
     Counted c;
-    c.chunk = (int)min(max((work + parts - 1) / parts * STG, (int64_t)a.chunk_s), (int64_t)1 << 30);
+    const int least = max(((uniform(longest) + a.splits_s - 1) / a.splits_s + STG - 1) / STG * STG, a.chunk_s);
+    c.chunk = (int)min(max((work + parts - 1) / parts * STG, (int64_t)least), (int64_t)1 << 30);
     int64_t items[PER], mine = 0;
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
@@ -1097,6 +1103,7 @@ inline Args args_of(const PrefixAttnShape& sh, const PrefixAttnPlan& p, const Pr
     // parts as counted_item cuts them are at most the slots and one for each tile, and a
     // request's units are filled up to whole rounds of eight
     const int64_t base_s = sh.n_req * p.tiles_s * sh.hk;
+    if (a.slots > 0 && a.chunk_s > kTreeOwn * KB) a.chunk_s = kTreeOwn * KB;
     if (a.slots > 0) a.blocks = a.items_p + a.slots + base_s + (p.tiles_s > 1 ? 8 * sh.n_req * p.tiles_s : 0);
     a.work_p = a.units_p / (p.splits_p > 0 ? p.splits_p : 1) * p.tiles_p * ((sh.prefix + STG - 1) / STG);
     a.chunk = reinterpret_cast<int32_t*>(a.part ? a.part + n * sh.hd : nullptr);

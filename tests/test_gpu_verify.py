@@ -454,6 +454,23 @@ def test_tree_attention_cut_by_the_lengths(name, hd):
     TreeBatch(40 + hd, new, kv, L, hq, hk, hd, 64, masks="any", max_kv=max_kv, pad=3).check()
 
 
+@pytest.mark.parametrize("hd", (64, 128))
+def test_far_bounds_cut_trees_where_near_ones_do(hd):
+    """A max_kv far above the lengths (a program's context length): the parts end where the lengths say, as under a bound
+    that is the longest length, as long as the workspace has room for them."""
+    cut = []
+    for max_kv in (7000, 1 << 20):
+        b = TreeBatch(60 + hd, [40, 100, 7], [5000, 300, 7000], 0, 2, 1, hd, 64, max_kv=max_kv)
+        b.check()
+        d, c = b.desc()
+        ws = torch.zeros(cola.tree_attn_workspace_bytes(d, c), dtype=torch.uint8, device=DEV)
+        out, lse = torch.empty_like(b.q), torch.empty((b.hq, b.T), device=DEV)
+        cola.tree_attn(d, c, b.q, b.K, b.V, None, i32(b.tab), i32(b.kv), i32(b.start), torch.from_numpy(W.words(b.masks, b.max_new)).to(DEV), out, lse, ws)
+        cut.append((int(ws[-64:-60].view(torch.int32)[0]), out, lse))
+    assert cut[0][0] == cut[1][0] == 256
+    assert torch.equal(cut[0][1], cut[1][1]) and torch.equal(cut[0][2], cut[1][2])
+
+
 def test_tree_attention_without_starts_pitches_and_scale():
     b = TreeBatch(1, [1] * 9, [4, 0, 17, 60, 33, 1, 16, 100, 12], 40, 4, 2, 64, 16, pad=3, ldq=4 * 64 + 24, ldo=4 * 64 + 8, scale=0.3)
     a, la = b.check()

@@ -207,10 +207,13 @@ def cut_by_lengths(p, hd, hk, g, prefix, max_new, max_kv, lens):
     work = sum(t * -(-e // stage) for t, e in zip(tiles, ends)) * hk
     if p.splits_p:
         work += hk * p.tiles_p * -(-prefix // stage)
-    chunk = min(max(-(-work // parts) * stage, p.chunk_s), 1 << 30)
+    longest = max([e for t, e in zip(tiles, ends) if t] + [0])
+    up = lambda x, n: -(-x // n)
+    least = max(up(up(longest, p.splits_s), stage) * stage, min(p.chunk_s, 256))
+    chunk = min(max(-(-work // parts) * stage, least), 1 << 30)
     items = []
     for r, (t, e) in enumerate(zip(tiles, ends)):
-        units = min(-(-e // chunk), p.splits_s) * hk
+        units = min(-(-e // chunk), p.splits_s) * hk if t else 0
         for j in range(units if t == 1 else -(-units // 8) * 8 * t):
             unit, tile = (j, 0) if t == 1 else ((j >> 3) // t * 8 + (j & 7), (j >> 3) % t)
             items.append((r, unit % hk, unit // hk, tile) if unit < units else None)
