@@ -557,8 +557,8 @@ int cola_norm_rope_fwd(const cola_rope_desc* desc, double eps, const void* q, co
  * desc as in the forward: dq_out and dk_out have the pitches ldqo and ldko; q, dq, k and
  * dk have ldq and ldk.  dq may be q or dq_out, dk may be k or dk_out (same pointer and
  * pitch).  dg_q and dg_k (fp32 [head_dim]) are overwritten, zeros for T = 0; NULL: not
- * wanted.  They are summed in a fixed order.  ws: scratch that holds nothing between
- * calls, 4-byte aligned. */
+ * wanted, and where there are no such heads.  They are summed in a fixed order.  ws:
+ * scratch that holds nothing between calls, 4-byte aligned. */
 size_t cola_norm_rope_workspace_bytes(const cola_rope_desc* desc);
 int cola_norm_rope_bwd(const cola_rope_desc* desc, double eps, const void* dq_out, const void* dk_out, const void* q,
                        const void* k, const void* g_q, const void* g_k, const int32_t* positions, void* dq, void* dk,
@@ -610,7 +610,10 @@ int cola_tree_map(const cola_tree_map_desc* desc, const int32_t* parent, const i
  * keys kv_len[r] - n + j, a row t sees those whose bit j is set in mask[t][..] (W =
  * ceil(max_new / 64) words a row, 8-byte aligned; bits from n on count for nothing).  Any
  * masks are taken: a row may not see itself, or nothing at all (out = 0, lse = -inf).
- * max_new is at most COLA_TREE_MAX. */
+ * max_new is at most COLA_TREE_MAX.  Where few requests have many rows their keys are cut
+ * by the lengths of all requests of the call: the data that a row's last bits depend on
+ * has the other requests' kv_len and start in it, and a max_kv far above the lengths costs
+ * nothing as long as the workspace has room for their parts. */
 size_t cola_tree_attn_workspace_bytes(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache);
 int cola_tree_attn(const cola_prefix_attn_desc* desc, const cola_cache_desc* cache, const void* q, const void* K,
                    const void* V, const int32_t* prefix_table, const int32_t* table, const int32_t* kv_len,

@@ -15,11 +15,14 @@
 // so that no wave waits for another between the rows.
 //
 // 980 rows of 128003 bf16 logits of 40 requests, histories of up to 8000 tokens, 200 biases
-// each and masks for the rows (533 MB): 142 us, 3.8 TB/s; without rules 88 us, 6.0 TB/s.
-// What is between is the counting (a third: 66 workgroups of a request read its history), the
+// each and masks for the rows (533 MB): 141 us, 3.8 TB/s (three sets of tensors in turn);
+// without rules 115 us, 4.4 TB/s: rows of 128003 begin off their lines.
+// What is between is the counting (66 workgroups of a request read its history), the
 // masks' bits and the vectors that hold tokens of the history, nearly all here (21 vector
 // instructions a logit, which take 52 % of the launch).  One row of 32000 fp32 logits: 5.4
-// us, a launch and five loads one after the other.
+// us, a launch and five loads one after the other.  256 rows of requests of their own (138
+// MB): 77 us, 1.8 TB/s: each of a row's 32 workgroups reads the request's history and builds
+// its chunk's counts for one row; fp32 (269 MB) 91.
 #include "rows.hpp"
 #include "serve.hpp"
 
@@ -90,8 +93,11 @@ struct Draft {
     uint32_t seen, answer;
 };
 
-// PV NVEC elements of a row to a thread; PAST: results past the caches (980 rows of 128003:
-// 121 us against 128).
+// PV NVEC elements of a row to a thread; PAST: results past the caches, which leaves them to
+// the inputs (256 rows of 128003 bf16 logits, one to a request, 138 MB: 78 us against 85; 980
+// rows of 32000: 56 against 60; 980 of 128000: 132 either way).  Where rows begin off their
+// lines it costs more than it gives at larger sizes (980 of 128003: 142 against 138, fp32
+// 235 against 225).
 template <bool BF16, int NVEC, bool PAST>
 __global__ __launch_bounds__(NTHR) void logits_kernel(const LogitsArgs a, const int rows, const int chunks, const int64_t base) {
     constexpr int PV = BF16 ? 8 : 4, CW = 64 * PV * NVEC, C = CW * NTHR / 64;
@@ -419,9 +425,12 @@ hipError_t go(const LogitsArgs& a, int rows, bool past, hipStream_t s) {
 hipError_t launch_logits(bool bf16, const LogitsArgs& a, hipStream_t s) {
     // Chunks of up to 4096 tokens (32 KB of LDS, four workgroups a CU) as large as leave 1024
     // workgroups of one row, and rows to a workgroup (of one request, so as many as it may
-    // have) while there are 2048: the rows of a request share its counts (980 rows, chunks of
-    // 4096: 333 us with one row, 155 with 4, 129 with 8, 121 with 16; chunks of 2048 349, 158,
-    // 130 and 124; 256 rows of requests of their own 78 against 93).
+    // have) while there are 2048: the rows of a request share its counts (980 rows of 128003
+    // of 40 requests, all rules, two sets of tensors in turn, chunks of 4096: 345 us with one
+    // row, 158 with 4, 134 with 8, 130 with 16; chunks of 2048 361, 163, 134 and 130; 256 rows
+    // of requests of their own 77 against 92).  max_new only bounds a request's rows: where
+    // most have one, a workgroup counts for several requests in turn, which costs nothing
+    // (980 requests of one row, none drafted, max_new 48: 284 us against 295 with max_new 1).
     const int pv = NTHR * (bf16 ? 8 : 4), most = bf16 ? 2 : 4;
     int nvec = 1;
     while (nvec < most && a.T * ((a.V + 2 * pv * nvec - 1) / (2 * pv * nvec)) >= 1024) nvec *= 2;

@@ -9,15 +9,20 @@
 // rows of 32 + 32 heads of 64 (537 MB, 805 MB): forward 106 us, backward 164 us, 5.1 and 4.9
 // TB/s, where a large copy reaches 5.1; 8191 rows of 32 + 8 heads of 128 of which half turn,
 // interleaved (252 MB): backward 67 us, 3.8 TB/s, the vector unit busy for 40 % of it (the
-// row's cosines, formed by every group, are a third of its work); 1536 rows of 32 + 8 into
-// the cache (37 MB): 11.9 us.  256 rows: 5.2 us forward, a launch; backward 12, two of them.
+// row's cosines, formed by every group, are a third of its work), and the last quarter
+// of its workgroups alone on the chip; 1536 rows of 32 + 8 into the cache (37 MB): 11.9 us.
+// fp32: gradients of 8191 rows of 32 + 8 heads of 128 (503 MB) 104 us, 4.9 TB/s; 6001 such
+// rows into the cache (295 MB) 70 us, 4.2 TB/s.  256 rows: 5.2 us forward, a launch;
+// backward 12, two of them.
 //
 // A head is a group of L lanes (a power of two, 64 at most), a lane one unit of it as
 // in rope.hip (MU of them where a head has more than 64): a pair of vectors that turn
 // into each other, so that the rotation stays in the lane and the mean is the only
-// thing that the group exchanges (log2 L steps between registers).  The rest is the
-// rotation's: a row's groups share out its heads, loads of several heads are in
-// flight before the cosines are formed.
+// thing that the group exchanges (log2 L steps between registers).  Heads that are no
+// power of two leave lanes idle, three of eight at 80, two at 96: 16000 rows of 20 + 5
+// heads of 80 (128 MB, 192 MB) take 34 us forward, 3.8 TB/s, and 69 backward, 2.8.  The
+// rest is the rotation's: a row's groups share out its heads, loads of several heads are
+// in flight before the cosines are formed.
 //
 // dg is summed in a fixed order: a thread over its rows and heads, the groups of a
 // workgroup, and the workgroups (at most kParts of them) in a second launch.

@@ -890,9 +890,9 @@ __device__ __forceinline__ void wide_item(const Args& a, char* lds, const int32_
 }
 
 // Kinds of tiles: 16 or 32 rows whose keys a workgroup's waves share (ONE, TWO); 128
-// rows against keys in LDS (WIDE); for trees 64 rows as ONE and TWO, too (FOUR).  On the requests' own keys, where each has one
-// token, all rows of a tile see the same: ONE becomes FLAT, or SOLO with a tile to
-// a wave.
+// rows against keys in LDS (WIDE); for trees 64 rows as ONE and TWO, too (FOUR).  On the
+// requests' own keys, where each has one token, all rows of a tile see the same: ONE
+// becomes FLAT, or SOLO with a tile to a wave.
 // Behind a short prefix there are no tiles for it: each request's own items take its
 // keys ALONG, and nothing is left to join.
 enum Kind : int { ONE = 1, TWO = 2, SOLO = 3, FLAT = 4, ALONG = 5, FOUR = 6, WIDE = 8 };
@@ -1019,7 +1019,9 @@ __device__ __forceinline__ void any_item(const Args& a, char* lds, const int32_t
 }
 
 // NP, NS: kinds of the tiles on the prefix and on the requests' own keys.
-// SEE: causal, or trees.  COUNTED: the own keys are cut by the lengths.
+// SEE: causal, or trees.  COUNTED: the own keys are cut by the lengths.  Wide tiles of trees
+// at heads of 64 are held to 128 registers, four waves a SIMD (COUNTED at the price of two
+// registers spilled, 12 bytes of scratch a lane).
 template <int HD, int NP, int NS, int SEE, bool COUNTED>
 __global__ __launch_bounds__(NTHR, (SEE == SEE_TREE && HD == 64 && NS == WIDE ? 4 : NP == WIDE || NS == WIDE || NS == FOUR ? 2 : 1)) void prefix_attn_kernel(const Args a) {
     constexpr int LDS = kLdsBytes<HD, NP> > kLdsBytes<HD, NS> ? kLdsBytes<HD, NP> : kLdsBytes<HD, NS>;
